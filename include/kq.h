@@ -24,6 +24,12 @@
  *   kq_reconstruct       end of Sec. 3.2: recover the weight tensor from codebook + indices.
  *   kq_compress_stack    all of the above for the layers of a network in one call.
  *   kq_forgy_select      the k-means initialisation (k distinct kernels in a seeded order).
+ *   kq_quantize_groups   a fully-connected layer in 4 bits with group scales; kq_group_linear and
+ *                        kq_group_linear_grad_input run it from its codes, forwards and backwards.
+ *   kq_checkpoint_pack   an activation in 8 bits, kept for the backward pass;
+ *                        kq_checkpoint_grad_scales and kq_checkpoint_grad_weight take the
+ *                        gradients of the group scales (Eq. 2's idea: a shared value moves with
+ *                        the gradients of what it stands for) or of the whole weight from it.
  *   kq_accounting        Eq. (4), (6), (7): storage bits, compression ratio, bits per parameter.
  *
  * Conventions shared by every call
@@ -66,7 +72,7 @@ extern "C" {
 typedef enum kq_status {
     KQ_OK = 0,
     KQ_ERR_ARG = 1,          /* null pointer, bad size, misaligned pointer */
-    KQ_ERR_UNSUPPORTED = 2,  /* dim != 9, k above KQ_MAX_K, bits outside 1..16 */
+    KQ_ERR_UNSUPPORTED = 2,  /* dim != 9, k above KQ_MAX_K, bits outside 1..16, group, type or size not served */
     KQ_ERR_WORKSPACE = 3,    /* workspace missing, too small or misaligned */
     KQ_ERR_RANGE = 4,        /* KQ_F_VALIDATE: a kernel (or gradient) value is NaN or infinite */
     KQ_ERR_HIP = 5           /* a HIP runtime call failed */
@@ -579,6 +585,92 @@ size_t kq_fit_layer_noalloc_max_bytes(void);
 kq_status kq_fit_layer_noalloc(const float* X, int64_t n, int32_t dim, int32_t k, const float* C_init, int32_t iters,
                                float* C, int32_t* idx, int32_t* counts, double* distortion, uint32_t flags,
                                void* stream);
+
+/*
+ * Fully-connected layers in 4 bits with group scales.
+ *
+ *   W_hat[o][c] = scales[o][c / group] * L[code[o][c]],  o < n output, c < k input features.
+ *   scales device [n][ceil(k / group)] bf16; group 32, 64 or 128 (else KQ_ERR_UNSUPPORTED).
+ *   L: levels == NULL for the integers -8 .. 7, or a device table of 16 bf16 levels in
+ *   ascending order (for instance those kq_quantize_scalars finds with 4 bits), finite, one of
+ *   them not zero.  Levels have to lie in fp16's range where the activations are fp16.
+ *   codes: kq_group_code_bytes(n, k) bytes, 16-byte aligned: tiles of 16 rows by 128 columns of
+ *   1 KB, [ceil(n / 16)][ceil(k / 128)][16][64].  In a row's 64 bytes, dword 4 q + i (little
+ *   endian) holds columns 32 i + 8 q + 0 .. 7, column j of them in bits 4 b .. 4 b + 3 with
+ *   b = (j & 1) * 4 + j / 2.  Rows and columns past the matrix hold 0.
+ *   1 <= n, k <= KQ_GROUP_MAX_FEATURES, and no matrix of a call has more than
+ *   KQ_GROUP_MAX_VALUES values (else KQ_ERR_UNSUPPORTED).
+ *   Types are KQ_T_*; matrices are row-major with a row pitch in elements (ld >= the columns),
+ *   aligned to their type.  Activations are bf16 or fp16 (fp32: KQ_ERR_UNSUPPORTED), in the
+ *   type of the output; 0 <= m <= KQ_GROUP_MAX_ROWS rows, and m = 0 writes nothing (gradients
+ *   of parameters are zero then).
+ *
+ * kq_quantize_groups -- codes and scales of W (device [n][k], any KQ_T_* type):
+ *   a = max |w| of the group; scale = bf16(fp32(a / top)), top = 7 or the largest |level|, 0 where
+ *   that is below 2^-126; code = the level nearest to fp32(w / scale) (0 where the scale is 0),
+ *   the lower one where two are as near (t is compared with the fp32 midpoints of neighbours).
+ *   A group with an infinity or NaN gets a NaN scale: all of it reconstructs to NaN.
+ * kq_reconstruct_groups -- W_hat in any KQ_T_* type, fp32 products rounded once.
+ * kq_group_linear -- Y[m][n] = X[m][k] W_hat^T + bias (fp32 [n], or NULL).  Sums in fp32.  For up to 16
+ *   rows of X the levels multiply X exactly and a group's fp32 sum takes the scale; beyond, the weights
+ *   are rounded to the type of X first.  An infinity in X makes its row of Y infinite or NaN, as do
+ *   values of 2^122 and more.  A row of Y depends on its row of X and on m alone, not on other rows.
+ * kq_group_linear_grad_input -- dX[m][k] = dY[m][n] W_hat, the weights rounded to the type of dY.
+ *   workspaces: the *_workspace_bytes of the same m, n, k (may be 0: ws may be NULL then).
+ */
+#define KQ_T_F32 0
+#define KQ_T_BF16 1
+#define KQ_T_F16 2
+#define KQ_GROUP_MAX_FEATURES (1 << 24)
+#define KQ_GROUP_MAX_VALUES ((int64_t)1 << 36)
+#define KQ_GROUP_MAX_ROWS (1 << 30)
+size_t kq_group_code_bytes(int64_t n, int64_t k);
+kq_status kq_quantize_groups(const void* W, int32_t type, int64_t ldw, int64_t n, int64_t k, int32_t group,
+                             const void* levels, uint8_t* codes, void* scales, void* stream);
+kq_status kq_reconstruct_groups(const uint8_t* codes, const void* scales, const void* levels, int64_t n, int64_t k,
+                                int32_t group, int32_t type, void* W_hat, int64_t ldw, void* stream);
+size_t kq_group_linear_workspace_bytes(int64_t m, int64_t n, int64_t k);
+kq_status kq_group_linear(const void* X, int32_t type, int64_t ldx, int64_t m, int64_t n, int64_t k,
+                          const uint8_t* codes, const void* scales, const void* levels, int32_t group,
+                          const float* bias, void* Y, int64_t ldy, void* ws, size_t ws_bytes, void* stream);
+size_t kq_group_linear_grad_input_workspace_bytes(int64_t m, int64_t n, int64_t k);
+kq_status kq_group_linear_grad_input(const void* dY, int32_t type, int64_t ldy, int64_t m, int64_t n, int64_t k,
+                                     const uint8_t* codes, const void* scales, const void* levels, int32_t group,
+                                     void* dX, int64_t ldx, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Activation checkpoints in 8 bits, and the gradients taken from them.
+ *
+ *   Groups of KQ_CHECKPOINT_GROUP neighbours of a row share a power of two: with
+ *   E = floor(log2 max |x|), e = max(E - 6, -126) (fp16 inputs: at least -24),
+ *   q = rint(x 2^-e) clipped to [-127, 127] and x_hat = q 2^e, which bf16 holds exactly (and
+ *   fp16, for fp16 inputs).  |x - x_hat| is at most half a step 2^e, or one step where |x| is
+ *   above 127.5 of them.  A group with an infinity or NaN is NaN when it is read.
+ *   q device [m][kq] int8, 16-byte aligned, kq = k rounded up to the group (zeros past k);
+ *   exps device [m][kq / KQ_CHECKPOINT_GROUP] uint8: e + 127, or 255 for NaN.
+ *
+ * kq_checkpoint_pack, kq_checkpoint_restore -- X [m][k] of any KQ_T_* type, with a row pitch.
+ * kq_checkpoint_grad_weight -- dW[o][c] = sum_m dY[m][o] x_hat[m][c], fp32 [n][k] with row pitch
+ *   lddw.
+ * kq_checkpoint_grad_scales -- dscales[o][g] = sum over the group's columns of L[code] dW, fp32
+ *   [n][ceil(k / group)]; dW is never written.
+ *   dbias (fp32 [n], or NULL): sum_m dY[m][o].  dY bf16 or fp16; an fp16 dY needs a checkpoint
+ *   whose values fp16 can hold.  Sums in fp32, in an order that the sizes alone decide.
+ *   workspace: kq_checkpoint_grad_workspace_bytes(m, n, k, group), group 0 for the weight's.
+ */
+#define KQ_CHECKPOINT_GROUP 32
+kq_status kq_checkpoint_pack(const void* X, int32_t type, int64_t ldx, int64_t m, int64_t k, int8_t* q, uint8_t* exps,
+                             void* stream);
+kq_status kq_checkpoint_restore(const int8_t* q, const uint8_t* exps, int64_t m, int64_t k, int32_t type, void* X_hat,
+                                int64_t ldx, void* stream);
+size_t kq_checkpoint_grad_workspace_bytes(int64_t m, int64_t n, int64_t k, int32_t group);
+kq_status kq_checkpoint_grad_scales(const void* dY, int32_t type, int64_t ldy, int64_t m, int64_t n, int64_t k,
+                                    const int8_t* q, const uint8_t* exps, const uint8_t* codes, const void* levels,
+                                    int32_t group, float* dscales, float* dbias, void* ws, size_t ws_bytes,
+                                    void* stream);
+kq_status kq_checkpoint_grad_weight(const void* dY, int32_t type, int64_t ldy, int64_t m, int64_t n, int64_t k,
+                                    const int8_t* q, const uint8_t* exps, float* dW, int64_t lddw, float* dbias,
+                                    void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -12,7 +12,10 @@ Entry points (same names as the C ABI):
   kq_fit_layer_yinyang (and the Yinyang class over kq_yinyang_init / kq_yinyang_assign),
   kq_codebook_grad_step, kq_codebook_grad_step_stack, kq_quantize_scalars, kq_search_codebook_size,
   kq_quantize_codebook, kq_quantize_codebook_stack, kq_pack_bits, kq_unpack_bits,
-  kq_reconstruct, kq_reconstruct_packed.
+  kq_reconstruct, kq_reconstruct_packed;
+  fully-connected layers in 4 bits: kq_quantize_groups, kq_reconstruct_groups, kq_group_linear,
+  kq_group_linear_grad_input; 8-bit activations: kq_checkpoint_pack, kq_checkpoint_restore,
+  kq_checkpoint_grad_scales, kq_checkpoint_grad_weight; GroupLinear, a layer over them.
 """
 from __future__ import annotations
 
@@ -105,6 +108,20 @@ def _load():
         "kq_index_bits": ([_I32], _I32),
         "kq_accounting": ([_I64, _I32, _I32, _I32, _P, _P, _P], _I32),
         "kq_forgy_select": ([_P, _I64, _I32, _I32, ctypes.c_uint64, _P], _I32),
+        "kq_group_code_bytes": ([_I64, _I64], _SZ),
+        "kq_quantize_groups": ([_P, _I32, _I64, _I64, _I64, _I32, _P, _P, _P, _P], _I32),
+        "kq_reconstruct_groups": ([_P, _P, _P, _I64, _I64, _I32, _I32, _P, _I64, _P], _I32),
+        "kq_group_linear_workspace_bytes": ([_I64, _I64, _I64], _SZ),
+        "kq_group_linear": ([_P, _I32, _I64, _I64, _I64, _I64, _P, _P, _P, _I32, _P, _P, _I64, _P, _SZ, _P], _I32),
+        "kq_group_linear_grad_input_workspace_bytes": ([_I64, _I64, _I64], _SZ),
+        "kq_group_linear_grad_input": ([_P, _I32, _I64, _I64, _I64, _I64, _P, _P, _P, _I32, _P, _I64, _P, _SZ, _P],
+                                       _I32),
+        "kq_checkpoint_pack": ([_P, _I32, _I64, _I64, _I64, _P, _P, _P], _I32),
+        "kq_checkpoint_restore": ([_P, _P, _I64, _I64, _I32, _P, _I64, _P], _I32),
+        "kq_checkpoint_grad_workspace_bytes": ([_I64, _I64, _I64, _I32], _SZ),
+        "kq_checkpoint_grad_scales": ([_P, _I32, _I64, _I64, _I64, _I64, _P, _P, _P, _P, _I32, _P, _P, _P, _SZ, _P],
+                                      _I32),
+        "kq_checkpoint_grad_weight": ([_P, _I32, _I64, _I64, _I64, _I64, _P, _P, _P, _I64, _P, _P, _SZ, _P], _I32),
         "kq_fit_layer_noalloc_max_bytes": ([], _SZ),
         "kq_fit_layer_noalloc": ([_P, _I64, _I32, _I32, _P, _I32, _P, _P, _P, _P, _U32, _P], _I32),
     }
@@ -142,8 +159,14 @@ EXPORTED = ["kq_status_string", "kq_abi_version", "kq_workspace_bytes", "kq_stac
             "kq_codebook_grad_step", "kq_codebook_grad_step_stack", "kq_quantize_scalars_workspace_bytes",
             "kq_quantize_scalars", "kq_search_workspace_bytes", "kq_search_codebook_size",
             "kq_compress_workspace_bytes", "kq_compress_stack", "kq_index_bits", "kq_accounting",
-            "kq_forgy_select", "kq_fit_layer_noalloc_max_bytes", "kq_fit_layer_noalloc"]
+            "kq_forgy_select", "kq_fit_layer_noalloc_max_bytes", "kq_fit_layer_noalloc",
+            "kq_group_code_bytes", "kq_quantize_groups", "kq_reconstruct_groups", "kq_group_linear_workspace_bytes",
+            "kq_group_linear", "kq_group_linear_grad_input_workspace_bytes", "kq_group_linear_grad_input",
+            "kq_checkpoint_pack", "kq_checkpoint_restore", "kq_checkpoint_grad_workspace_bytes",
+            "kq_checkpoint_grad_scales", "kq_checkpoint_grad_weight"]
 KQ_MAX_PACK_JOBS = 32
+KQ_T_F32, KQ_T_BF16, KQ_T_F16 = 0, 1, 2
+KQ_CHECKPOINT_GROUP = 32
 
 
 class KqError(RuntimeError):
@@ -871,3 +894,269 @@ def kq_compress_stack(comp: Compression, validate: bool = False, round_events=No
     _check(lib.kq_compress_stack(ctypes.cast(comp.layers, _P), comp.n_layers, comp.iters, comp.mode, comp.bits,
                                  comp.cbq_iters, KQ_F_VALIDATE if validate else 0, ev, comp.ws.data_ptr(),
                                  comp.ws.numel(), _stream(comp.device)), "kq_compress_stack")
+
+
+# ---- fully-connected layers in 4 bits, activations in 8 ---------------------------------------
+
+_TYPES = {torch.float32: KQ_T_F32, torch.bfloat16: KQ_T_BF16, torch.float16: KQ_T_F16}
+_ACTS = {torch.bfloat16: KQ_T_BF16, torch.float16: KQ_T_F16}
+
+
+def _rows(t, types, name, cols=None):
+    """A matrix of rows for the library: (tensor [m, cols], its type, row pitch).  Rows may be strided; a row's
+    values are neighbours.  Leading dimensions (or none, a single row) are flattened where that needs no copy."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    ty = types.get(t.dtype)
+    if ty is None:
+        raise TypeError(f"{name} must be one of {', '.join(str(d) for d in types)}, got {t.dtype}")
+    if t.dim() != 2:
+        if t.dim() == 0 or not t.is_contiguous():
+            raise ValueError(f"{name} must be a matrix, a vector, or contiguous")
+        t = t.view(-1, t.shape[-1])
+    m, k = t.shape
+    if cols is not None and k != cols:
+        raise ValueError(f"{name} must have {cols} columns, got {k}")
+    if k == 0:
+        raise ValueError(f"{name} must have columns")
+    ld = t.stride(0) if m > 1 else k
+    if (k > 1 and t.stride(1) != 1) or ld < k:
+        raise ValueError(f"{name} must have rows of neighbouring values that do not overlap")
+    return t, ty, ld
+
+
+def _same_device(dev, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, not on {dev}")
+
+
+def _levels(levels):
+    return levels if levels is None else _dev(levels, torch.bfloat16, "levels", (16,))
+
+
+def _groups(k: int, group: int) -> int:
+    if group not in (32, 64, 128):
+        raise ValueError(f"group must be 32, 64 or 128, got {group}")
+    return -(-k // group)
+
+
+def group_codes_shape(n: int, k: int):
+    """Shape of the packed codes of an [n, k] weight: 1 KB tiles of 16 rows by 128 columns."""
+    return (-(-n // 16), -(-k // 128), 16, 64)
+
+
+def kq_quantize_groups(W, group: int = 128, levels=None, codes=None, scales=None):
+    """4-bit codes of a weight matrix (fp32, bf16 or fp16, rows may be strided) with a bf16 scale for `group`
+    neighbouring columns.  levels: None for -8 .. 7 or 16 ascending bf16 levels.  Returns (codes uint8 packed,
+    scales bfloat16 [n, ceil(k / group)]); include/kq.h has the formulas and the layout."""
+    W, ty, ld = _rows(W, _TYPES, "W")
+    n, k = W.shape
+    dev = W.device
+    G = _groups(k, group)
+    levels = _levels(levels)
+    shape = group_codes_shape(n, k)
+    if n == 0:
+        raise ValueError("W must have rows")
+    codes = torch.empty(shape, dtype=torch.uint8, device=dev) if codes is None else _dev(codes, torch.uint8, "codes", shape)
+    scales = torch.empty(n, G, dtype=torch.bfloat16, device=dev) if scales is None else _dev(scales, torch.bfloat16, "scales", (n, G))
+    _same_device(dev, levels=levels, codes=codes, scales=scales)
+    _check(lib.kq_quantize_groups(W.data_ptr(), ty, ld, n, k, group, _ptr(levels), codes.data_ptr(), scales.data_ptr(),
+                                  _stream(dev)), "kq_quantize_groups")
+    return codes, scales
+
+
+def _weights(codes, scales, k, group, levels, n=None):
+    """Checks packed weights; returns (n, k, levels)."""
+    k = int(k)
+    if n is None:
+        if not isinstance(scales, torch.Tensor) or scales.dim() != 2:
+            raise TypeError("scales must be a [n, groups] tensor")
+        n = scales.shape[0]
+        _dev(scales, torch.bfloat16, "scales", (n, _groups(k, group)))
+    _groups(k, group)
+    _dev(codes, torch.uint8, "codes", group_codes_shape(n, k))
+    levels = _levels(levels)
+    _same_device(codes.device, scales=scales, levels=levels)
+    return n, k, levels
+
+
+def kq_reconstruct_groups(codes, scales, in_features: int, group: int = 128, levels=None, dtype=torch.float32, W_hat=None):
+    """The weights that codes and scales stand for, [n, in_features] of `dtype` (or W_hat's)."""
+    n, k, levels = _weights(codes, scales, in_features, group, levels)
+    dev = codes.device
+    if W_hat is None:
+        if dtype not in _TYPES:
+            raise TypeError(f"dtype must be one of {', '.join(str(d) for d in _TYPES)}")
+        W_hat = torch.empty(n, k, dtype=dtype, device=dev)
+    out, ty, ld = _rows(W_hat, _TYPES, "W_hat", k)
+    if out.shape[0] != n:
+        raise ValueError(f"W_hat must have {n} rows")
+    _same_device(dev, W_hat=W_hat)
+    _check(lib.kq_reconstruct_groups(codes.data_ptr(), scales.data_ptr(), _ptr(levels), n, k, group, ty,
+                                     out.data_ptr(), ld, _stream(dev)), "kq_reconstruct_groups")
+    return W_hat
+
+
+def _out_rows(out, like, lead, cols, types, name):
+    """An output of lead + (cols,) values: given, or allocated in like's type.  Returns (out, matrix, pitch)."""
+    if out is None:
+        out = torch.empty(*lead, cols, dtype=like.dtype, device=like.device)
+    elif tuple(out.shape) != (*lead, cols):
+        raise ValueError(f"{name} must have shape {(*lead, cols)}, got {tuple(out.shape)}")
+    elif out.dtype != like.dtype:
+        raise TypeError(f"{name} must be {like.dtype}, got {out.dtype}")
+    t, _, ld = _rows(out, types, name, cols)
+    _same_device(like.device, **{name: out})
+    return out, t, ld
+
+
+def _scratch_for(dev, nb, workspace):
+    if workspace is not None:
+        _dev(workspace, torch.uint8, "workspace")
+        _same_device(dev, workspace=workspace)
+        return workspace.data_ptr(), workspace.numel()
+    if nb == 0:
+        return None, 0
+    ws = _ws(dev, nb)
+    return ws.data_ptr(), ws.numel()
+
+
+def kq_group_linear(X, codes, scales, group: int = 128, levels=None, bias=None, Y=None, workspace=None):
+    """Y = X W_hat^T + bias: X [..., k] bf16 or fp16 (a matrix may have strided rows), bias fp32 [n] or None, Y
+    [..., n] in X's type.  From one row (a token) to any number of them."""
+    x, ty, ldx = _rows(X, _ACTS, "X")
+    m, k = x.shape
+    n, k, levels = _weights(codes, scales, k, group, levels)
+    dev = x.device
+    if bias is not None:
+        _dev(bias, torch.float32, "bias", (n,))
+    _same_device(dev, codes=codes, bias=bias)
+    Y, y, ldy = _out_rows(Y, X, X.shape[:-1], n, _ACTS, "Y")
+    wp, wn = _scratch_for(dev, lib.kq_group_linear_workspace_bytes(m, n, k), workspace)
+    _check(lib.kq_group_linear(x.data_ptr(), ty, ldx, m, n, k, codes.data_ptr(), scales.data_ptr(), _ptr(levels), group,
+                               _ptr(bias), y.data_ptr(), ldy, wp, wn, _stream(dev)), "kq_group_linear")
+    return Y
+
+
+def kq_group_linear_grad_input(dY, codes, scales, in_features: int, group: int = 128, levels=None, dX=None, workspace=None):
+    """dX = dY W_hat: dY [..., n] bf16 or fp16, dX [..., in_features] in its type."""
+    dy, ty, ldy = _rows(dY, _ACTS, "dY")
+    n, k, levels = _weights(codes, scales, in_features, group, levels)
+    m = dy.shape[0]
+    dev = dy.device
+    if dy.shape[1] != n:
+        raise ValueError(f"dY must have {n} columns, got {dy.shape[1]}")
+    _same_device(dev, codes=codes)
+    dX, dx, ldx = _out_rows(dX, dY, dY.shape[:-1], k, _ACTS, "dX")
+    wp, wn = _scratch_for(dev, lib.kq_group_linear_grad_input_workspace_bytes(m, n, k), workspace)
+    _check(lib.kq_group_linear_grad_input(dy.data_ptr(), ty, ldy, m, n, k, codes.data_ptr(), scales.data_ptr(),
+                                          _ptr(levels), group, dx.data_ptr(), ldx, wp, wn, _stream(dev)),
+           "kq_group_linear_grad_input")
+    return dX
+
+
+def _checkpoint_shapes(m, k):
+    kq_ = -(-k // KQ_CHECKPOINT_GROUP) * KQ_CHECKPOINT_GROUP
+    return (m, kq_), (m, kq_ // KQ_CHECKPOINT_GROUP)
+
+
+def kq_checkpoint_pack(X, q=None, exps=None):
+    """An activation [..., k] (fp32, bf16 or fp16) in 8 bits: int8 values and a power of two for 32 neighbours.
+    Returns (q int8 [m, k rounded up to 32], exps uint8 [m, that / 32]), m the product of the leading sizes."""
+    x, ty, ld = _rows(X, _TYPES, "X")
+    m, k = x.shape
+    dev = x.device
+    qs, es = _checkpoint_shapes(m, k)
+    q = torch.empty(qs, dtype=torch.int8, device=dev) if q is None else _dev(q, torch.int8, "q", qs)
+    exps = torch.empty(es, dtype=torch.uint8, device=dev) if exps is None else _dev(exps, torch.uint8, "exps", es)
+    _same_device(dev, q=q, exps=exps)
+    _check(lib.kq_checkpoint_pack(x.data_ptr(), ty, ld, m, k, q.data_ptr(), exps.data_ptr(), _stream(dev)),
+           "kq_checkpoint_pack")
+    return q, exps
+
+
+def _checkpoint(q, exps, k):
+    k = int(k)
+    if not isinstance(q, torch.Tensor) or q.dim() != 2:
+        raise TypeError("q must be a [m, columns] tensor")
+    qs, es = _checkpoint_shapes(q.shape[0], k)
+    _dev(q, torch.int8, "q", qs)
+    _dev(exps, torch.uint8, "exps", es)
+    _same_device(q.device, exps=exps)
+    return q.shape[0], k
+
+
+def kq_checkpoint_restore(q, exps, in_features: int, dtype=torch.float32, X_hat=None):
+    """The activation that a checkpoint stands for, [m, in_features] of `dtype` (or X_hat's)."""
+    m, k = _checkpoint(q, exps, in_features)
+    if X_hat is None:
+        if dtype not in _TYPES:
+            raise TypeError(f"dtype must be one of {', '.join(str(d) for d in _TYPES)}")
+        X_hat = torch.empty(m, k, dtype=dtype, device=q.device)
+    out, ty, ld = _rows(X_hat, _TYPES, "X_hat", k)
+    if out.shape[0] != m:
+        raise ValueError(f"X_hat must have {m} rows")
+    _same_device(q.device, X_hat=X_hat)
+    _check(lib.kq_checkpoint_restore(q.data_ptr(), exps.data_ptr(), m, k, ty, out.data_ptr(), ld, _stream(q.device)),
+           "kq_checkpoint_restore")
+    return X_hat
+
+
+def _grad_rows(dY, q, m, n):
+    dy, ty, ldy = _rows(dY, _ACTS, "dY", n)
+    if dy.shape[0] != m:
+        raise ValueError(f"dY must have {m} rows as the checkpoint, got {dy.shape[0]}")
+    _same_device(dy.device, q=q)
+    return dy, ty, ldy
+
+
+def _bias_out(dev, n, bias, dbias):
+    if dbias is not None:
+        _same_device(dev, dbias=dbias)
+        return _dev(dbias, torch.float32, "dbias", (n,))
+    return torch.empty(n, dtype=torch.float32, device=dev) if bias else None
+
+
+def kq_checkpoint_grad_scales(dY, q, exps, codes, in_features: int, group: int = 128, levels=None, bias: bool = False,
+                              dscales=None, dbias=None, workspace=None):
+    """Gradient of the group scales (fp32 [n, groups]) from dY [..., n] and the checkpoint of X: the sum of level *
+    (dY^T X_hat) over each group, without the product in memory.  bias: also dbias = the column sums of dY.
+    Returns (dscales, dbias or None)."""
+    m, k = _checkpoint(q, exps, in_features)
+    n = dY.shape[-1] if isinstance(dY, torch.Tensor) and dY.dim() else 0
+    dy, ty, ldy = _grad_rows(dY, q, m, n)
+    _, _, levels = _weights(codes, None, k, group, levels, n)
+    dev = dy.device
+    _same_device(dev, codes=codes)
+    G = _groups(k, group)
+    dscales = torch.empty(n, G, dtype=torch.float32, device=dev) if dscales is None else _dev(dscales, torch.float32, "dscales", (n, G))
+    _same_device(dev, dscales=dscales)
+    dbias = _bias_out(dev, n, bias, dbias)
+    wp, wn = _scratch_for(dev, lib.kq_checkpoint_grad_workspace_bytes(m, n, k, group), workspace)
+    _check(lib.kq_checkpoint_grad_scales(dy.data_ptr(), ty, ldy, m, n, k, q.data_ptr(), exps.data_ptr(), codes.data_ptr(),
+                                         _ptr(levels), group, dscales.data_ptr(), _ptr(dbias), wp, wn, _stream(dev)),
+           "kq_checkpoint_grad_scales")
+    return dscales, dbias
+
+
+def kq_checkpoint_grad_weight(dY, q, exps, in_features: int, bias: bool = False, dW=None, dbias=None, workspace=None):
+    """Gradient of a whole weight matrix, dY^T X_hat (fp32 [n, in_features]), from the checkpoint of X.  bias: also
+    the column sums of dY.  Returns (dW, dbias or None)."""
+    m, k = _checkpoint(q, exps, in_features)
+    n = dY.shape[-1] if isinstance(dY, torch.Tensor) and dY.dim() else 0
+    dy, ty, ldy = _grad_rows(dY, q, m, n)
+    dev = dy.device
+    if dW is None:
+        dW = torch.empty(n, k, dtype=torch.float32, device=dev)
+    elif dW.dtype != torch.float32:
+        raise TypeError(f"dW must be float32, got {dW.dtype}")
+    out, _, ldw = _rows(dW, _TYPES, "dW", k)
+    if out.shape[0] != n:
+        raise ValueError(f"dW must have {n} rows")
+    _same_device(dev, dW=dW)
+    dbias = _bias_out(dev, n, bias, dbias)
+    wp, wn = _scratch_for(dev, lib.kq_checkpoint_grad_workspace_bytes(m, n, k, 0), workspace)
+    _check(lib.kq_checkpoint_grad_weight(dy.data_ptr(), ty, ldy, m, n, k, q.data_ptr(), exps.data_ptr(), out.data_ptr(),
+                                         ldw, _ptr(dbias), wp, wn, _stream(dev)), "kq_checkpoint_grad_weight")
+    return dW, dbias

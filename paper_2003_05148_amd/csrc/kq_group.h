@@ -1,0 +1,183 @@
+// Fully-connected layers in 4 bits with group scales, and 8-bit activation checkpoints: what the
+// translation units share.
+//
+// Packed codes.  W is cut into tiles of 16 rows by 128 columns of 1 KB, row tiles outermost:
+// [ceil(n/16)][ceil(k/128)][16 rows][64 bytes].  In a row's 64 bytes, dword 4 q + i holds columns
+// 32 i + 8 q + 0..7, and in a dword nibble (j & 1) * 4 + j / 2 holds column j of its eight.  So
+//   * a wave that loads 16 bytes a lane (lane = row + 16 q ... in the matrix instruction's own order)
+//     reads one contiguous kilobyte, and dword i of lane (row, q) is exactly that lane's operand of
+//     the i-th 16x16x32 matrix instruction of the tile: columns 8 q .. 8 q + 7 of 32-column block i;
+//   * nibbles r and r + 4 are the neighbours 2 r and 2 r + 1, so one shift and one mask leave a pair
+//     of neighbouring columns in the two halves of a register, where 16-bit values are wanted.
+// Rows and columns past the matrix hold code 0 and are never used with a non-zero factor.
+#pragma once
+
+#include "kq_internal.h"
+
+namespace kq {
+
+constexpr int kTileRows = 16;
+constexpr int kTileCols = 128;
+constexpr int kTileBytes = kTileRows * kTileCols / 2;
+constexpr int kCkGroup = KQ_CHECKPOINT_GROUP;
+
+inline __host__ __device__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
+inline __host__ __device__ int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+using f32x4 = __attribute__((ext_vector_type(4))) float;
+using f32x2 = __attribute__((ext_vector_type(2))) float;
+using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
+using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
+using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
+using f16x2 = __attribute__((ext_vector_type(2))) _Float16;
+using u32x4 = __attribute__((ext_vector_type(4))) unsigned;
+using u32x2 = __attribute__((ext_vector_type(2))) unsigned;
+
+__device__ __forceinline__ float bf16_bits_to_f32(unsigned h) { return __builtin_bit_cast(float, h << 16); }
+
+// The two 16-bit activation types.
+template <bool BF>
+struct Act {
+    static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+        if constexpr (BF)
+            return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+        else
+            return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+    // two fp32 values rounded to nearest into the halves of a register
+    static __device__ __forceinline__ unsigned pack(float lo, float hi) {
+        const f32x2 v = {lo, hi};
+        if constexpr (BF) return __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2));
+        else return __builtin_bit_cast(unsigned, __builtin_convertvector(v, f16x2));
+    }
+    // the same for values that the type holds exactly
+    static __device__ __forceinline__ unsigned pack_exact(float lo, float hi) {
+        if constexpr (BF)
+            return __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, hi), __builtin_bit_cast(unsigned, lo), 0x07060302u);
+        else
+            return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_pkrtz(lo, hi));
+    }
+    static __device__ __forceinline__ float lo(unsigned v) {
+        if constexpr (BF) return __builtin_bit_cast(float, v << 16);
+        else return (float)__builtin_bit_cast(f16x2, v).x;
+    }
+    static __device__ __forceinline__ float hi(unsigned v) {
+        if constexpr (BF) return __builtin_bit_cast(float, v & 0xffff0000u);
+        else return (float)__builtin_bit_cast(f16x2, v).y;
+    }
+    static __device__ __forceinline__ unsigned short one(float v) { return (unsigned short)(pack(v, 0.0f) & 0xffffu); }
+};
+
+// 16 levels as two byte tables of 16 entries in registers; a look-up is four byte permutes.
+struct LevelTable {
+    unsigned lo[4], hi[4];  // low and high bytes of the 16-bit levels, four a register
+};
+
+// ---- device parameters and launchers (checked by the C entry points before) ------------------------
+
+struct GroupWeights {
+    const uint8_t* codes;
+    const uint16_t* scales;  // bf16 [n][groups]
+    const uint16_t* levels;  // bf16 [16], or NULL: -8 .. 7
+    int n, k;
+    int log_group;           // 5, 6 or 7
+    int groups;              // ceil(k / group)
+    int ktiles;              // ceil(k / 128)
+    int ntiles;              // ceil(n / 16)
+};
+
+struct QuantizeParams {
+    const void* W;
+    int64_t ldw;
+    int type;
+    int n, k, log_group, groups, ktiles;
+    const uint16_t* levels;
+    uint8_t* codes;
+    uint16_t* scales;
+};
+hipError_t launch_quantize_groups(const QuantizeParams& p, hipStream_t s);
+
+struct ReconstructGroupsParams {
+    GroupWeights w;
+    int type;
+    void* W_hat;
+    int64_t ldw;
+};
+hipError_t launch_reconstruct_groups(const ReconstructGroupsParams& p, hipStream_t s);
+
+struct CheckpointParams {
+    void* X;       // read by pack, written by restore
+    int64_t ldx;
+    int type;
+    int64_t m;
+    int k, kq;     // kq = k rounded up to the group: the pitch of q
+    int8_t* q;
+    uint8_t* exps;
+};
+hipError_t launch_checkpoint_pack(const CheckpointParams& p, hipStream_t s);
+hipError_t launch_checkpoint_restore(const CheckpointParams& p, hipStream_t s);
+
+struct BiasGradParams {
+    const void* dY;
+    int64_t ldy;
+    int type;
+    int64_t m;
+    int n;
+    float* dbias;
+};
+hipError_t launch_bias_grad(const BiasGradParams& p, hipStream_t s);
+
+// The products.  `i` is the contiguous dimension of the output, `j` its rows, `c` the contraction:
+//   linear      Y[m][n]  = sum_k X[m][k] W[n][k]     i = n, j = m, c = k
+//   grad input  dX[m][k] = sum_n dY[m][n] W[n][k]    i = k, j = m, c = n
+//   grad weight dW[n][k] = sum_m dY[m][n] X^[m][k]   i = k, j = n, c = m   (scales: reduced in the epilogue)
+enum class Product { Linear = 0, GradInput = 1, GradWeight = 2, GradScales = 3 };
+
+struct GemmParams {
+    GroupWeights w;          // Linear, GradInput, GradScales (codes and levels only)
+    const void* B;           // X (Linear) or dY
+    int64_t ldb;
+    const int8_t* q;         // the checkpoint: GradWeight, GradScales
+    const uint8_t* exps;
+    int kq;
+    int64_t I, J, C;         // sizes along i, j, c
+    const float* bias;
+    void* out;               // 16-bit (Linear, GradInput) or fp32
+    int64_t ldo;
+    float* part;             // partial sums of a split contraction, or NULL
+    int splits;
+    int steps_per_split;     // 64-deep steps of the contraction a workgroup takes
+    int itiles, jtiles;
+};
+struct GemmPlan {
+    int bi, bj;              // output tile
+    int splits, steps_per_split;
+    size_t ws_bytes;
+};
+GemmPlan gemm_plan(Product mode, int64_t I, int64_t J, int64_t C, int groups);
+hipError_t launch_gemm(Product mode, bool bf16, const GemmPlan& plan, GemmParams p, hipStream_t s);
+
+// Y = X W^T for at most kMatvecRows rows of X.
+constexpr int kMatvecRows = 16;
+constexpr int kMatvecLdsRows = 4;         // up to so many rows of X go through LDS
+constexpr int kMatvecLdsBytes = 32768;
+struct MatvecParams {
+    GroupWeights w;
+    const void* X;
+    int64_t ldx;
+    int m;
+    const float* bias;
+    void* Y;
+    int64_t ldy;
+    float* part;             // partial sums [splits][m][n], or NULL
+    int splits, blocks_per_split;  // 128-column blocks a workgroup takes
+    int chunk;
+};
+struct MatvecPlan {
+    int splits, blocks_per_split;
+    size_t ws_bytes;
+};
+MatvecPlan matvec_plan(int m, int64_t n, int64_t k);
+hipError_t launch_matvec(bool bf16, const MatvecPlan& plan, MatvecParams p, hipStream_t s);
+
+}  // namespace kq

@@ -1,0 +1,581 @@
+"""Fully-connected layers in 4 bits with group scales, and 8-bit activation checkpoints, on the GPU
+against plain forms in 64 bits.
+
+Tolerances (set from the arithmetic, before any run).  u is the unit roundoff of the output's type (bf16
+2^-8, fp16 2^-11, fp32 2^-24), S = sum |a| |b| of a product's terms in 64 bits:
+  * codes, scales, checkpoint values and exponents, and what they stand for: equal, bit for bit;
+  * a product with exact factors and fp32 sums over c terms: |y - y64| <= u |y64| + (c + 16) 2^-24 F S, where
+    F = 1, and F = 16 for the integer levels -8 .. 7, which may be summed as level + 24 with 24 sum(x) taken
+    off: at most (31 + 24) / max(|level|, 1), over |level| averaging 4;
+  * with weights rounded to the activation's type: also u S, and 2^-24 sum |x| for fp16's subnormals;
+  * 2-norms: ||y - y64|| <= (u, twice where weights are rounded, + 2^-18) ||y64|| for random operands.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+kq = pytest.importorskip("paper_2003_05148_amd")
+DEV = torch.device("cuda:0")
+BF, HF, F32 = torch.bfloat16, torch.float16, torch.float32
+U = {BF: 2.0 ** -8, HF: 2.0 ** -11, F32: 2.0 ** -24}
+TINY = {BF: 2.0 ** -133, HF: 2.0 ** -25, F32: 2.0 ** -149}   # half the smallest subnormal
+
+
+def gen(seed):
+    return torch.Generator(device="cpu").manual_seed(seed)
+
+
+def table(seed):
+    """16 ascending bf16 levels, not symmetric, two of them equal."""
+    v = torch.randn(16, generator=gen(seed), dtype=torch.float64)
+    v[3] = v[4]
+    return v.to(BF).sort().values
+
+
+def values(levels):
+    return torch.arange(-8, 8, dtype=torch.float64) if levels is None else levels.double().cpu()
+
+
+def column_nibbles():
+    c = torch.arange(128)
+    i, q, j = c // 32, c // 8 % 4, c % 8
+    return 8 * (4 * q + i) + (j % 2) * 4 + j // 2
+
+
+def pack(codes):
+    """The documented layout, from codes uint8 [n, k] on the CPU."""
+    n, k = codes.shape
+    nt, kt = -(-n // 16), -(-k // 128)
+    full = torch.zeros(nt * 16, kt * 128, dtype=torch.uint8)
+    full[:n, :k] = codes
+    nib = torch.empty(nt, kt, 16, 128, dtype=torch.uint8)
+    nib[..., column_nibbles()] = full.view(nt, 16, kt, 128).permute(0, 2, 1, 3)
+    return nib[..., 0::2] | (nib[..., 1::2] << 4)
+
+
+def unpack(packed, n, k):
+    nt, kt = packed.shape[:2]
+    nib = torch.stack((packed & 15, packed >> 4), dim=-1).view(nt, kt, 16, 128)
+    return nib[..., column_nibbles()].permute(0, 2, 1, 3).reshape(nt * 16, kt * 128)[:n, :k]
+
+
+class Layer:
+    """Random codes and scales on the device, and the weights in 64 bits."""
+
+    def __init__(self, n, k, group, levels, seed, scale=0.02):
+        g = gen(seed)
+        self.n, self.k, self.group = n, k, group
+        self.codes = torch.randint(0, 16, (n, k), generator=g, dtype=torch.uint8)
+        G = -(-k // group)
+        self.scales = (scale * (0.5 + torch.rand(n, G, generator=g))).to(BF)
+        self.levels = levels
+        self.packed = pack(self.codes).to(DEV)
+        self.dscales = self.scales.to(DEV)
+        self.dlevels = None if levels is None else levels.to(DEV)
+
+    @property
+    def W(self):
+        which = torch.arange(self.k) // self.group
+        return values(self.levels)[self.codes.long()] * self.scales.double()[:, which]
+
+    def kw(self):
+        return dict(group=self.group, levels=self.dlevels)
+
+
+def acts(m, k, dtype, seed, scale=1.0):
+    return (scale * torch.randn(m, k, generator=gen(seed))).to(dtype)
+
+
+def check(y, y64, S, dtype, terms, rounded, integers, xsum=None, norm=True):
+    """y against the product in 64 bits within the tolerances of this file's head."""
+    y = y.double().cpu()
+    u = U[dtype]
+    tol = u * y64.abs() + (terms + 16) * 2.0 ** -24 * (16 if integers else 1) * S + TINY[dtype]
+    if rounded:
+        tol = tol + u * S
+        if dtype == HF:
+            tol = tol + 2.0 ** -24 * xsum
+    err = (y - y64).abs()
+    assert torch.all(err <= tol), float((err - tol).max())
+    if norm and y64.numel() >= 64:
+        rel = float(err.norm() / y64.norm())
+        assert rel <= (2 * u if rounded else u) + 2.0 ** -18, rel
+
+
+# ---- quantizer ---------------------------------------------------------------------------------
+
+def quantize_plain(W, group, levels):
+    """(codes, scales) by fp32 arithmetic on the CPU."""
+    n, k = W.shape
+    w = W.float().numpy()
+    lv = values(levels).float().numpy()
+    top = np.float32(7.0) if levels is None else np.abs(lv).max()
+    mid = (np.float32(0.5) * (lv[:-1] + lv[1:])).astype(np.float32)
+    G = -(-k // group)
+    codes = np.zeros((n, k), np.uint8)
+    scales = torch.zeros(n, G, dtype=BF)
+    with np.errstate(invalid="ignore", over="ignore"):
+        for g in range(G):
+            b = w[:, g * group:(g + 1) * group]
+            a = np.abs(b).max(1)
+            bad = ~np.isfinite(b).all(1)
+            s = torch.from_numpy(np.where(bad, np.nan, a / top).astype(np.float32)).to(BF)
+            s = torch.where(s.float() < 2.0 ** -126, torch.zeros_like(s), s)
+            scales[:, g] = s
+            sf = s.float().numpy()[:, None]
+            t = np.where(sf > 0, b / np.where(sf > 0, sf, 1), np.float32(0)).astype(np.float32)
+            codes[:, g * group:(g + 1) * group] = (t[:, :, None] > mid).sum(2)
+    return torch.from_numpy(codes), scales
+
+
+def same_bits(a, b):
+    a, b = a.cpu().contiguous(), b.cpu().contiguous()
+    return torch.equal(torch.nan_to_num(a.float(), nan=12345.0), torch.nan_to_num(b.float(), nan=12345.0))
+
+
+@pytest.mark.parametrize("n,k", [(1, 1), (5, 31), (16, 128), (17, 129), (33, 200), (100, 1023), (3, 4099)])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("dtype,lut", [(F32, False), (BF, True), (HF, False), (F32, True)])
+def test_quantize_equals_the_plain_form(n, k, group, dtype, lut):
+    levels = table(n + k) if lut else None
+    W = (0.05 * torch.randn(n, k, generator=gen(n * k + group))).to(dtype)
+    W[n // 2, : min(k, 40)] = 0                       # a group of zeros (or part of one)
+    codes, scales = quantize_plain(W, group, levels)
+    dl = None if levels is None else levels.to(DEV)
+    gc, gs = kq.kq_quantize_groups(W.to(DEV), group=group, levels=dl)
+    assert same_bits(gs, scales)
+    assert torch.equal(unpack(gc.cpu(), n, k), codes)
+    assert torch.equal(gc.cpu(), pack(codes))         # and zeros past the matrix
+    for out in (F32, BF, HF):
+        What = kq.kq_reconstruct_groups(gc, gs, k, group=group, levels=dl, dtype=out)
+        exact = values(levels).float()[codes.long()] * scales.float()[:, torch.arange(k) // group]
+        assert torch.equal(What.cpu(), exact.to(out))
+
+
+def test_quantize_ties_go_to_the_lower_level():
+    """Multiples of half a scale: the group's largest weight is 7, the scale 1."""
+    W = torch.zeros(1, 128)
+    W[0, :29] = torch.arange(29) * 0.5 - 7.0
+    codes, scales = kq.kq_quantize_groups(W.to(DEV), group=128)
+    assert float(scales[0, 0]) == 1.0
+    got = unpack(codes.cpu(), 1, 128)[0].to(torch.int64) - 8
+    assert torch.equal(got, torch.ceil(W[0].double() - 0.5).to(torch.int64))
+
+
+def test_quantize_extremes():
+    """Infinities and NaN spoil their own group only; tiny and huge groups; a strided matrix."""
+    W = torch.randn(20, 256, generator=gen(3))
+    W[2, 5] = float("inf")
+    W[3, 200] = float("nan")
+    W[4, :128] = 1e-45
+    W[5, :128] *= 1e38
+    W[6, :128] = -3e-38
+    wide = torch.full((20, 300), 7.7)
+    wide[:, 9:265] = W
+    codes, scales = kq.kq_quantize_groups(wide.to(DEV)[:, 9:265], group=128)
+    pc, ps = quantize_plain(W, 128, None)
+    assert same_bits(scales, ps)
+    ok = torch.isfinite(ps)[:, torch.arange(256) // 128]
+    assert torch.equal(unpack(codes.cpu(), 20, 256)[ok], pc[ok])
+    What = kq.kq_reconstruct_groups(codes, scales, 256).cpu()
+    assert torch.equal(torch.isnan(What), ~ok)
+    assert float(scales[4, 0]) == 0 and torch.all(What[4, :128] == 0)
+    assert torch.all((What - W)[ok].abs() <= (0.5 + 2.0 ** -6) * ps.float()[:, torch.arange(256) // 128][ok] + 8 * 2.0 ** -126)
+
+
+# ---- linear --------------------------------------------------------------------------------------
+
+LINEAR = [(1, 1, 1), (1, 1000, 512), (1, 17, 4099), (2, 5, 33), (3, 129, 127), (13, 300, 1023), (15, 64, 128), (16, 100, 257),
+          (17, 33, 640), (31, 200, 96), (33, 1000, 129), (64, 256, 512), (65, 127, 300), (129, 130, 385), (300, 515, 1030)]
+
+
+@pytest.mark.parametrize("m,n,k", LINEAR)
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("group,lut", [(32, True), (64, False), (128, False), (128, True)])
+def test_linear(m, n, k, dtype, group, lut):
+    L = Layer(n, k, group, table(k) if lut else None, seed=m + n + k)
+    X = acts(m, k, dtype, seed=m * 7 + k)
+    bias = torch.randn(n, generator=gen(n)) if (m + n) % 2 else None
+    Y = kq.kq_group_linear(X.to(DEV), L.packed, L.dscales, bias=None if bias is None else bias.to(DEV), **L.kw())
+    assert Y.shape == (m, n) and Y.dtype == dtype
+    W = L.W
+    y64 = X.double() @ W.T
+    S = X.double().abs() @ W.abs().T
+    if bias is not None:
+        y64, S = y64 + bias.double(), S + bias.double().abs()
+    check(Y, y64, S, dtype, k, m > 16, not lut, xsum=X.double().abs().sum(1, keepdim=True))
+
+
+def test_linear_vector_and_batch_shapes():
+    L = Layer(48, 160, 32, None, seed=1)
+    X = acts(6, 160, BF, seed=2).to(DEV)
+    Y = kq.kq_group_linear(X, L.packed, L.dscales, **L.kw())
+    assert torch.equal(kq.kq_group_linear(X.view(2, 3, 160), L.packed, L.dscales, **L.kw()), Y.view(2, 3, 48))
+    one = kq.kq_group_linear(X[0], L.packed, L.dscales, **L.kw())
+    assert one.shape == (48,)
+    check(one[None], X[:1].double().cpu() @ L.W.T, X[:1].double().cpu().abs() @ L.W.abs().T, BF, 160, False, True)
+    assert kq.kq_group_linear(X[:0], L.packed, L.dscales, **L.kw()).shape == (0, 48)
+    assert kq.kq_group_linear_grad_input(Y[:0], L.packed, L.dscales, 160, **L.kw()).shape == (0, 160)
+
+
+@pytest.mark.parametrize("m", [1, 9, 40, 200])
+@pytest.mark.parametrize("off", [0, 1, 3])
+def test_linear_strided_rows_and_offsets(m, off):
+    """Rows inside a wider buffer that starts anywhere; nothing else of the output is written."""
+    n, k = 70, 201
+    L = Layer(n, k, 64, None, seed=off)
+    X = acts(m, k, HF, seed=5)
+    wide = torch.full((m, k + 37), float("nan"), dtype=HF)
+    wide[:, off:off + k] = X
+    out = torch.full((m, n + 13), 5.0, dtype=HF, device=DEV)
+    Y = kq.kq_group_linear(wide.to(DEV)[:, off:off + k], L.packed, L.dscales, Y=out[:, off:off + n], **L.kw())
+    assert Y.data_ptr() == out[:, off:].data_ptr()
+    check(Y, X.double() @ L.W.T, X.double().abs() @ L.W.abs().T, HF, k, m > 16, True,
+          xsum=X.double().abs().sum(1, keepdim=True))
+    assert torch.all(out[:, :off] == 5) and torch.all(out[:, off + n:] == 5)
+    dwide = torch.full((m, n + 11), float("inf"), dtype=HF)
+    dwide[:, off:off + n] = acts(m, n, HF, seed=6)
+    dY = dwide[:, off:off + n]
+    dout = torch.full((m, k + 5), 5.0, dtype=HF, device=DEV)
+    dX = kq.kq_group_linear_grad_input(dwide.to(DEV)[:, off:off + n], L.packed, L.dscales, k, dX=dout[:, off:off + k], **L.kw())
+    check(dX, dY.double() @ L.W, dY.double().abs() @ L.W.abs(), HF, n, True, False,
+          xsum=dY.double().abs().sum(1, keepdim=True))
+    assert torch.all(dout[:, :off] == 5) and torch.all(dout[:, off + k:] == 5)
+
+
+@pytest.mark.parametrize("m", [1, 16, 17, 130])
+@pytest.mark.parametrize("lut", [False, True])
+def test_linear_special_values_stay_in_their_row(m, lut):
+    """A NaN or an infinity in X reaches its row of Y alone, a NaN scale its column alone; a zero scale gives zeros."""
+    n, k = 50, 300
+    L = Layer(n, k, 128, table(4) if lut else None, seed=8)
+    s = L.scales.clone()
+    s[7, 1] = float("nan")
+    s[9, :] = 0
+    X = acts(m, k, BF, seed=9)
+    X[m - 1, 150] = float("nan")
+    if m > 2:
+        X[1, 299] = float("inf")
+    Y = kq.kq_group_linear(X.to(DEV), L.packed, s.to(DEV), **L.kw()).float().cpu()
+    bad = torch.zeros(m, n, dtype=torch.bool)
+    bad[m - 1] = True
+    bad[:, 7] = True
+    if m > 2:
+        assert not torch.isfinite(Y[1]).any()
+        bad[1] = True
+    assert torch.isnan(Y[m - 1]).all() and torch.isnan(Y[:, 7]).all()
+    assert torch.isfinite(Y[~bad]).all()
+    rows = [r for r in range(m) if not bad[r].all()]
+    assert torch.all(Y[rows, 9] == 0)
+
+
+# ---- gradient of the input ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 300, 700), (5, 33, 65), (16, 129, 1023), (37, 1000, 130), (64, 64, 64), (129, 257, 385),
+                                   (300, 515, 1030)])
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("group,lut", [(32, False), (64, True), (128, False)])
+def test_grad_input(m, n, k, dtype, group, lut):
+    L = Layer(n, k, group, table(n) if lut else None, seed=m + n + k)
+    dY = acts(m, n, dtype, seed=m * 3 + n)
+    dX = kq.kq_group_linear_grad_input(dY.to(DEV), L.packed, L.dscales, k, **L.kw())
+    assert dX.shape == (m, k) and dX.dtype == dtype
+    W = L.W
+    check(dX, dY.double() @ W, dY.double().abs() @ W.abs(), dtype, n, True, False,
+          xsum=dY.double().abs().sum(1, keepdim=True))
+
+
+# ---- checkpoints ------------------------------------------------------------------------------------------
+
+def checkpoint_plain(X):
+    """(q, exps) in 64 bits."""
+    m, k = X.shape
+    kp = -(-k // 32) * 32
+    x = torch.zeros(m, kp, dtype=torch.float64)
+    x[:, :k] = X.double()
+    x = x.view(m, kp // 32, 32)
+    bad = ~torch.isfinite(x).all(2)
+    a = torch.where(bad, torch.zeros(()).double(), x.abs().amax(2).nan_to_num(0, 0, 0))
+    least = -24 if X.dtype == HF else -126
+    e = torch.where(a > 0, torch.frexp(a)[1].long() - 7, torch.full(a.shape, least)).clamp(min=least)
+    q = torch.round(x * torch.exp2(-e.double())[:, :, None]).clamp(-127, 127)
+    q = torch.where(bad[:, :, None], torch.zeros(()).double(), q).to(torch.int8).view(m, kp)
+    return q, torch.where(bad, torch.full(e.shape, 255), e + 127).to(torch.uint8)
+
+
+def restored(q, exps, k):
+    step = torch.where(exps == 255, torch.full((), float("nan")).double(), torch.exp2(exps.double() - 127))
+    return (q.double().view(*exps.shape, 32) * step[:, :, None]).view(q.shape)[:, :k]
+
+
+@pytest.mark.parametrize("m,k", [(1, 1), (1, 32), (3, 33), (7, 1000), (33, 257), (130, 96)])
+@pytest.mark.parametrize("dtype", [F32, BF, HF])
+def test_checkpoint_equals_the_plain_form(m, k, dtype):
+    g = gen(m * k)
+    X = torch.randn(m, k, generator=g) * torch.exp2(torch.randint(-30, 12, (m, 1), generator=g).float())
+    X = X.to(dtype)
+    X[0, :40] = 0
+    q, exps = kq.kq_checkpoint_pack(X.to(DEV))
+    pq, pe = checkpoint_plain(X)
+    assert torch.equal(exps.cpu(), pe) and torch.equal(q.cpu(), pq)
+    want = restored(pq, pe, k)
+    for out in (F32, BF, dtype):   # exact: no rounding in fp32, bf16, or the input's own type
+        got = kq.kq_checkpoint_restore(q, exps, k, dtype=out)
+        assert got.dtype == out and torch.equal(got.cpu().double(), want)
+    kp = pe.shape[1] * 32
+    xe = torch.zeros(m, kp, dtype=torch.float64)
+    xe[:, :k] = X.double()
+    step = torch.exp2(pe.double() - 127).repeat_interleave(32, 1)
+    err = (xe - restored(pq, pe, kp)).abs()
+    assert torch.all(err <= torch.where(xe.abs() > 127.5 * step, step, 0.5 * step))
+
+
+def test_checkpoint_extremes():
+    """The largest and smallest numbers of each type, infinities and NaN, strided rows."""
+    for dtype, big, small in ((F32, 3.4028234e38, 1e-45), (BF, 3.3895314e38, 9.2e-41), (HF, 65504.0, 6e-8)):
+        X = torch.zeros(6, 96, dtype=dtype)
+        X[0, 3], X[0, 4] = big, -big
+        X[1, 40] = small
+        X[2, 64] = float("inf")
+        X[3, 31] = float("nan")
+        X[4, 0], X[4, 1] = big, small
+        X[5] = 1.0
+        wide = torch.zeros(6, 101, dtype=dtype)
+        wide[:, 3:99] = X
+        q, exps = kq.kq_checkpoint_pack(wide.to(DEV)[:, 3:99])
+        pq, pe = checkpoint_plain(X)
+        assert torch.equal(exps.cpu(), pe) and torch.equal(q.cpu(), pq)
+        got = kq.kq_checkpoint_restore(q, exps, 96, dtype=dtype).cpu()
+        assert torch.isnan(got[2, 64:]).all() and torch.isfinite(got[2, :64]).all()
+        assert torch.isnan(got[3, :32]).all() and torch.isfinite(got[3, 32:]).all()
+        assert torch.isfinite(got[[0, 1, 4, 5]]).all() and torch.all(got[5] == 1.0)
+
+
+# ---- gradients from a checkpoint ------------------------------------------------------------------------------
+
+GRADS = [(0, 5, 40), (1, 1, 1), (1, 70, 300), (2, 17, 33), (63, 130, 129), (64, 128, 128), (65, 33, 1023), (200, 300, 257),
+         (513, 129, 515)]
+
+
+def grad_inputs(m, n, k, dtype):
+    X = acts(m, k, dtype, seed=m + k)
+    dY = acts(m, n, dtype, seed=m + n + 1, scale=0.05)
+    q, exps = kq.kq_checkpoint_pack(X.to(DEV))
+    return dY, q, exps, restored(q.cpu(), exps.cpu(), k)
+
+
+@pytest.mark.parametrize("m,n,k", GRADS)
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_grad_weight(m, n, k, dtype):
+    dY, q, exps, xh = grad_inputs(m, n, k, dtype)
+    out = torch.full((n, k + 3), 5.0, device=DEV)
+    dW, db = kq.kq_checkpoint_grad_weight(dY.to(DEV), q, exps, k, bias=True, dW=out[:, 1:k + 1])
+    d = dY.double()
+    check(dW, d.T @ xh, d.abs().T @ xh.abs(), F32, m, False, False, norm=m > 0)
+    check(db, d.sum(0), d.abs().sum(0), F32, m, False, False, norm=False)
+    assert torch.all(out[:, 0] == 5) and torch.all(out[:, k + 1:] == 5)
+    assert kq.kq_checkpoint_grad_weight(dY.to(DEV), q, exps, k)[1] is None
+
+
+@pytest.mark.parametrize("m,n,k", GRADS)
+@pytest.mark.parametrize("dtype,group,lut", [(BF, 32, False), (HF, 64, True), (BF, 128, True), (HF, 128, False)])
+def test_grad_scales(m, n, k, dtype, group, lut):
+    L = Layer(n, k, group, table(m + n) if lut else None, seed=n + k)
+    dY, q, exps, xh = grad_inputs(m, n, k, dtype)
+    ds, db = kq.kq_checkpoint_grad_scales(dY.to(DEV), q, exps, L.packed, k, bias=True, **L.kw())
+    d = dY.double()
+    lv = values(L.levels)[L.codes.long()]
+    which = torch.arange(k) // group
+    G = L.scales.shape[1]
+    want = torch.zeros(n, G, dtype=torch.float64).index_add_(1, which, (d.T @ xh) * lv)
+    S = torch.zeros(n, G, dtype=torch.float64).index_add_(1, which, (d.abs().T @ xh.abs()) * lv.abs())
+    check(ds, want, S, F32, m + group, False, False, norm=False)
+    check(db, d.sum(0), d.abs().sum(0), F32, m, False, False, norm=False)
+
+
+def test_scale_gradient_against_differences():
+    """d/ds of sum(dY * (X_hat W_hat(s)^T)) by central differences in 64 bits: the loss is linear in the scales, so
+    the difference is exact up to rounding (2^-40 of the terms, far below the gradient's fp32 sums)."""
+    m, n, k, group = 37, 20, 200, 64
+    L = Layer(n, k, group, table(11), seed=12)
+    dY, q, exps, xh = grad_inputs(m, n, k, BF)
+    ds, _ = kq.kq_checkpoint_grad_scales(dY.to(DEV), q, exps, L.packed, k, **L.kw())
+    lv = values(L.levels)[L.codes.long()]
+    which = torch.arange(k) // group
+
+    def loss(s):
+        return float((dY.double() * (xh @ (lv * s[:, which]).T)).sum())
+
+    s0 = L.scales.double()
+    S = torch.zeros(n, s0.shape[1], dtype=torch.float64).index_add_(1, which, (dY.double().abs().T @ xh.abs()) * lv.abs())
+    for r, g in [(0, 0), (7, 1), (19, 3), (11, 2)]:
+        h = torch.zeros_like(s0)
+        h[r, g] = 2.0 ** -6
+        num = (loss(s0 + h) - loss(s0 - h)) / 2.0 ** -5
+        assert abs(num - float(ds[r, g])) <= (m + group + 16) * 2.0 ** -24 * float(S[r, g]) + 1e-7
+
+
+def test_input_gradient_against_differences():
+    """The same for dX: the loss is linear in X."""
+    m, n, k = 3, 40, 70
+    L = Layer(n, k, 32, None, seed=13)
+    dY = acts(m, n, HF, seed=14)
+    dX = kq.kq_group_linear_grad_input(dY.to(DEV), L.packed, L.dscales, k, **L.kw()).double().cpu()
+    X = acts(m, k, HF, seed=15).double()
+    W = L.W
+    S = dY.double().abs() @ W.abs()
+    for r, c in [(0, 0), (1, 69), (2, 33)]:
+        h = torch.zeros_like(X)
+        h[r, c] = 0.5
+        num = float((dY.double() * ((X + h) @ W.T - (X - h) @ W.T)).sum())
+        assert abs(num - float(dX[r, c])) <= (U[HF] * 2 + (n + 16) * 2.0 ** -24) * float(S[r, c]) + 2.0 ** -24 * float(dY.double().abs()[r].sum())
+
+
+def test_nan_in_a_checkpoint_reaches_its_columns_alone():
+    m, n, k = 70, 40, 200
+    X = acts(m, k, BF, seed=1)
+    X[50, 70] = float("inf")
+    q, exps = kq.kq_checkpoint_pack(X.to(DEV))
+    dW, _ = kq.kq_checkpoint_grad_weight(acts(m, n, BF, seed=2).to(DEV), q, exps, k)
+    bad = torch.isnan(dW).all(0).cpu()
+    assert bad[64:96].all() and not bad[:64].any() and not bad[96:].any()
+    assert torch.isfinite(dW[:, ~bad.to(DEV)]).all()
+
+
+# ---- long and large, streams, graphs, repeats --------------------------------------------------------------------
+
+def test_rows_beyond_32_bit_offsets():
+    """The last rows of matrices of more than 2^31 values."""
+    k, n = 25088, 16
+    m = (1 << 31) // k + 40
+    L = Layer(n, k, 128, None, seed=3, scale=0.001)
+    X = torch.zeros(m, k, dtype=BF, device=DEV)
+    tail = acts(20, k, BF, seed=4)
+    X[-20:] = tail.to(DEV)
+    Y = kq.kq_group_linear(X, L.packed, L.dscales, **L.kw())
+    check(Y[-20:], tail.double() @ L.W.T, tail.double().abs() @ L.W.abs().T, BF, k, True, True)
+    assert torch.all(Y[:-20] == 0)
+    q, exps = kq.kq_checkpoint_pack(X)
+    pq, pe = checkpoint_plain(tail)
+    assert torch.equal(q[-20:].cpu(), pq) and torch.equal(exps[-20:].cpu(), pe)
+    dY = torch.zeros(m, n, dtype=BF, device=DEV)
+    dY[-20:] = acts(20, n, BF, seed=5).to(DEV)
+    dW, _ = kq.kq_checkpoint_grad_weight(dY, q, exps, k)
+    d = dY[-20:].double().cpu()
+    xh = restored(pq, pe, k)
+    check(dW, d.T @ xh, d.abs().T @ xh.abs(), F32, 20, False, False)
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 4096, 4096), (8, 512, 25088), (64, 300, 4096), (2048, 100, 130)])
+def test_results_repeat_bit_for_bit(m, n, k):
+    L = Layer(n, k, 128, None, seed=1)
+    X = acts(m, k, BF, seed=2).to(DEV)
+    dY = acts(m, n, BF, seed=3).to(DEV)
+    q, exps = kq.kq_checkpoint_pack(X)
+
+    def all_of():
+        return [kq.kq_group_linear(X, L.packed, L.dscales), kq.kq_group_linear_grad_input(dY, L.packed, L.dscales, k),
+                *kq.kq_checkpoint_grad_scales(dY, q, exps, L.packed, k, bias=True), kq.kq_checkpoint_grad_weight(dY, q, exps, k)[0]]
+
+    first = all_of()
+    for _ in range(5):
+        for a, b in zip(first, all_of()):
+            assert torch.equal(a, b)
+
+
+def test_two_streams_and_a_graph():
+    """Calls of different sizes on two streams, then a captured step replayed between eager work, against the same
+    calls one after another."""
+    jobs = []
+    for m, n, k in ((3, 1000, 4096), (40, 700, 1030)):
+        L = Layer(n, k, 64, table(m), seed=m)
+        jobs.append((L, acts(m, k, BF, seed=m).to(DEV), acts(m, n, BF, seed=m + 1).to(DEV)))
+
+    def step(job):
+        L, X, dY = job
+        q, exps = kq.kq_checkpoint_pack(X)
+        return [kq.kq_group_linear(X, L.packed, L.dscales, **L.kw()),
+                kq.kq_group_linear_grad_input(dY, L.packed, L.dscales, L.k, **L.kw()),
+                *kq.kq_checkpoint_grad_scales(dY, q, exps, L.packed, L.k, bias=True, **L.kw()),
+                kq.kq_checkpoint_grad_weight(dY, q, exps, L.k)[0]]
+
+    want = [[t.clone() for t in step(j)] for j in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(DEV) for _ in jobs]
+    for _ in range(5):
+        got = []
+        for s, j in zip(streams, jobs):
+            with torch.cuda.stream(s):
+                got.append(step(j))
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            assert all(torch.equal(a, b) for a, b in zip(g, w))
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(streams[0]):
+        step(jobs[0])
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        out = step(jobs[0])
+    for r in range(4):
+        for t in out:
+            t.zero_()
+        step(jobs[1])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want[0])), r
+
+
+def test_refusals():
+    L = Layer(20, 100, 32, None, seed=1)
+    X = acts(4, 100, BF, seed=1).to(DEV)
+    lin = lambda **kw: kq.kq_group_linear(**{**dict(X=X, codes=L.packed, scales=L.dscales, group=32), **kw})
+    assert lin().shape == (4, 20)
+    with pytest.raises(TypeError):
+        lin(X=X.float())                        # fp32 activations
+    with pytest.raises(TypeError):
+        lin(X=X.cpu())
+    with pytest.raises(ValueError):
+        lin(group=16)
+    with pytest.raises(ValueError):
+        lin(group=64)                           # scales of another group
+    with pytest.raises(ValueError):
+        lin(X=X[:, :60])                        # two groups, where the scales are for four
+    with pytest.raises(ValueError):
+        lin(X=X.t())
+    with pytest.raises(TypeError):
+        lin(scales=L.dscales.float())
+    with pytest.raises(ValueError):
+        lin(codes=L.packed[:1])
+    with pytest.raises(TypeError):
+        lin(levels=torch.zeros(16, device=DEV))
+    with pytest.raises(ValueError):
+        lin(levels=torch.zeros(15, device=DEV, dtype=BF))
+    with pytest.raises(ValueError):
+        lin(bias=torch.zeros(19, device=DEV))
+    with pytest.raises(ValueError):
+        lin(Y=torch.empty(4, 21, device=DEV, dtype=BF))
+    with pytest.raises(TypeError):
+        lin(Y=torch.empty(4, 20, device=DEV, dtype=HF))
+    with pytest.raises(ValueError):
+        lin(X=X[:1].expand(4, 100))             # rows that overlap
+    q, exps = kq.kq_checkpoint_pack(X)
+    dY = acts(4, 20, BF, seed=2).to(DEV)
+    with pytest.raises(ValueError):
+        kq.kq_checkpoint_restore(q, exps, 128 + 1)
+    with pytest.raises(ValueError):
+        kq.kq_checkpoint_grad_weight(dY[:3], q, exps, 100)
+    with pytest.raises(TypeError):
+        kq.kq_checkpoint_grad_weight(dY.float(), q, exps, 100)
+    with pytest.raises(ValueError):
+        kq.kq_checkpoint_grad_scales(dY, q, exps, L.packed, 200, group=32)
+    with pytest.raises(TypeError):
+        kq.kq_checkpoint_pack(X.double())
+    with pytest.raises(TypeError):
+        kq.kq_quantize_groups(X.double())
+    with pytest.raises(ValueError):
+        kq.kq_group_linear_grad_input(dY[:, :19], L.packed, L.dscales, 100, group=32)
