@@ -902,6 +902,19 @@ _TYPES = {torch.float32: KQ_T_F32, torch.bfloat16: KQ_T_BF16, torch.float16: KQ_
 _ACTS = {torch.bfloat16: KQ_T_BF16, torch.float16: KQ_T_F16}
 
 
+# The plain case of the calls below in one C++ call (checks, outputs, scratch and the library call); it
+# returns None for anything else, and then the checks here say what is wrong, or convert.
+if _kqhost is not None and _raw_stream is not None:
+    _kqhost.bind(tuple(ctypes.cast(getattr(lib, f), _P).value for f in (
+        "kq_quantize_groups", "kq_reconstruct_groups", "kq_group_linear_workspace_bytes", "kq_group_linear",
+        "kq_group_linear_grad_input_workspace_bytes", "kq_group_linear_grad_input", "kq_checkpoint_pack",
+        "kq_checkpoint_restore", "kq_checkpoint_grad_workspace_bytes", "kq_checkpoint_grad_scales",
+        "kq_checkpoint_grad_weight")), _raw_stream, lambda device, nbytes: _ws(device, nbytes))
+    _fast = _kqhost
+else:
+    _fast = None
+
+
 def _rows(t, types, name, cols=None):
     """A matrix of rows for the library: (tensor [m, cols], its type, row pitch).  Rows may be strided; a row's
     values are neighbours.  Leading dimensions (or none, a single row) are flattened where that needs no copy."""
@@ -950,6 +963,10 @@ def kq_quantize_groups(W, group: int = 128, levels=None, codes=None, scales=None
     """4-bit codes of a weight matrix (fp32, bf16 or fp16, rows may be strided) with a bf16 scale for `group`
     neighbouring columns.  levels: None for -8 .. 7 or 16 ascending bf16 levels.  Returns (codes uint8 packed,
     scales bfloat16 [n, ceil(k / group)]); include/kq.h has the formulas and the layout."""
+    if _fast is not None and codes is None and scales is None:
+        r = _fast.quantize_groups(W, group, levels)
+        if r is not None:
+            return r
     W, ty, ld = _rows(W, _TYPES, "W")
     n, k = W.shape
     dev = W.device
@@ -983,6 +1000,10 @@ def _weights(codes, scales, k, group, levels, n=None):
 
 def kq_reconstruct_groups(codes, scales, in_features: int, group: int = 128, levels=None, dtype=torch.float32, W_hat=None):
     """The weights that codes and scales stand for, [n, in_features] of `dtype` (or W_hat's)."""
+    if _fast is not None and W_hat is None:
+        r = _fast.reconstruct_groups(codes, scales, in_features, group, levels, _TYPES.get(dtype, -1))
+        if r is not None:
+            return r
     n, k, levels = _weights(codes, scales, in_features, group, levels)
     dev = codes.device
     if W_hat is None:
@@ -1025,6 +1046,10 @@ def _scratch_for(dev, nb, workspace):
 def kq_group_linear(X, codes, scales, group: int = 128, levels=None, bias=None, Y=None, workspace=None):
     """Y = X W_hat^T + bias: X [..., k] bf16 or fp16 (a matrix may have strided rows), bias fp32 [n] or None, Y
     [..., n] in X's type.  From one row (a token) to any number of them."""
+    if _fast is not None and workspace is None:
+        r = _fast.group_linear(X, codes, scales, group, levels, bias, Y)
+        if r is not None:
+            return r
     x, ty, ldx = _rows(X, _ACTS, "X")
     m, k = x.shape
     n, k, levels = _weights(codes, scales, k, group, levels)
@@ -1041,6 +1066,10 @@ def kq_group_linear(X, codes, scales, group: int = 128, levels=None, bias=None, 
 
 def kq_group_linear_grad_input(dY, codes, scales, in_features: int, group: int = 128, levels=None, dX=None, workspace=None):
     """dX = dY W_hat: dY [..., n] bf16 or fp16, dX [..., in_features] in its type."""
+    if _fast is not None and workspace is None:
+        r = _fast.grad_input(dY, codes, scales, in_features, group, levels, dX)
+        if r is not None:
+            return r
     dy, ty, ldy = _rows(dY, _ACTS, "dY")
     n, k, levels = _weights(codes, scales, in_features, group, levels)
     m = dy.shape[0]
@@ -1064,6 +1093,10 @@ def _checkpoint_shapes(m, k):
 def kq_checkpoint_pack(X, q=None, exps=None):
     """An activation [..., k] (fp32, bf16 or fp16) in 8 bits: int8 values and a power of two for 32 neighbours.
     Returns (q int8 [m, k rounded up to 32], exps uint8 [m, that / 32]), m the product of the leading sizes."""
+    if _fast is not None and q is None and exps is None:
+        r = _fast.checkpoint_pack(X)
+        if r is not None:
+            return r
     x, ty, ld = _rows(X, _TYPES, "X")
     m, k = x.shape
     dev = x.device
@@ -1089,6 +1122,10 @@ def _checkpoint(q, exps, k):
 
 def kq_checkpoint_restore(q, exps, in_features: int, dtype=torch.float32, X_hat=None):
     """The activation that a checkpoint stands for, [m, in_features] of `dtype` (or X_hat's)."""
+    if _fast is not None and X_hat is None:
+        r = _fast.checkpoint_restore(q, exps, in_features, _TYPES.get(dtype, -1))
+        if r is not None:
+            return r
     m, k = _checkpoint(q, exps, in_features)
     if X_hat is None:
         if dtype not in _TYPES:
@@ -1123,6 +1160,10 @@ def kq_checkpoint_grad_scales(dY, q, exps, codes, in_features: int, group: int =
     """Gradient of the group scales (fp32 [n, groups]) from dY [..., n] and the checkpoint of X: the sum of level *
     (dY^T X_hat) over each group, without the product in memory.  bias: also dbias = the column sums of dY.
     Returns (dscales, dbias or None)."""
+    if _fast is not None and dscales is None and dbias is None and workspace is None:
+        r = _fast.grad_scales(dY, q, exps, codes, in_features, group, levels, bias)
+        if r is not None:
+            return r
     m, k = _checkpoint(q, exps, in_features)
     n = dY.shape[-1] if isinstance(dY, torch.Tensor) and dY.dim() else 0
     dy, ty, ldy = _grad_rows(dY, q, m, n)
@@ -1143,6 +1184,10 @@ def kq_checkpoint_grad_scales(dY, q, exps, codes, in_features: int, group: int =
 def kq_checkpoint_grad_weight(dY, q, exps, in_features: int, bias: bool = False, dW=None, dbias=None, workspace=None):
     """Gradient of a whole weight matrix, dY^T X_hat (fp32 [n, in_features]), from the checkpoint of X.  bias: also
     the column sums of dY.  Returns (dW, dbias or None)."""
+    if _fast is not None and dW is None and dbias is None and workspace is None:
+        r = _fast.grad_weight(dY, q, exps, in_features, bias)
+        if r is not None:
+            return r
     m, k = _checkpoint(q, exps, in_features)
     n = dY.shape[-1] if isinstance(dY, torch.Tensor) and dY.dim() else 0
     dy, ty, ldy = _grad_rows(dY, q, m, n)
