@@ -622,7 +622,7 @@ kq_status kq_fit_layer_noalloc(const float* X, int64_t n, int32_t dim, int32_t k
 #define KQ_T_BF16 1
 #define KQ_T_F16 2
 #define KQ_GROUP_MAX_FEATURES (1 << 24)
-#define KQ_GROUP_MAX_VALUES ((int64_t)1 << 36)
+#define KQ_GROUP_MAX_VALUES ((int64_t)1 << 34)
 #define KQ_GROUP_MAX_ROWS (1 << 30)
 size_t kq_group_code_bytes(int64_t n, int64_t k);
 kq_status kq_quantize_groups(const void* W, int32_t type, int64_t ldw, int64_t n, int64_t k, int32_t group,

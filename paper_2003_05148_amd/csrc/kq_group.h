@@ -73,6 +73,30 @@ struct LevelTable {
     unsigned lo[4], hi[4];  // low and high bytes of the 16-bit levels, four a register
 };
 
+template <bool BF>
+__device__ __forceinline__ LevelTable load_levels(const uint16_t* levels) {
+    LevelTable t;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        unsigned a, b;  // levels 4 r .. 4 r + 3 in two registers
+        if constexpr (BF) {
+            a = (unsigned)levels[4 * r] | (unsigned)levels[4 * r + 1] << 16;
+            b = (unsigned)levels[4 * r + 2] | (unsigned)levels[4 * r + 3] << 16;
+        } else {  // fp16 holds a bf16 level exactly from 2^-14 on, and to 2^-25 below
+            a = Act<false>::pack(bf16_bits_to_f32(levels[4 * r]), bf16_bits_to_f32(levels[4 * r + 1]));
+            b = Act<false>::pack(bf16_bits_to_f32(levels[4 * r + 2]), bf16_bits_to_f32(levels[4 * r + 3]));
+        }
+        t.lo[r] = __builtin_amdgcn_perm(b, a, 0x06040200u);
+        t.hi[r] = __builtin_amdgcn_perm(b, a, 0x07050301u);
+    }
+    return t;
+}
+
+// the bytes of a 16-entry table at four indices (0..15, one a byte)
+__device__ __forceinline__ unsigned look_up(const unsigned (&t)[4], unsigned low3, unsigned pick) {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(t[3], t[2], low3), __builtin_amdgcn_perm(t[1], t[0], low3), pick);
+}
+
 // ---- device parameters and launchers (checked by the C entry points before) ------------------------
 
 struct GroupWeights {
@@ -157,10 +181,22 @@ struct GemmPlan {
 GemmPlan gemm_plan(Product mode, int64_t I, int64_t J, int64_t C, int groups);
 hipError_t launch_gemm(Product mode, bool bf16, const GemmPlan& plan, GemmParams p, hipStream_t s);
 
+// out[r][c] = sum over the splits of part[split][r][c], in order, + bias[c]
+struct JoinParams {
+    const float* part;
+    int splits;
+    int64_t rows, cols;
+    const float* bias;
+    void* out;
+    int64_t ldo;
+    int type;
+};
+hipError_t launch_join(const JoinParams& p, hipStream_t s);
+
 // Y = X W^T for at most kMatvecRows rows of X.
 constexpr int kMatvecRows = 16;
 constexpr int kMatvecLdsRows = 4;         // up to so many rows of X go through LDS
-constexpr int kMatvecLdsBytes = 32768;
+constexpr int kMatvecLdsBytes = 65536;
 struct MatvecParams {
     GroupWeights w;
     const void* X;
@@ -174,7 +210,7 @@ struct MatvecParams {
     int chunk;
 };
 struct MatvecPlan {
-    int splits, blocks_per_split;
+    int row_tiles, waves, splits, blocks_per_split;
     size_t ws_bytes;
 };
 MatvecPlan matvec_plan(int m, int64_t n, int64_t k);

@@ -75,13 +75,12 @@ __device__ __forceinline__ unsigned max_bits(const float (&v)[8]) {
 }
 
 // ---- quantizer -----------------------------------------------------------------------------------------
-// One wave per 16 x 128 tile of codes; lane (row r, quarter q) = (lane / 4, lane % 4) takes the four dwords
-// of its 16 bytes: columns 32 i + 8 q + 0..7 for i = 0..3, so the lanes of a row read 32 consecutive columns
-// at a time and a group's columns lie in the row's four lanes.  Per group: a = max |w| (a non-finite value is
-// larger than every other), s = bf16(a / top) with top = 7 or the largest |level| (zero below the normal
-// range, NaN where a is not finite), and per weight t = w / s in fp32 and the nearest level to t, the lower
-// one of two that are as near: for -8 .. 7 by rounding, for a table by counting the midpoints of
-// neighbouring levels below t.
+// Sixteen lanes a row of a 16 x 128 tile, 8 neighbouring columns and one dword of codes a lane, four rows a
+// wave: a row's lanes read contiguous memory, and a group's columns lie in 4, 8 or 16 neighbouring lanes.
+// Per group: a = max |w| (a non-finite value is larger than every other), s = bf16(a / top) with top = 7 or
+// the largest |level| (zero below the normal range, NaN where a is not finite), and per weight t = w / s in
+// fp32 and the nearest level to t, the lower one of two that are as near: for -8 .. 7 by rounding, for a
+// table by a binary search of the midpoints of neighbouring levels, the midpoints below t being counted.
 __device__ __forceinline__ unsigned nearest_integer_code(float t) {
     float r = __builtin_rintf(t);       // ties to even
     if (r - t == 0.5f) r -= 1.0f;       // a tie that went up
@@ -91,90 +90,64 @@ __device__ __forceinline__ unsigned nearest_integer_code(float t) {
 
 template <int TYPE, bool LUT>
 __global__ __launch_bounds__(256) void quantize_groups_kernel(const QuantizeParams p) {
-    const int lane = threadIdx.x & 63;
-    const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, l16 = lane & 15;
+    const int64_t id = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);  // row of a tile: tile * 16 + row
+    const int64_t tile = id >> 4;
     const int64_t tiles = (int64_t)ceil_div(p.n, kTileRows) * p.ktiles;
-    if (tile >= tiles) return;
-    const int nt = (int)(tile / p.ktiles), kt = (int)(tile % p.ktiles);
-    const int row = nt * kTileRows + (lane >> 2), q = lane & 3;
-    const bool live = row < p.n;
-    const int limit = live ? p.k : 0;
-    const int64_t at = (int64_t)row * p.ldw;
-
-    float mid[15];
+    __shared__ float s_mid[16];
     float top = 7.0f;
     if constexpr (LUT) {
-        float prev = bf16_bits_to_f32(p.levels[0]);
-        top = __builtin_fabsf(prev);
+        if (threadIdx.x < 15)
+            s_mid[threadIdx.x] = 0.5f * (bf16_bits_to_f32(p.levels[threadIdx.x]) + bf16_bits_to_f32(p.levels[threadIdx.x + 1]));
+        top = 0.0f;
 #pragma unroll
-        for (int j = 1; j < 16; ++j) {
-            const float l = bf16_bits_to_f32(p.levels[j]);
-            mid[j - 1] = 0.5f * (prev + l);
-            top = __builtin_fmaxf(top, __builtin_fabsf(l));
-            prev = l;
-        }
+        for (int j = 0; j < 16; ++j) top = __builtin_fmaxf(top, __builtin_fabsf(bf16_bits_to_f32(p.levels[j])));
+        __syncthreads();
     }
-
-    float v[4][8];
-    unsigned a[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        load_columns<TYPE>(p.W, at, kt * kTileCols + 32 * i + 8 * q, limit, v[i]);
-        a[i] = max_bits(v[i]);
+    if (tile >= tiles) return;  // (all lanes of a row, and of the workgroup's rows of the tile)
+    const int nt = (int)(tile / p.ktiles), kt = (int)(tile - (int64_t)nt * p.ktiles);
+    const int row = nt * kTileRows + (int)(id & 15);
+    const bool live = row < p.n;
+    const int limit = live ? p.k : 0;
+    const int c0 = kt * kTileCols + 8 * l16;
+    float v[8];
+    load_columns<TYPE>(p.W, (int64_t)row * p.ldw, c0, limit, v);
+    unsigned a = max_bits(v);
+    for (int off = 1; off < 1 << (p.log_group - 3); off <<= 1) {
+        const unsigned o = __shfl_xor(a, off);
+        a = o > a ? o : a;
     }
-    // largest magnitude of each 32-column block over the row's four lanes, then over the group's blocks
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-#pragma unroll
-        for (int off = 1; off <= 2; off <<= 1) {
-            const unsigned o = __shfl_xor(a[i], off);
-            a[i] = o > a[i] ? o : a[i];
-        }
+    float s;
+    if (a >= 0x7f800000u) {
+        s = __builtin_bit_cast(float, 0x7fc00000u);
+    } else {
+        s = bf16_bits_to_f32(Act<true>::one(__builtin_bit_cast(float, a) / top));
+        if (s < 0x1p-126f) s = 0.0f;
     }
-    if (p.log_group >= 6) {
-        a[0] = a[1] = a[0] > a[1] ? a[0] : a[1];
-        a[2] = a[3] = a[2] > a[3] ? a[2] : a[3];
-    }
-    if (p.log_group >= 7) a[0] = a[1] = a[2] = a[3] = a[0] > a[2] ? a[0] : a[2];
-
-    unsigned dw[4];
+    if (live && c0 < p.k && (c0 & ((1 << p.log_group) - 1)) == 0)
+        p.scales[(int64_t)row * p.groups + (c0 >> p.log_group)] = (uint16_t)(__builtin_bit_cast(unsigned, s) >> 16);
+    unsigned d = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float s;
-        if (a[i] >= 0x7f800000u) {
-            s = __builtin_bit_cast(float, 0x7fc00000u);
+    for (int j = 0; j < 8; ++j) {
+        const float t = s > 0.0f ? v[j] / s : 0.0f;
+        unsigned code;
+        if constexpr (LUT) {
+            code = 0;
+#pragma unroll
+            for (int step = 8; step >= 1; step >>= 1) code += t > s_mid[code + step - 1] ? step : 0;
         } else {
-            s = bf16_bits_to_f32(Act<true>::one(__builtin_bit_cast(float, a[i]) / top));
-            if (s < 0x1p-126f) s = 0.0f;
+            code = nearest_integer_code(t);
         }
-        const int c0 = kt * kTileCols + 32 * i;
-        const int g = c0 >> p.log_group;
-        if (q == 0 && live && c0 < p.k && (c0 & ((1 << p.log_group) - 1)) == 0)
-            p.scales[(int64_t)row * p.groups + g] = (uint16_t)(__builtin_bit_cast(unsigned, s) >> 16);
-        unsigned d = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float t = s > 0.0f ? v[i][j] / s : 0.0f;
-            unsigned code;
-            if constexpr (LUT) {
-                code = 0;
-#pragma unroll
-                for (int b = 0; b < 15; ++b) code += t > mid[b] ? 1u : 0u;
-            } else {
-                code = nearest_integer_code(t);
-            }
-            if (c0 + 8 * q + j >= limit) code = 0;
-            d |= code << (4 * ((j & 1) * 4 + (j >> 1)));
-        }
-        dw[i] = d;
+        if (c0 + j >= limit) code = 0;
+        d |= code << (4 * ((j & 1) * 4 + (j >> 1)));
     }
-    u32x4 o = {dw[0], dw[1], dw[2], dw[3]};
-    *(u32x4*)(p.codes + tile * kTileBytes + lane * 16) = o;
+    // columns 8 l .. 8 l + 7 are dword 4 (l % 4) + l / 4 of the row
+    *(unsigned*)(p.codes + id * 64 + ((l16 & 3) * 4 + (l16 >> 2)) * 4) = d;
 }
 
 hipError_t launch_quantize_groups(const QuantizeParams& p, hipStream_t s) {
     const int64_t tiles = (int64_t)ceil_div(p.n, kTileRows) * p.ktiles;
-    const dim3 grid((unsigned)ceil_div64(tiles, 4)), block(256);
+    const dim3 grid((unsigned)tiles), block(256);
     const bool lut = p.levels != nullptr;
 #define KQ_LAUNCH(T)                                                        \
     if (lut) quantize_groups_kernel<T, true><<<grid, block, 0, s>>>(p);     \
@@ -187,39 +160,40 @@ hipError_t launch_quantize_groups(const QuantizeParams& p, hipStream_t s) {
 }
 
 // ---- reconstruction: W_hat[n][k] = scale * level -----------------------------------------------------------
-// The quantizer's layout backwards: one wave per tile, 16 bytes of codes a lane.
+// A workgroup a tile, 16 lanes a row.  A lane writes four neighbouring columns at a time, 4 l + 64 h, so a
+// row's lanes write contiguous memory; two lanes share a dword of codes.
 template <int TYPE, bool LUT>
 __global__ __launch_bounds__(256) void reconstruct_groups_kernel(const ReconstructGroupsParams p) {
-    const int lane = threadIdx.x & 63;
-    const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int64_t tiles = (int64_t)p.w.ntiles * p.w.ktiles;
+    const int l16 = threadIdx.x & 15;
+    const int64_t tile = blockIdx.x;
     __shared__ float s_level[16];
-    if (threadIdx.x < 16)
-        s_level[threadIdx.x] = LUT ? bf16_bits_to_f32(p.w.levels[threadIdx.x]) : (float)((int)threadIdx.x - 8);
-    __syncthreads();
-    if (tile >= tiles) return;
-    const int nt = (int)(tile / p.w.ktiles), kt = (int)(tile % p.w.ktiles);
-    const int row = nt * kTileRows + (lane >> 2), q = lane & 3;
+    if constexpr (LUT) {
+        if (threadIdx.x < 16) s_level[threadIdx.x] = bf16_bits_to_f32(p.w.levels[threadIdx.x]);
+        __syncthreads();
+    }
+    const int nt = (int)(tile / p.w.ktiles), kt = (int)(tile - (int64_t)nt * p.w.ktiles);
+    const int r = threadIdx.x >> 4, row = nt * kTileRows + r;
     if (row >= p.w.n) return;
-    const u32x4 dw = *(const u32x4*)(p.w.codes + tile * kTileBytes + lane * 16);
+    const unsigned* codes = (const unsigned*)(p.w.codes + tile * kTileBytes + r * 64);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int c0 = kt * kTileCols + 32 * i + 8 * q;
+    for (int h = 0; h < 2; ++h) {
+        const int cc = 64 * h + 4 * l16, c0 = kt * kTileCols + cc;  // dword 4 q + i of columns 32 i + 8 q
         if (c0 >= p.w.k) break;
+        const unsigned d = codes[((cc >> 3) & 3) * 4 + (cc >> 5)] >> (8 * (l16 & 1));
         const float s = bf16_bits_to_f32(p.w.scales[(int64_t)row * p.w.groups + (c0 >> p.w.log_group)]);
-        float v[8];
+        float v[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const unsigned code = (dw[i] >> (4 * ((j & 1) * 4 + (j >> 1)))) & 15u;
+        for (int j = 0; j < 4; ++j) {  // the second four columns are the second nibble of each pair
+            const unsigned code = (d >> (16 * (j & 1) + 4 * (j >> 1))) & 15u;
             v[j] = s * (LUT ? s_level[code] : (float)((int)code - 8));
         }
-        store_values<TYPE, 8>(p.W_hat, (int64_t)row * p.ldw + c0, v, p.w.k - c0);
+        store_values<TYPE, 4>(p.W_hat, (int64_t)row * p.ldw + c0, v, p.w.k - c0);
     }
 }
 
 hipError_t launch_reconstruct_groups(const ReconstructGroupsParams& p, hipStream_t s) {
     const int64_t tiles = (int64_t)p.w.ntiles * p.w.ktiles;
-    const dim3 grid((unsigned)ceil_div64(tiles, 4)), block(256);
+    const dim3 grid((unsigned)tiles), block(256);
     const bool lut = p.w.levels != nullptr;
 #define KQ_LAUNCH(T)                                                           \
     if (lut) reconstruct_groups_kernel<T, true><<<grid, block, 0, s>>>(p);     \
@@ -325,33 +299,78 @@ hipError_t launch_checkpoint_pack(const CheckpointParams& p, hipStream_t s) { re
 hipError_t launch_checkpoint_restore(const CheckpointParams& p, hipStream_t s) { return launch_checkpoint<false>(p, s); }
 
 // ---- bias gradient: dbias[n] = sum_m dY[m][n] ------------------------------------------------------------------
-// A workgroup adds 32 columns: 4 lanes of 8 columns, 64 rows at a time, then the 64 partial sums in order.
+// A workgroup of 512 threads adds 32 columns: four lanes of 8 columns a row, 128 rows at a time; 16 lanes'
+// sums are added by a butterfly, then the eight waves' in order.
 template <bool BF>
-__global__ __launch_bounds__(256) void bias_grad_kernel(const BiasGradParams p) {
-    __shared__ float s_part[64][33];
-    const int cl = threadIdx.x & 3, rl = threadIdx.x >> 2;
-    const int c0 = blockIdx.x * 32 + cl * 8;
+__global__ __launch_bounds__(512) void bias_grad_kernel(const BiasGradParams p) {
+    __shared__ float s_part[8][32];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int c0 = blockIdx.x * 32 + 8 * (lane & 3);
     float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (int64_t r = rl; r < p.m; r += 64) {
+#pragma unroll 4
+    for (int64_t r = threadIdx.x >> 2; r < p.m; r += 128) {
         float v[8];
         load_columns<BF ? KQ_T_BF16 : KQ_T_F16>(p.dY, r * p.ldy, c0, p.n, v);
 #pragma unroll
         for (int t = 0; t < 8; ++t) acc[t] += v[t];
     }
 #pragma unroll
-    for (int t = 0; t < 8; ++t) s_part[rl][cl * 8 + t] = acc[t];
+    for (int t = 0; t < 8; ++t) {
+#pragma unroll
+        for (int off = 4; off < 64; off <<= 1) acc[t] += __shfl_xor(acc[t], off);
+        if (lane < 4) s_part[wave][8 * lane + t] = acc[t];
+    }
     __syncthreads();
-    if (threadIdx.x < 32 && (int)(blockIdx.x * 32 + threadIdx.x) < p.n) {
-        float v = 0.0f;
-        for (int r = 0; r < 64; ++r) v += s_part[r][threadIdx.x];
-        p.dbias[blockIdx.x * 32 + threadIdx.x] = v;
+    const int c = blockIdx.x * 32 + threadIdx.x;
+    if (threadIdx.x < 32 && c < p.n) {
+        float v = s_part[0][threadIdx.x];
+        for (int w = 1; w < 8; ++w) v += s_part[w][threadIdx.x];
+        p.dbias[c] = v;
     }
 }
 
 hipError_t launch_bias_grad(const BiasGradParams& p, hipStream_t s) {
-    const dim3 grid((unsigned)ceil_div(p.n, 32)), block(256);
+    const dim3 grid((unsigned)ceil_div(p.n, 32)), block(512);
     if (p.type == KQ_T_BF16) bias_grad_kernel<true><<<grid, block, 0, s>>>(p);
     else bias_grad_kernel<false><<<grid, block, 0, s>>>(p);
+    return hipGetLastError();
+}
+
+// ---- partial sums of a split contraction -------------------------------------------------------------------------
+template <int TYPE>
+__global__ __launch_bounds__(256) void join_kernel(const JoinParams p) {
+    const int64_t per_row = (p.cols + 3) >> 2, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t r = id / per_row, c = (id - r * per_row) * 4, total = p.rows * p.cols;
+    if (r >= p.rows) return;
+    float v[4] = {0, 0, 0, 0};
+    const float* part = p.part + r * p.cols + c;
+    const int count = (int)min((int64_t)4, p.cols - c);
+    if (count == 4) {
+        for (int s = 0; s < p.splits; ++s, part += total) {
+            float x[4];
+            __builtin_memcpy(x, part, 16);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) v[t] += x[t];
+        }
+    } else {
+        for (int s = 0; s < p.splits; ++s, part += total)
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                if (t < count) v[t] += part[t];
+    }
+    if (p.bias) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+            if (t < count) v[t] += p.bias[c + t];
+    }
+    store_values<TYPE, 4>(p.out, r * p.ldo + c, v, count);
+}
+
+hipError_t launch_join(const JoinParams& p, hipStream_t s) {
+    const dim3 grid((unsigned)ceil_div64(p.rows * ((p.cols + 3) >> 2), 256)), block(256);
+    if (p.type == KQ_T_F32) join_kernel<KQ_T_F32><<<grid, block, 0, s>>>(p);
+    else if (p.type == KQ_T_BF16) join_kernel<KQ_T_BF16><<<grid, block, 0, s>>>(p);
+    else join_kernel<KQ_T_F16><<<grid, block, 0, s>>>(p);
     return hipGetLastError();
 }
 

@@ -15,30 +15,6 @@ namespace kq {
 
 // ---- codes to 16-bit values -------------------------------------------------------------------------------
 
-template <bool BF>
-__device__ __forceinline__ LevelTable load_levels(const uint16_t* levels) {
-    LevelTable t;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        unsigned a, b;  // levels 4 r .. 4 r + 3 in two registers
-        if constexpr (BF) {
-            a = (unsigned)levels[4 * r] | (unsigned)levels[4 * r + 1] << 16;
-            b = (unsigned)levels[4 * r + 2] | (unsigned)levels[4 * r + 3] << 16;
-        } else {  // fp16 holds a bf16 level exactly from 2^-14 on, and to 2^-25 below
-            a = Act<false>::pack(bf16_bits_to_f32(levels[4 * r]), bf16_bits_to_f32(levels[4 * r + 1]));
-            b = Act<false>::pack(bf16_bits_to_f32(levels[4 * r + 2]), bf16_bits_to_f32(levels[4 * r + 3]));
-        }
-        t.lo[r] = __builtin_amdgcn_perm(b, a, 0x06040200u);
-        t.hi[r] = __builtin_amdgcn_perm(b, a, 0x07050301u);
-    }
-    return t;
-}
-
-// the bytes of a 16-entry table at four indices (0..15, one a byte)
-__device__ __forceinline__ unsigned look_up(const unsigned (&t)[4], unsigned low3, unsigned pick) {
-    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(t[3], t[2], low3), __builtin_amdgcn_perm(t[1], t[0], low3), pick);
-}
-
 // the 8 columns of a dword of codes, in order: levels, or 16 + q without a table
 template <bool BF, bool LUT>
 __device__ __forceinline__ u32x4 decode(unsigned d, const LevelTable& t) {
@@ -67,9 +43,9 @@ __device__ __forceinline__ u32x4 decode(unsigned d, const LevelTable& t) {
 }
 
 // 8 neighbours of a row of X from column c, zeros from `limit` on
-__device__ __forceinline__ u32x4 load_x(const uint16_t* row, int c, int limit) {
+__device__ __forceinline__ u32x4 load_x(const uint16_t* row, int c, int limit, bool full) {
     u32x4 v;
-    if (c + 8 <= limit) {
+    if (full || c + 8 <= limit) {
         __builtin_memcpy(&v, row + c, 16);
     } else {
 #pragma unroll
@@ -82,119 +58,118 @@ __device__ __forceinline__ u32x4 load_x(const uint16_t* row, int c, int limit) {
     return v;
 }
 
-// MT: 16-row tiles of X.  XLDS: X (at most kMatvecLdsRows rows) is staged through LDS in chunks of
-// p.chunk blocks; otherwise its fragments are loaded from the caches.
-template <bool BF, bool LUT, int MT, int WAVES, int U, bool XLDS>
+// GPB: groups a block (1, 2 or 4).  RT: 16-row tiles of W a workgroup takes.  XLDS: X (at most
+// kMatvecLdsRows rows) is staged through LDS in chunks of p.chunk blocks; otherwise its fragments come from
+// the caches with the codes.  A wave loads its next block while it multiplies the one before.
+template <bool BF, bool LUT, int GPB, int WAVES, int RT, bool XLDS>
 __global__ __launch_bounds__(64 * WAVES) void group_matvec_kernel(const MatvecParams p) {
-    constexpr int kSumBytes = WAVES * MT * 64 * 16;
+    constexpr int kSumBytes = WAVES * RT * 64 * 16;
     constexpr int kXBytes = XLDS ? kMatvecLdsBytes : 0;
+    constexpr int kPieces = 4 / GPB;  // 32-column pieces a group
     __shared__ u32x4 s_buf[(kSumBytes > kXBytes ? kSumBytes : kXBytes) / 16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r16 = lane & 15, q = lane >> 4;
-    const int nt = blockIdx.x;
-    const int n = nt * kTileRows + r16;
+    const int nt0 = blockIdx.x * RT;
     const int k_begin = blockIdx.y * p.blocks_per_split;
     const int k_end = min(k_begin + p.blocks_per_split, p.w.ktiles);
-    const uint8_t* codes = p.w.codes + (int64_t)nt * p.w.ktiles * kTileBytes + r16 * 64 + q * 16;
-    const uint16_t* scales = p.w.scales + (int64_t)min(n, p.w.n - 1) * p.w.groups;
-    const int gpb = kTileCols >> p.w.log_group;  // groups a block: 1, 2 or 4
+    // row tiles and rows past the last repeat it: what they give is not stored
+    const uint8_t* codes[RT];
+    const uint16_t* scales[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        codes[t] = p.w.codes + (int64_t)min(nt0 + t, p.w.ntiles - 1) * p.w.ktiles * kTileBytes;
+        scales[t] = p.w.scales + (int64_t)min((nt0 + t) * kTileRows + r16, p.w.n - 1) * p.w.groups;
+    }
+    const unsigned code_off = r16 * 64 + q * 16;
+    const uint16_t* xrow = (const uint16_t*)p.X + (int64_t)min(r16, p.m - 1) * p.ldx;
 
-    LevelTable table;
-    if constexpr (LUT) table = load_levels<BF>(p.w.levels);
     const unsigned offset_bits = BF ? 0xc1c0c1c0u : 0xce00ce00u;  // a pair of -24
     const u32x4 offset = {offset_bits, offset_bits, offset_bits, offset_bits};
-
-    const uint16_t* xrow[MT];
+    LevelTable table;
+    f32x4 y[RT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) xrow[t] = (const uint16_t*)p.X + (int64_t)min(16 * t + r16, p.m - 1) * p.ldx;
-
-    f32x4 y[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) y[t] = f32x4{0, 0, 0, 0};
+    for (int t = 0; t < RT; ++t) y[t] = f32x4{0, 0, 0, 0};
 
     const int chunk = XLDS ? p.chunk : k_end - k_begin;
     const int pitch = chunk * 16 + 4;  // 16-byte pieces of a staged row: rows 64 bytes apart in the banks
+    struct Block {
+        u32x4 codes[RT], x[XLDS ? 1 : 4];
+        unsigned short s[RT][GPB];
+    };
+    auto fetch = [&](Block& f, int kb) {  // past the end, the last block again
+        const int b = min(kb, p.w.ktiles - 1);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            f.codes[t] = *(const u32x4*)(codes[t] + (int64_t)b * kTileBytes + code_off);
+            if (GPB == 1 || (b + 1) * GPB <= p.w.groups) {
+                __builtin_memcpy(f.s[t], scales[t] + b * GPB, 2 * GPB);
+            } else {
+#pragma unroll
+                for (int g = 0; g < GPB; ++g) f.s[t][g] = scales[t][min(b * GPB + g, p.w.groups - 1)];
+            }
+        }
+        if constexpr (!XLDS) {
+            const bool full = (b + 1) * kTileCols <= p.w.k;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f.x[i] = load_x(xrow, b * kTileCols + 32 * i + 8 * q, p.w.k, full);
+        }
+    };
     for (int c0 = k_begin; c0 < k_end; c0 += chunk) {
         const int c1 = min(c0 + chunk, k_end);
-        u32x4 next[U];
-        unsigned short ns[U][4];
-        auto fetch = [&](int kb) {  // blocks kb, kb + WAVES, ...
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int b = min(kb + u * WAVES, p.w.ktiles - 1);
-                next[u] = *(const u32x4*)(codes + (int64_t)b * kTileBytes);
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    if (g < gpb) ns[u][g] = scales[min(b * gpb + g, p.w.groups - 1)];
-            }
-        };
-        fetch(c0 + wave);
+        Block next;
+        fetch(next, c0 + wave);
+        if constexpr (LUT) table = load_levels<BF>(p.w.levels);  // (after the loads that take longest)
         if constexpr (XLDS) {
             __syncthreads();  // the previous chunk is read
             const int pieces = (c1 - c0) * 16;
-            for (int id = threadIdx.x; id < p.m * pieces; id += 64 * WAVES) {
-                const int r = id / pieces, ch = id - r * pieces;
-                s_buf[r * pitch + ch] = load_x((const uint16_t*)p.X + (int64_t)r * p.ldx, c0 * kTileCols + ch * 8, p.w.k);
-            }
+            for (int r = 0; r < p.m; ++r)
+                for (int ch = threadIdx.x; ch < pieces; ch += 64 * WAVES)
+                    s_buf[r * pitch + ch] = load_x((const uint16_t*)p.X + (int64_t)r * p.ldx, c0 * kTileCols + ch * 8, p.w.k, false);
             __syncthreads();
         }
-        for (int kb = c0 + wave; kb < c1; kb += U * WAVES) {
-            u32x4 cur[U];
-            unsigned short cs[U][4];
+        for (int b = c0 + wave; b < c1; b += WAVES) {
+            const Block cur = next;
+            if (b + WAVES < c1) fetch(next, b + WAVES);
+            f32x4 acc[RT], base;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                cur[u] = next[u];
+            for (int i = 0; i < 4; ++i) {
+                u32x4 x;
+                if constexpr (XLDS) x = s_buf[min(r16, p.m - 1) * pitch + (b - c0) * 16 + 4 * i + q];
+                else x = cur.x[i];
+                if (i % kPieces == 0) base = f32x4{0, 0, 0, 0};
+                if constexpr (!LUT) base = Act<BF>::mfma(x, offset, base);  // once for all row tiles
 #pragma unroll
-                for (int g = 0; g < 4; ++g) cs[u][g] = ns[u][g];
-            }
-            if (kb + U * WAVES < c1) fetch(kb + U * WAVES);
+                for (int t = 0; t < RT; ++t) {
+                    const u32x4 w = decode<BF, LUT>(cur.codes[t][i], table);
+                    if (i % kPieces == 0) acc[t] = f32x4{0, 0, 0, 0};
+                    acc[t] = Act<BF>::mfma(x, w, acc[t]);
+                    if ((i + 1) % kPieces == 0) {  // the group's last piece
+                        if constexpr (!LUT) acc[t] += base;
+                        const float s = bf16_bits_to_f32(cur.s[t][i / kPieces]);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int b = kb + u * WAVES;
-                if (b < c1) {
-                    f32x4 acc[MT];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const u32x4 w = decode<BF, LUT>(cur[u][i], table);
-                        const int col = b * kTileCols + 32 * i + 8 * q;
-                        const bool first = (i & ((1 << (p.w.log_group - 5)) - 1)) == 0;
-#pragma unroll
-                        for (int t = 0; t < MT; ++t) {
-                            u32x4 x;
-                            if constexpr (XLDS) x = s_buf[min(r16, p.m - 1) * pitch + (b - c0) * 16 + 4 * i + q];
-                            else x = load_x(xrow[t], col, p.w.k);
-                            if (first) acc[t] = f32x4{0, 0, 0, 0};
-                            if constexpr (!LUT) acc[t] = Act<BF>::mfma(x, offset, acc[t]);
-                            acc[t] = Act<BF>::mfma(x, w, acc[t]);
-                        }
-                        if (((i + 1) & ((1 << (p.w.log_group - 5)) - 1)) == 0) {
-                            const int g = i >> (p.w.log_group - 5);
-                            const float s = bf16_bits_to_f32(g == 0 ? cs[u][0] : g == 1 ? cs[u][1] : g == 2 ? cs[u][2] : cs[u][3]);
-#pragma unroll
-                            for (int t = 0; t < MT; ++t)
-#pragma unroll
-                                for (int r = 0; r < 4; ++r) y[t][r] = __builtin_fmaf(s, acc[t][r], y[t][r]);
-                        }
+                        for (int r = 0; r < 4; ++r) y[t][r] = __builtin_fmaf(s, acc[t][r], y[t][r]);
                     }
                 }
             }
         }
     }
 
-    // lane holds Y[16 t + 4 q + r][n]: the waves' sums in order
+    // lane holds Y[4 q + r][16 (nt0 + t) + r16]: the waves' sums in order
     if constexpr (XLDS) __syncthreads();
     f32x4* s_sum = (f32x4*)s_buf;
 #pragma unroll
-    for (int t = 0; t < MT; ++t) s_sum[(t * WAVES + wave) * 64 + lane] = y[t];
+    for (int t = 0; t < RT; ++t) s_sum[(t * WAVES + wave) * 64 + lane] = y[t];
     __syncthreads();
-    for (int t = wave; t < MT; t += WAVES) {
-        f32x4 v = s_sum[t * WAVES * 64 + lane];
-        for (int w = 1; w < WAVES; ++w) v += s_sum[(t * WAVES + w) * 64 + lane];
+    if (wave < RT) {
+        f32x4 v = s_sum[wave * WAVES * 64 + lane];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v += s_sum[(wave * WAVES + w) * 64 + lane];
+        const int n = (nt0 + wave) * kTileRows + r16;
         if (n < p.w.n) {
             const float bias = p.bias && !p.part ? p.bias[n] : 0.0f;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int m = 16 * t + 4 * q + r;
+                const int m = 4 * q + r;
                 if (m < p.m) {
                     if (p.part) p.part[((int64_t)blockIdx.y * p.m + m) * p.w.n + n] = v[r];
                     else ((uint16_t*)p.Y)[(int64_t)m * p.ldy + n] = Act<BF>::one(v[r] + bias);
@@ -204,32 +179,72 @@ __global__ __launch_bounds__(64 * WAVES) void group_matvec_kernel(const MatvecPa
     }
 }
 
+// Row tiles a workgroup takes, splits of the columns and waves.  A workgroup's time grows with the bytes of X
+// it reads beside its codes, so several row tiles share a workgroup's X where X is long or there are more row
+// tiles than the chip has room for; the columns are split where the workgroups would not fill the chip and
+// are long enough to pay for the joining launch (about 3 us).  Measured (us, rows of X / n x k, group 128;
+// row tiles x splits):
+//   16 / 4096 x 25088: 1x1 27.9, 2x2 20.1, 4x4 17.5    8 / 4096 x 12288: 1x1 13.1, 2x2 12.4, 4x4 12.4
+//   16 / 4096 x 8192:  1x1 12.2, 2x2 11.2, 4x4 11.4    16 / 8192 x 8192: 1x1 22.0, 2x1 15.2, 4x2 15.2
+//   16 / 1000 x 8192:  1x1 11.9, 1x2 9.5, 1x4 7.7      16 / 1000 x 25088: 1x1 27.5, 1x4 11.8, 4x8 12.8
+//    1 / 1000 x 4096:  1x1 4.9, 1x2 7.7                 1 / 1000 x 25088: 1x1 10.5, 1x2 9.7, 1x4 8.0
+// and of waves: 1 / 4096 x 25088, 8 waves 13.1, 16 waves 11.4; 1 / 4096 x 4096, 4 waves 5.2, 8 4.4, 16 4.4;
+// 1 / 1000 x 512 (kernel alone), 4 waves 3.2, 8 3.8, 16 4.7.
 MatvecPlan matvec_plan(int m, int64_t n, int64_t k) {
     MatvecPlan v = {};
-    v.splits = 1;
-    v.blocks_per_split = (int)ceil_div64(k, kTileCols);
-    v.ws_bytes = 0;
+    const int64_t blocks = ceil_div64(k, kTileCols), tiles = ceil_div64(n, kTileRows);
+    const bool lds = m <= kMatvecLdsRows;
+    v.row_tiles = lds ? 1 : tiles >= 1024 || (blocks >= 96 && tiles > 128) ? 4 : tiles >= 512 ? 2 : 1;
+    const int64_t groups = ceil_div64(tiles, v.row_tiles), room = groups < 256 ? 256 / groups : 1;
+    const int64_t long_enough = lds ? (blocks >= 128 ? blocks / 48 : 1) : (blocks >= 64 ? blocks / 16 : 1);
+    const int64_t splits = room < long_enough ? room : long_enough;
+    v.blocks_per_split = (int)ceil_div64(blocks, splits);
+    v.splits = (int)ceil_div64(blocks, v.blocks_per_split);
+    v.waves = v.blocks_per_split < 16 ? 4 : v.blocks_per_split < 96 || !lds ? 8 : 16;
+    if (v.row_tiles == 4) v.waves = 8;
+    v.ws_bytes = v.splits > 1 ? (size_t)v.splits * (size_t)m * (size_t)n * sizeof(float) : 0;
     return v;
 }
 
+template <bool BF, bool LUT, int GPB>
+static void launch_matvec_groups(const MatvecPlan& v, const MatvecParams& p, hipStream_t s) {
+    const dim3 grid((unsigned)ceil_div(p.w.ntiles, v.row_tiles), (unsigned)p.splits), block(64 * v.waves);
+    if (p.m <= kMatvecLdsRows) {
+        if (v.waves == 16) group_matvec_kernel<BF, LUT, GPB, 16, 1, true><<<grid, block, 0, s>>>(p);
+        else if (v.waves == 8) group_matvec_kernel<BF, LUT, GPB, 8, 1, true><<<grid, block, 0, s>>>(p);
+        else group_matvec_kernel<BF, LUT, GPB, 4, 1, true><<<grid, block, 0, s>>>(p);
+    } else if (v.row_tiles == 1) {
+        if (v.waves == 8) group_matvec_kernel<BF, LUT, GPB, 8, 1, false><<<grid, block, 0, s>>>(p);
+        else group_matvec_kernel<BF, LUT, GPB, 4, 1, false><<<grid, block, 0, s>>>(p);
+    } else if (v.row_tiles == 2) {
+        if (v.waves == 8) group_matvec_kernel<BF, LUT, GPB, 8, 2, false><<<grid, block, 0, s>>>(p);
+        else group_matvec_kernel<BF, LUT, GPB, 4, 2, false><<<grid, block, 0, s>>>(p);
+    } else {
+        group_matvec_kernel<BF, LUT, GPB, 8, 4, false><<<grid, block, 0, s>>>(p);
+    }
+}
 template <bool BF, bool LUT>
-static void launch_matvec_type(const MatvecParams& p, hipStream_t s) {
-    const dim3 grid((unsigned)p.w.ntiles, (unsigned)p.splits);
-    if (p.m <= kMatvecLdsRows) group_matvec_kernel<BF, LUT, 1, 8, 4, true><<<grid, 512, 0, s>>>(p);
-    else group_matvec_kernel<BF, LUT, 1, 8, 4, false><<<grid, 512, 0, s>>>(p);
+static void launch_matvec_type(const MatvecPlan& v, const MatvecParams& p, hipStream_t s) {
+    if (p.w.log_group == 7) launch_matvec_groups<BF, LUT, 1>(v, p, s);
+    else if (p.w.log_group == 6) launch_matvec_groups<BF, LUT, 2>(v, p, s);
+    else launch_matvec_groups<BF, LUT, 4>(v, p, s);
 }
 
 hipError_t launch_matvec(bool bf16, const MatvecPlan& plan, MatvecParams p, hipStream_t s) {
     p.splits = plan.splits;
     p.blocks_per_split = plan.blocks_per_split;
+    if (p.splits == 1) p.part = nullptr;
     // blocks of X in LDS at a time: m rows of 16 pieces a block, and 4 pieces between rows
     p.chunk = (kMatvecLdsBytes / 16 / p.m - 4) / 16;
     const bool lut = p.w.levels != nullptr;
-    if (bf16 && lut) launch_matvec_type<true, true>(p, s);
-    if (bf16 && !lut) launch_matvec_type<true, false>(p, s);
-    if (!bf16 && lut) launch_matvec_type<false, true>(p, s);
-    if (!bf16 && !lut) launch_matvec_type<false, false>(p, s);
-    return hipGetLastError();
+    if (bf16 && lut) launch_matvec_type<true, true>(plan, p, s);
+    if (bf16 && !lut) launch_matvec_type<true, false>(plan, p, s);
+    if (!bf16 && lut) launch_matvec_type<false, true>(plan, p, s);
+    if (!bf16 && !lut) launch_matvec_type<false, false>(plan, p, s);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits == 1) return e;
+    const JoinParams j = {p.part, p.splits, p.m, p.w.n, p.bias, p.Y, p.ldy, bf16 ? KQ_T_BF16 : KQ_T_F16};
+    return launch_join(j, s);
 }
 
 }  // namespace kq

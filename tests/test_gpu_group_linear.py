@@ -579,3 +579,71 @@ def test_refusals():
         kq.kq_quantize_groups(X.double())
     with pytest.raises(ValueError):
         kq.kq_group_linear_grad_input(dY[:, :19], L.packed, L.dscales, 100, group=32)
+
+
+LARGE = [("linear", 2048, 4096, 200, 128, False), ("linear", 2048, 2100, 300, 64, True), ("linear", 300, 4096, 1030, 32, False),
+         ("linear", 16, 4100, 12300, 128, False), ("linear", 9, 8192, 640, 64, True), ("linear", 5, 16400, 200, 32, False),
+         ("linear", 2, 1000, 25088, 128, False), ("grad_input", 3000, 130, 4097, 128, False), ("grad_input", 2000, 333, 2100, 32, True),
+         ("grad_input", 40, 4096, 1000, 64, False), ("weight", 130, 3500, 4104, 64, False), ("weight", 1000, 2049, 1026, 64, False),
+         ("scales", 130, 3500, 4104, 32, True), ("scales", 1111, 2100, 2056, 128, False), ("scales", 5000, 300, 520, 64, True)]
+
+
+@pytest.mark.parametrize("op,m,n,k,group,lut", LARGE)
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_sizes_that_take_other_tiles_and_splits(op, m, n, k, group, lut, dtype):
+    """Sizes at which the larger tiles, the row tiles of the matrix-vector kernel and the split contractions run
+    (the reference in 64 bits on the GPU)."""
+    L = Layer(n, k, group, table(k) if lut else None, seed=n + k)
+    W = L.W.to(DEV)
+
+    def close(y, y64, S, out, terms, rounded, integers, xsum=None, norm=True):
+        check(y, y64.cpu(), S.cpu(), out, terms, rounded, integers, xsum=None if xsum is None else xsum.cpu(), norm=norm)
+
+    if op == "linear":
+        X = acts(m, k, dtype, seed=m).to(DEV)
+        bias = torch.randn(n, generator=gen(n)).to(DEV)
+        Y = kq.kq_group_linear(X, L.packed, L.dscales, bias=bias, **L.kw())
+        x = X.double()
+        close(Y, x @ W.T.contiguous() + bias.double(), x.abs() @ W.abs().T.contiguous() + bias.double().abs(), dtype, k, m > 16, not lut,
+              xsum=x.abs().sum(1, keepdim=True))
+        return
+    dY = acts(m, n, dtype, seed=m + 1, scale=0.05).to(DEV)
+    d = dY.double()
+    if op == "grad_input":
+        dX = kq.kq_group_linear_grad_input(dY, L.packed, L.dscales, k, **L.kw())
+        close(dX, d @ W, d.abs() @ W.abs(), dtype, n, True, False, xsum=d.abs().sum(1, keepdim=True))
+        return
+    q, exps = kq.kq_checkpoint_pack(acts(m, k, dtype, seed=m + 2).to(DEV))
+    xh = kq.kq_checkpoint_restore(q, exps, k).double()
+    want, S = d.T.contiguous() @ xh, d.abs().T.contiguous() @ xh.abs()
+    if op == "weight":
+        dW, db = kq.kq_checkpoint_grad_weight(dY, q, exps, k, bias=True)
+        close(dW, want, S, F32, m, False, False)
+    else:
+        ds, db = kq.kq_checkpoint_grad_scales(dY, q, exps, L.packed, k, bias=True, **L.kw())
+        lv = values(L.levels).to(DEV)[L.codes.long().to(DEV)]
+        which = (torch.arange(k) // group).to(DEV)
+        zero = torch.zeros(n, L.scales.shape[1], dtype=torch.float64, device=DEV)
+        close(ds, zero.index_add(1, which, want * lv), zero.index_add(1, which, S * lv.abs()), F32, m + group, False, False, norm=False)
+    close(db, d.sum(0), d.abs().sum(0), F32, m, False, False, norm=False)
+
+
+def test_the_general_path_gives_the_same(monkeypatch):
+    """Calls through the checks in Python instead of the binding's C++ ones."""
+    L = Layer(200, 300, 64, table(5), seed=5)
+    X, dY = acts(40, 300, BF, seed=6).to(DEV), acts(40, 200, BF, seed=7).to(DEV)
+    W = torch.randn(200, 300, generator=gen(8)).to(DEV)
+
+    def step():
+        q, exps = kq.kq_checkpoint_pack(X)
+        return [*kq.kq_quantize_groups(W, 64, L.dlevels), kq.kq_reconstruct_groups(L.packed, L.dscales, 300, dtype=BF, **L.kw()), q, exps,
+                kq.kq_checkpoint_restore(q, exps, 300, dtype=BF), kq.kq_group_linear(X, L.packed, L.dscales, **L.kw()),
+                kq.kq_group_linear_grad_input(dY, L.packed, L.dscales, 300, **L.kw()),
+                *kq.kq_checkpoint_grad_scales(dY, q, exps, L.packed, 300, bias=True, **L.kw()),
+                *kq.kq_checkpoint_grad_weight(dY, q, exps, 300, bias=True)]
+
+    assert kq._fast is not None
+    want = step()
+    monkeypatch.setattr(kq, "_fast", None)
+    for a, b in zip(want, step()):
+        assert a.dtype == b.dtype and a.shape == b.shape and torch.equal(a, b)
