@@ -616,24 +616,25 @@ kq_status kq_fit_layer_noalloc(const float* X, int64_t n, int32_t dim, int32_t k
  *   are rounded to the type of X first.  An infinity in X makes its row of Y infinite or NaN, as do
  *   values of 2^122 and more.  A row of Y depends on its row of X and on m alone, not on other rows.
  * kq_group_linear_grad_input -- dX[m][k] = dY[m][n] W_hat, the weights rounded to the type of dY.
- *   workspaces: the *_workspace_bytes of the same m, n, k (may be 0: ws may be NULL then).
+ *   workspaces: the *_workspace_bytes of the same arguments (may be 0: ws may be NULL then).  Above 16 rows,
+ *   an X or dY that is not 16-byte aligned, or whose columns or pitch are not multiples of 8, is copied there.
  */
 #define KQ_T_F32 0
 #define KQ_T_BF16 1
 #define KQ_T_F16 2
 #define KQ_GROUP_MAX_FEATURES (1 << 24)
 #define KQ_GROUP_MAX_VALUES ((int64_t)1 << 34)
-#define KQ_GROUP_MAX_ROWS (1 << 30)
+#define KQ_GROUP_MAX_ROWS (1 << 22)
 size_t kq_group_code_bytes(int64_t n, int64_t k);
 kq_status kq_quantize_groups(const void* W, int32_t type, int64_t ldw, int64_t n, int64_t k, int32_t group,
                              const void* levels, uint8_t* codes, void* scales, void* stream);
 kq_status kq_reconstruct_groups(const uint8_t* codes, const void* scales, const void* levels, int64_t n, int64_t k,
                                 int32_t group, int32_t type, void* W_hat, int64_t ldw, void* stream);
-size_t kq_group_linear_workspace_bytes(int64_t m, int64_t n, int64_t k);
+size_t kq_group_linear_workspace_bytes(const void* X, int64_t ldx, int64_t m, int64_t n, int64_t k);
 kq_status kq_group_linear(const void* X, int32_t type, int64_t ldx, int64_t m, int64_t n, int64_t k,
                           const uint8_t* codes, const void* scales, const void* levels, int32_t group,
                           const float* bias, void* Y, int64_t ldy, void* ws, size_t ws_bytes, void* stream);
-size_t kq_group_linear_grad_input_workspace_bytes(int64_t m, int64_t n, int64_t k);
+size_t kq_group_linear_grad_input_workspace_bytes(const void* dY, int64_t ldy, int64_t m, int64_t n, int64_t k);
 kq_status kq_group_linear_grad_input(const void* dY, int32_t type, int64_t ldy, int64_t m, int64_t n, int64_t k,
                                      const uint8_t* codes, const void* scales, const void* levels, int32_t group,
                                      void* dX, int64_t ldx, void* ws, size_t ws_bytes, void* stream);
@@ -656,7 +657,8 @@ kq_status kq_group_linear_grad_input(const void* dY, int32_t type, int64_t ldy, 
  *   [n][ceil(k / group)]; dW is never written.
  *   dbias (fp32 [n], or NULL): sum_m dY[m][o].  dY bf16 or fp16; an fp16 dY needs a checkpoint
  *   whose values fp16 can hold.  Sums in fp32, in an order that the sizes alone decide.
- *   workspace: kq_checkpoint_grad_workspace_bytes(m, n, k, group), group 0 for the weight's.
+ *   workspace: kq_checkpoint_grad_workspace_bytes(m, n, k, group), group 0 for the weight's; it holds dY
+ *   transposed, and the partial sums of a split contraction.
  */
 #define KQ_CHECKPOINT_GROUP 32
 kq_status kq_checkpoint_pack(const void* X, int32_t type, int64_t ldx, int64_t m, int64_t k, int8_t* q, uint8_t* exps,

@@ -111,9 +111,9 @@ def _load():
         "kq_group_code_bytes": ([_I64, _I64], _SZ),
         "kq_quantize_groups": ([_P, _I32, _I64, _I64, _I64, _I32, _P, _P, _P, _P], _I32),
         "kq_reconstruct_groups": ([_P, _P, _P, _I64, _I64, _I32, _I32, _P, _I64, _P], _I32),
-        "kq_group_linear_workspace_bytes": ([_I64, _I64, _I64], _SZ),
+        "kq_group_linear_workspace_bytes": ([_P, _I64, _I64, _I64, _I64], _SZ),
         "kq_group_linear": ([_P, _I32, _I64, _I64, _I64, _I64, _P, _P, _P, _I32, _P, _P, _I64, _P, _SZ, _P], _I32),
-        "kq_group_linear_grad_input_workspace_bytes": ([_I64, _I64, _I64], _SZ),
+        "kq_group_linear_grad_input_workspace_bytes": ([_P, _I64, _I64, _I64, _I64], _SZ),
         "kq_group_linear_grad_input": ([_P, _I32, _I64, _I64, _I64, _I64, _P, _P, _P, _I32, _P, _I64, _P, _SZ, _P],
                                        _I32),
         "kq_checkpoint_pack": ([_P, _I32, _I64, _I64, _I64, _P, _P, _P], _I32),
@@ -1058,7 +1058,7 @@ def kq_group_linear(X, codes, scales, group: int = 128, levels=None, bias=None, 
         _dev(bias, torch.float32, "bias", (n,))
     _same_device(dev, codes=codes, bias=bias)
     Y, y, ldy = _out_rows(Y, X, X.shape[:-1], n, _ACTS, "Y")
-    wp, wn = _scratch_for(dev, lib.kq_group_linear_workspace_bytes(m, n, k), workspace)
+    wp, wn = _scratch_for(dev, lib.kq_group_linear_workspace_bytes(x.data_ptr(), ldx, m, n, k), workspace)
     _check(lib.kq_group_linear(x.data_ptr(), ty, ldx, m, n, k, codes.data_ptr(), scales.data_ptr(), _ptr(levels), group,
                                _ptr(bias), y.data_ptr(), ldy, wp, wn, _stream(dev)), "kq_group_linear")
     return Y
@@ -1078,7 +1078,7 @@ def kq_group_linear_grad_input(dY, codes, scales, in_features: int, group: int =
         raise ValueError(f"dY must have {n} columns, got {dy.shape[1]}")
     _same_device(dev, codes=codes)
     dX, dx, ldx = _out_rows(dX, dY, dY.shape[:-1], k, _ACTS, "dX")
-    wp, wn = _scratch_for(dev, lib.kq_group_linear_grad_input_workspace_bytes(m, n, k), workspace)
+    wp, wn = _scratch_for(dev, lib.kq_group_linear_grad_input_workspace_bytes(dy.data_ptr(), ldy, m, n, k), workspace)
     _check(lib.kq_group_linear_grad_input(dy.data_ptr(), ty, ldy, m, n, k, codes.data_ptr(), scales.data_ptr(),
                                           _ptr(levels), group, dx.data_ptr(), ldx, wp, wn, _stream(dev)),
            "kq_group_linear_grad_input")

@@ -141,16 +141,6 @@ struct CheckpointParams {
 hipError_t launch_checkpoint_pack(const CheckpointParams& p, hipStream_t s);
 hipError_t launch_checkpoint_restore(const CheckpointParams& p, hipStream_t s);
 
-struct BiasGradParams {
-    const void* dY;
-    int64_t ldy;
-    int type;
-    int64_t m;
-    int n;
-    float* dbias;
-};
-hipError_t launch_bias_grad(const BiasGradParams& p, hipStream_t s);
-
 // The products.  `i` is the contiguous dimension of the output, `j` its rows, `c` the contraction:
 //   linear      Y[m][n]  = sum_k X[m][k] W[n][k]     i = n, j = m, c = k
 //   grad input  dX[m][k] = sum_n dY[m][n] W[n][k]    i = k, j = m, c = n
@@ -159,7 +149,7 @@ enum class Product { Linear = 0, GradInput = 1, GradWeight = 2, GradScales = 3 }
 
 struct GemmParams {
     GroupWeights w;          // Linear, GradInput, GradScales (codes and levels only)
-    const void* B;           // X (Linear) or dY
+    const void* B;           // X (Linear) or dY; in the kernel [J][C] in aligned rows
     int64_t ldb;
     const int8_t* q;         // the checkpoint: GradWeight, GradScales
     const uint8_t* exps;
@@ -168,6 +158,9 @@ struct GemmParams {
     const float* bias;
     void* out;               // 16-bit (Linear, GradInput) or fp32
     int64_t ldo;
+    float* dbias;            // column sums of dY, or NULL: from bias_parts partial ones [bias_parts][J]
+    float* bias_part;
+    int bias_parts;
     float* part;             // partial sums of a split contraction, or NULL
     int splits;
     int steps_per_split;     // 64-deep steps of the contraction a workgroup takes
@@ -176,10 +169,23 @@ struct GemmParams {
 struct GemmPlan {
     int bi, bj;              // output tile
     int splits, steps_per_split;
-    size_t ws_bytes;
+    bool stage_b;            // B is transposed or copied into the workspace, rows of `pitch` values
+    int64_t pitch;
+    int bias_parts;
+    size_t part_bytes, b_bytes, ws_bytes;  // workspace: partial sums, B, partial column sums
 };
-GemmPlan gemm_plan(Product mode, int64_t I, int64_t J, int64_t C, int groups);
-hipError_t launch_gemm(Product mode, bool bf16, const GemmPlan& plan, GemmParams p, hipStream_t s);
+// B and ldb: X or dY as the call gets it (only its alignment counts; the gradients from a checkpoint take any)
+GemmPlan gemm_plan(Product mode, const void* B, int64_t ldb, int64_t I, int64_t J, int64_t C, int groups);
+hipError_t launch_gemm(Product mode, bool bf16, const GemmPlan& plan, GemmParams p, void* ws, hipStream_t s);
+
+struct StageBParams {
+    const void* in;
+    int64_t ld;
+    int64_t J, C;
+    void* out;
+    int64_t pitch;
+    float* bias_part;
+};
 
 // out[r][c] = sum over the splits of part[split][r][c], in order, + bias[c]
 struct JoinParams {

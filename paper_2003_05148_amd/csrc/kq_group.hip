@@ -1,5 +1,5 @@
-// The 4-bit group quantizer, the weights it stands for, 8-bit activation checkpoints and the bias
-// gradient: passes over memory.
+// The 4-bit group quantizer, the weights it stands for, 8-bit activation checkpoints and the sums of
+// split products: passes over memory.
 #include "kq_group.h"
 
 namespace kq {
@@ -272,69 +272,17 @@ __global__ __launch_bounds__(256) void checkpoint_restore_kernel(const Checkpoin
     else if (p.type == KQ_T_BF16) KERNEL<KQ_T_BF16><<<grid, block, 0, s>>>(p); \
     else KERNEL<KQ_T_F16><<<grid, block, 0, s>>>(p);
 
-// A launch has fewer than 2^32 threads: rows in pieces of at most 2^30 threads.
-template <bool PACK>
-static hipError_t launch_checkpoint(CheckpointParams p, hipStream_t s) {
-    const int per_row = p.kq >> 3;
-    const int64_t piece = (int64_t(1) << 30) / per_row, rows = p.m;
-    for (int64_t r = 0; r < rows; r += piece) {
-        p.m = rows - r < piece ? rows - r : piece;
-        const dim3 grid((unsigned)ceil_div64(p.m * per_row, 256)), block(256);
-        if constexpr (PACK) {
-            KQ_BY_TYPE(checkpoint_pack_kernel)
-        } else {
-            KQ_BY_TYPE(checkpoint_restore_kernel)
-        }
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        p.X = (char*)p.X + piece * p.ldx * (p.type == KQ_T_F32 ? 4 : 2);
-        p.q += piece * p.kq;
-        p.exps += piece * (p.kq / kCkGroup);
-    }
-    return hipSuccess;
-}
-#undef KQ_BY_TYPE
-
-hipError_t launch_checkpoint_pack(const CheckpointParams& p, hipStream_t s) { return launch_checkpoint<true>(p, s); }
-hipError_t launch_checkpoint_restore(const CheckpointParams& p, hipStream_t s) { return launch_checkpoint<false>(p, s); }
-
-// ---- bias gradient: dbias[n] = sum_m dY[m][n] ------------------------------------------------------------------
-// A workgroup of 512 threads adds 32 columns: four lanes of 8 columns a row, 128 rows at a time; 16 lanes'
-// sums are added by a butterfly, then the eight waves' in order.
-template <bool BF>
-__global__ __launch_bounds__(512) void bias_grad_kernel(const BiasGradParams p) {
-    __shared__ float s_part[8][32];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int c0 = blockIdx.x * 32 + 8 * (lane & 3);
-    float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll 4
-    for (int64_t r = threadIdx.x >> 2; r < p.m; r += 128) {
-        float v[8];
-        load_columns<BF ? KQ_T_BF16 : KQ_T_F16>(p.dY, r * p.ldy, c0, p.n, v);
-#pragma unroll
-        for (int t = 0; t < 8; ++t) acc[t] += v[t];
-    }
-#pragma unroll
-    for (int t = 0; t < 8; ++t) {
-#pragma unroll
-        for (int off = 4; off < 64; off <<= 1) acc[t] += __shfl_xor(acc[t], off);
-        if (lane < 4) s_part[wave][8 * lane + t] = acc[t];
-    }
-    __syncthreads();
-    const int c = blockIdx.x * 32 + threadIdx.x;
-    if (threadIdx.x < 32 && c < p.n) {
-        float v = s_part[0][threadIdx.x];
-        for (int w = 1; w < 8; ++w) v += s_part[w][threadIdx.x];
-        p.dbias[c] = v;
-    }
-}
-
-hipError_t launch_bias_grad(const BiasGradParams& p, hipStream_t s) {
-    const dim3 grid((unsigned)ceil_div(p.n, 32)), block(512);
-    if (p.type == KQ_T_BF16) bias_grad_kernel<true><<<grid, block, 0, s>>>(p);
-    else bias_grad_kernel<false><<<grid, block, 0, s>>>(p);
+hipError_t launch_checkpoint_pack(const CheckpointParams& p, hipStream_t s) {
+    const dim3 grid((unsigned)ceil_div64(p.m * (p.kq >> 3), 256)), block(256);
+    KQ_BY_TYPE(checkpoint_pack_kernel)
     return hipGetLastError();
 }
+hipError_t launch_checkpoint_restore(const CheckpointParams& p, hipStream_t s) {
+    const dim3 grid((unsigned)ceil_div64(p.m * (p.kq >> 3), 256)), block(256);
+    KQ_BY_TYPE(checkpoint_restore_kernel)
+    return hipGetLastError();
+}
+#undef KQ_BY_TYPE
 
 // ---- partial sums of a split contraction -------------------------------------------------------------------------
 template <int TYPE>

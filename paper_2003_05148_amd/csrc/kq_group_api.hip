@@ -95,9 +95,9 @@ kq_status kq_reconstruct_groups(const uint8_t* codes, const void* scales, const 
     return hip_status(launch_reconstruct_groups(p, (hipStream_t)stream));
 }
 
-size_t kq_group_linear_workspace_bytes(int64_t m, int64_t n, int64_t k) {
+size_t kq_group_linear_workspace_bytes(const void* X, int64_t ldx, int64_t m, int64_t n, int64_t k) {
     if (m < 1 || check_size(n, k) != KQ_OK || check_rows(m, n, k) != KQ_OK) return 0;
-    return m <= kMatvecRows ? matvec_plan((int)m, n, k).ws_bytes : gemm_plan(Product::Linear, n, m, k, 0).ws_bytes;
+    return m <= kMatvecRows ? matvec_plan((int)m, n, k).ws_bytes : gemm_plan(Product::Linear, X, ldx, n, m, k, 0).ws_bytes;
 }
 
 kq_status kq_group_linear(const void* X, int32_t type, int64_t ldx, int64_t m, int64_t n, int64_t k,
@@ -125,7 +125,7 @@ kq_status kq_group_linear(const void* X, int32_t type, int64_t ldx, int64_t m, i
         v.part = plan.ws_bytes ? (float*)ws : nullptr;
         return hip_status(launch_matvec(type == KQ_T_BF16, plan, v, (hipStream_t)stream));
     }
-    const GemmPlan plan = gemm_plan(Product::Linear, n, m, k, 0);
+    const GemmPlan plan = gemm_plan(Product::Linear, X, ldx, n, m, k, 0);
     if ((st = check_ws(ws, ws_bytes, plan.ws_bytes)) != KQ_OK) return st;
     p.B = X;
     p.ldb = ldx;
@@ -135,13 +135,12 @@ kq_status kq_group_linear(const void* X, int32_t type, int64_t ldx, int64_t m, i
     p.bias = bias;
     p.out = Y;
     p.ldo = ldy;
-    p.part = plan.ws_bytes ? (float*)ws : nullptr;
-    return hip_status(launch_gemm(Product::Linear, type == KQ_T_BF16, plan, p, (hipStream_t)stream));
+    return hip_status(launch_gemm(Product::Linear, type == KQ_T_BF16, plan, p, ws, (hipStream_t)stream));
 }
 
-size_t kq_group_linear_grad_input_workspace_bytes(int64_t m, int64_t n, int64_t k) {
+size_t kq_group_linear_grad_input_workspace_bytes(const void* dY, int64_t ldy, int64_t m, int64_t n, int64_t k) {
     if (m < 1 || check_size(n, k) != KQ_OK || check_rows(m, n, k) != KQ_OK) return 0;
-    return gemm_plan(Product::GradInput, k, m, n, 0).ws_bytes;
+    return gemm_plan(Product::GradInput, dY, ldy, k, m, n, 0).ws_bytes;
 }
 
 kq_status kq_group_linear_grad_input(const void* dY, int32_t type, int64_t ldy, int64_t m, int64_t n, int64_t k,
@@ -154,7 +153,7 @@ kq_status kq_group_linear_grad_input(const void* dY, int32_t type, int64_t ldy, 
     if ((st = check_rows(m, n, k)) != KQ_OK) return st;
     if (m == 0) return KQ_OK;
     if (!valid_tensor(dY, type, ldy, n) || !valid_tensor(dX, type, ldx, k)) return KQ_ERR_ARG;
-    const GemmPlan plan = gemm_plan(Product::GradInput, k, m, n, 0);
+    const GemmPlan plan = gemm_plan(Product::GradInput, dY, ldy, k, m, n, 0);
     if ((st = check_ws(ws, ws_bytes, plan.ws_bytes)) != KQ_OK) return st;
     p.B = dY;
     p.ldb = ldy;
@@ -163,8 +162,7 @@ kq_status kq_group_linear_grad_input(const void* dY, int32_t type, int64_t ldy, 
     p.C = n;
     p.out = dX;
     p.ldo = ldx;
-    p.part = plan.ws_bytes ? (float*)ws : nullptr;
-    return hip_status(launch_gemm(Product::GradInput, type == KQ_T_BF16, plan, p, (hipStream_t)stream));
+    return hip_status(launch_gemm(Product::GradInput, type == KQ_T_BF16, plan, p, ws, (hipStream_t)stream));
 }
 
 kq_status kq_checkpoint_pack(const void* X, int32_t type, int64_t ldx, int64_t m, int64_t k, int8_t* q, uint8_t* exps,
@@ -190,8 +188,8 @@ kq_status kq_checkpoint_restore(const int8_t* q, const uint8_t* exps, int64_t m,
 
 size_t kq_checkpoint_grad_workspace_bytes(int64_t m, int64_t n, int64_t k, int32_t group) {
     if (check_size(n, k) != KQ_OK || check_rows(m, n, k) != KQ_OK || (group != 0 && log2_group(group) < 0)) return 0;
-    if (group == 0) return gemm_plan(Product::GradWeight, k, n, m, 0).ws_bytes;
-    return gemm_plan(Product::GradScales, k, n, m, (int)ceil_div64(k, group)).ws_bytes;
+    if (group == 0) return gemm_plan(Product::GradWeight, nullptr, 0, k, n, m, 0).ws_bytes;
+    return gemm_plan(Product::GradScales, nullptr, 0, k, n, m, (int)ceil_div64(k, group)).ws_bytes;
 }
 
 namespace {
@@ -204,7 +202,7 @@ kq_status checkpoint_grad(Product mode, GemmParams& p, const void* dY, int32_t t
     if (!out || !aligned(out, 4) || ldo < 1 || ldo > (int64_t(1) << 40) || !aligned(dbias, 4)) return KQ_ERR_ARG;
     // without rows there is nothing to read, and the gradients are zero
     if (m > 0 && (!valid_tensor(dY, type, ldy, n) || !q || !aligned(q, 16) || !exps)) return KQ_ERR_ARG;
-    const GemmPlan plan = gemm_plan(mode, k, n, m, p.w.groups);
+    const GemmPlan plan = gemm_plan(mode, nullptr, 0, k, n, m, p.w.groups);
     if ((st = check_ws(ws, ws_bytes, plan.ws_bytes)) != KQ_OK) return st;
     p.B = dY;
     p.ldb = ldy;
@@ -216,13 +214,8 @@ kq_status checkpoint_grad(Product mode, GemmParams& p, const void* dY, int32_t t
     p.C = m;
     p.out = out;
     p.ldo = ldo;
-    p.part = plan.ws_bytes ? (float*)ws : nullptr;
-    hipError_t e = launch_gemm(mode, type == KQ_T_BF16, plan, p, stream);
-    if (e == hipSuccess && dbias) {
-        const BiasGradParams b = {dY, ldy, type, m, (int)n, dbias};
-        e = launch_bias_grad(b, stream);
-    }
-    return hip_status(e);
+    p.dbias = dbias;
+    return hip_status(launch_gemm(mode, type == KQ_T_BF16, plan, p, ws, stream));
 }
 }  // namespace
 

@@ -2,15 +2,22 @@
 //
 // Every product is out[j][i] = sum_c A[i][c] B[j][c] with i the contiguous dimension of the output, so
 // that a lane's four accumulators are neighbours in memory.  A workgroup holds a BI x BJ tile of the output
-// in registers and walks the contraction in steps of 64; a step's operands are staged through LDS as
-// 16-bit rows of 64 (128 bytes).  What differs between the products is how a step gets there:
-//   Linear      A = W from its codes (a row's eight columns are one dword), B = X as it is
+// in registers and walks the contraction in steps of 64; a step's operands lie in LDS as 16-bit rows of 64
+// (128 bytes), two steps' worth of them.
+//   Linear      A = W from its codes (a row's eight columns are one dword), B = X
 //   GradInput   A = W^T: eight rows' dwords of one thread are an 8 x 8 block, written transposed; B = dY
-//   GradWeight  A = X^^T from the checkpoint (8 rows x 4 columns a thread), B = dY^T (8 x 4 a thread)
+//   GradWeight  A = X^^T from the checkpoint (8 rows x 4 columns a thread), B = dY^T
 //   GradScales  the same product; the epilogue multiplies it by the levels and adds up each group
+// A goes through registers, where it becomes 16-bit values; B goes from memory to LDS directly, so it has to
+// lie in 16-byte aligned rows along c: dY is transposed into the workspace first (its column sums, the bias
+// gradient, are taken on the way), and an X or dY whose rows are not aligned is copied there.
 // Weights are s * level rounded once to the activation's type (bf16: s has 8 bits and -8..7 three, so
 // about half of them are exact); checkpoints and activations are exact, sums are fp32.
 #include "kq_group.h"
+
+#ifdef KQ_PROBE
+#include <stdlib.h>
+#endif
 
 namespace kq {
 
@@ -22,6 +29,12 @@ constexpr int kStep = 64;  // contraction per step
 __device__ __forceinline__ int swizzle(int r) { return (r ^ (r >> 2)) & 7; }
 __device__ __forceinline__ int lds_chunk(int r, int ch) { return r * 8 + (ch ^ swizzle(r)); }
 
+// A 16-byte store to LDS.  The compiler cannot always tell an ordinary one from the target of a direct load in
+// flight, and then waits for every load first; the step's end waits for both.
+__device__ __forceinline__ void write_lds(u32x4* at, u32x4 v) {
+    asm volatile("ds_write_b128 %0, %1" ::"v"((unsigned)(uintptr_t)(__attribute__((address_space(3))) u32x4*)at), "v"(v) : "memory");
+}
+
 // The bytes of four codes, 0..15 each, as fp32 s * level.
 template <bool LUT>
 struct Levels;
@@ -30,6 +43,7 @@ struct Levels<false> {
     __device__ __forceinline__ void init(const uint16_t*) {}
     // levels -8 .. 7: s * (q - 8) = fma(q, s, -8 s), exact
     static __device__ __forceinline__ void scaled(const Levels&, unsigned b, const float (&s)[4], float (&v)[4]) {
+        asm("" : "+v"(b));  // (unknown bytes: a byte conversion each, with no extraction before it)
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = __builtin_fmaf((float)((b >> (8 * j)) & 255u), s[j], -8.0f * s[j]);
     }
@@ -59,7 +73,7 @@ struct Levels<true> {
 };
 
 template <bool BF, bool LUT, int MODE, int BI, int BJ, int WI, int WJ>
-struct Gemm {
+struct StageA {
     static constexpr int NT = 64 * WI * WJ;
     static constexpr int MI = BI / WI / 16, MJ = BJ / WJ / 16;  // 16 x 16 tiles of a wave
     static constexpr bool kWeightRows = MODE == (int)Product::Linear;
@@ -68,18 +82,38 @@ struct Gemm {
     using A_ = Act<BF>;
     using L = Levels<LUT>;
 
-    // Pieces of a step that a thread stages: A and B tasks.  Rows past the output's edges repeat the last
-    // one (what they give is not stored); the contraction's edge is zero on both sides.
+    // A thread's pieces of a step.  Rows past the output's edge repeat the last one (what they give is not
+    // stored); past the contraction's edge B is zero, and so are A's scales.
     static constexpr int kATasks = kWeightRows ? BI * 4 : BI * 2;
     static constexpr int PA = kATasks / NT;
     static_assert(kATasks % NT == 0 && PA >= 1, "A tasks");
-    static constexpr int kBTasks = kCheckpoint ? BJ * 2 : BJ * 8;
-    static constexpr int PB = kBTasks / NT;
-    static_assert(kBTasks % NT == 0 && PB >= 1, "B tasks");
+    unsigned w[PA][kWeightRows ? 2 : 8];
+    unsigned short x[PA][kWeightRows ? 2 : 8];  // scales (bf16 bits) or checkpoint exponents
 
-    unsigned aw[PA][kWeightRows ? 2 : 8];
-    unsigned short as[PA][kWeightRows ? 2 : 8];  // scales (bf16 bits) or checkpoint exponents
-    unsigned bv[PB][kCheckpoint ? 16 : 4];
+    // Cache lines of a step's A: where line `id` of step 0 lies, and how far on it is a step later.
+    static constexpr int kLines = kWeightRows ? BI / 4 : kWeightCols ? BI / 4 + 64 : BI / 2 + 64;
+    static __device__ __forceinline__ const uint8_t* line(const GemmParams& p, int i0, int id, unsigned& stride) {
+        if constexpr (kWeightRows) {  // four lines a tile of codes and step (scales: a line holds many steps' worth)
+            const int nt = min((i0 >> 4) + (id >> 2), p.w.ntiles - 1);
+            stride = kTileBytes / 2;
+            return p.w.codes + (int64_t)nt * p.w.ktiles * kTileBytes + (id & 3) * 128;
+        } else if constexpr (kWeightCols) {
+            if (id < BI / 4) {  // 4 tiles of rows, BI / 128 of columns, eight lines each
+                const int kt = min((i0 >> 7) + (id >> 3) % (BI / 128), p.w.ktiles - 1);
+                stride = 4u * p.w.ktiles * kTileBytes;
+                return p.w.codes + ((int64_t)(id / (BI / 16)) * p.w.ktiles + kt) * kTileBytes + (id & 7) * 128;
+            }
+            stride = 2u * kStep * p.w.groups;
+            return (const uint8_t*)(p.w.scales + (int64_t)(id - BI / 4) * p.w.groups + (i0 >> p.w.log_group));
+        } else {
+            if (id < BI / 2) {
+                stride = (unsigned)kStep * p.kq;
+                return (const uint8_t*)p.q + (int64_t)(id / (BI / 128)) * p.kq + min(i0 + id % (BI / 128) * 128, p.kq - 1);
+            }
+            stride = (unsigned)kStep * (p.kq >> 5);
+            return p.exps + (int64_t)(id - BI / 2) * (p.kq >> 5) + (i0 >> 5);
+        }
+    }
 
     // Which rows of the contraction a thread's transposed tasks take: octet t * kOctets + ...; with 256
     // rows of output a wave has one octet, and its row addresses are scalar.
@@ -93,7 +127,7 @@ struct Gemm {
         return *(const T*)((const char*)base + off);
     }
 
-    __device__ __forceinline__ void load_a(const GemmParams& p, int i0, int c, int tid, int wave) {
+    __device__ __forceinline__ void load(const GemmParams& p, int i0, int c, int tid, int wave) {
         const bool full = c + kStep <= p.C;
 #pragma unroll
         for (int t = 0; t < PA; ++t) {
@@ -102,13 +136,13 @@ struct Gemm {
                 const int r = min(id >> 2, p.w.n - 1 - i0), q = id & 3;
                 const uint8_t* base = p.w.codes + ((int64_t)(i0 >> 4) * p.w.ktiles + (c >> 7)) * kTileBytes + ((c & 64) >> 3);
                 const u32x2 d = at<u32x2>(base, (unsigned)(r >> 4) * (unsigned)p.w.ktiles * kTileBytes + (r & 15) * 64 + q * 16);
-                aw[t][0] = d.x;
-                aw[t][1] = d.y;
+                w[t][0] = d.x;
+                w[t][1] = d.y;
                 const uint16_t* sc = p.w.scales + (int64_t)i0 * p.w.groups;
                 const unsigned row = (unsigned)r * (unsigned)p.w.groups;
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
-                    as[t][h] = at<unsigned short>(sc + min((c + 32 * h) >> p.w.log_group, p.w.groups - 1), 2 * row);
+                    x[t][h] = at<unsigned short>(sc + min((c + 32 * h) >> p.w.log_group, p.w.groups - 1), 2 * row);
             } else if constexpr (kWeightCols) {  // 8 rows, one dword: the even or the odd half of 8 columns
                 const int oct = octet<BI>(t, tid, wave), d = (id >> 1) % (BI / 8);
                 const int k = min(i0 + 8 * d, p.w.k - 1), n = c + 8 * oct;
@@ -117,9 +151,8 @@ struct Gemm {
                 const unsigned col = (unsigned)(k >> 7) * kTileBytes + dw * 4, g = 2 * (unsigned)(k >> p.w.log_group);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    aw[t][e] = at<unsigned>(base + e * 64, col);
-                    as[t][e] = at<unsigned short>(p.w.scales + (int64_t)min(n + e, p.w.n - 1) * p.w.groups, g);
-                    if (!full && n + e >= p.w.n) as[t][e] = 0;
+                    w[t][e] = at<unsigned>(base + e * 64, col);
+                    x[t][e] = at<unsigned short>(p.w.scales + (int64_t)min(n + e, p.w.n - 1) * p.w.groups, g);
                 }
             } else {  // 8 rows of the checkpoint, 4 columns
                 const int oct = octet<BI>(t, tid, wave), quad = id % (BI / 4);
@@ -128,28 +161,35 @@ struct Gemm {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int64_t row = full ? m + e : min(m + e, (int)p.C - 1);
-                    aw[t][e] = at<unsigned>(p.q + row * p.kq, k);
-                    as[t][e] = at<uint8_t>(p.exps + row * (p.kq >> 5), k >> 5);
-                    if (!full && m + e >= p.C) as[t][e] = 0;
+                    w[t][e] = at<unsigned>(p.q + row * p.kq, k);
+                    x[t][e] = at<uint8_t>(p.exps + row * (p.kq >> 5), k >> 5);
                 }
             }
         }
     }
 
-    __device__ __forceinline__ void store_a(u32x4* lds, int tid, int wave, const L& lv) const {
+    // c: the step's place in the contraction of C.  (What lies past its end was loaded from the last row; it
+    // is taken off here, where the loads have arrived.)
+    __device__ __forceinline__ void store(u32x4* lds, int64_t C, int c, int tid, int wave, const L& lv) const {
+        if (kWeightRows || c + kStep <= C) store_step<false>(lds, C, c, tid, wave, lv);
+        else store_step<true>(lds, C, c, tid, wave, lv);
+    }
+    template <bool EDGE>
+    __device__ __forceinline__ void store_step(u32x4* lds, int64_t C, int c, int tid, int wave, const L& lv) const {
 #pragma unroll
         for (int t = 0; t < PA; ++t) {
             const int id = t * NT + tid;
+            const int left = !EDGE ? 8 : (int)min(C - c - 8 * octet<BI>(t, tid, wave), (int64_t)8);  // rows of the octet
             if constexpr (kWeightRows) {
                 const int r = id >> 2, q = id & 3;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const float s1 = bf16_bits_to_f32(as[t][h]);
+                    const float s1 = bf16_bits_to_f32(x[t][h]);
                     const float s[4] = {s1, s1, s1, s1};
                     float e[4], o[4];  // nibbles 0 2 4 6 are columns 0 4 1 5, nibbles 1 3 5 7 columns 2 6 3 7
-                    L::scaled(lv, aw[t][h] & 0x0f0f0f0fu, s, e);
-                    L::scaled(lv, (aw[t][h] >> 4) & 0x0f0f0f0fu, s, o);
-                    lds[lds_chunk(r, 4 * h + q)] = u32x4{A_::pack(e[0], e[2]), A_::pack(o[0], o[2]), A_::pack(e[1], e[3]), A_::pack(o[1], o[3])};
+                    L::scaled(lv, w[t][h] & 0x0f0f0f0fu, s, e);
+                    L::scaled(lv, (w[t][h] >> 4) & 0x0f0f0f0fu, s, o);
+                    write_lds(lds + lds_chunk(r, 4 * h + q), u32x4{A_::pack(e[0], e[2]), A_::pack(o[0], o[2]), A_::pack(e[1], e[3]), A_::pack(o[1], o[3])});
                 }
             } else if constexpr (kWeightCols) {
                 const int par = id & 1, d = (id >> 1) % (BI / 8), oct = octet<BI>(t, tid, wave);
@@ -157,19 +197,19 @@ struct Gemm {
                 u32x4 out[4];  // column 8 d + 2 j + par, 8 rows each
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {  // rows 2 e and 2 e + 1
-                    const unsigned w = __builtin_amdgcn_perm(aw[t][2 * e + 1], aw[t][2 * e], half);
-                    const float s0 = bf16_bits_to_f32(as[t][2 * e]), s1 = bf16_bits_to_f32(as[t][2 * e + 1]);
+                    const unsigned pairw = __builtin_amdgcn_perm(w[t][2 * e + 1], w[t][2 * e], half);
+                    const float s0 = bf16_bits_to_f32(2 * e < left ? x[t][2 * e] : 0), s1 = bf16_bits_to_f32(2 * e + 1 < left ? x[t][2 * e + 1] : 0);
                     const float s[4] = {s0, s0, s1, s1};
-                    float x[4], y[4];  // columns 0, 2 of both rows; columns 1, 3
-                    L::scaled(lv, w & 0x0f0f0f0fu, s, x);
-                    L::scaled(lv, (w >> 4) & 0x0f0f0f0fu, s, y);
-                    out[0][e] = A_::pack(x[0], x[2]);
-                    out[1][e] = A_::pack(y[0], y[2]);
-                    out[2][e] = A_::pack(x[1], x[3]);
-                    out[3][e] = A_::pack(y[1], y[3]);
+                    float ev[4], od[4];  // columns 0, 2 of both rows; columns 1, 3
+                    L::scaled(lv, pairw & 0x0f0f0f0fu, s, ev);
+                    L::scaled(lv, (pairw >> 4) & 0x0f0f0f0fu, s, od);
+                    out[0][e] = A_::pack(ev[0], ev[2]);
+                    out[1][e] = A_::pack(od[0], od[2]);
+                    out[2][e] = A_::pack(ev[1], ev[3]);
+                    out[3][e] = A_::pack(od[1], od[3]);
                 }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) lds[lds_chunk(8 * d + 2 * j + par, oct)] = out[j];
+                for (int j = 0; j < 4; ++j) write_lds(lds + lds_chunk(8 * d + 2 * j + par, oct), out[j]);
             } else {
                 const int quad = id % (BI / 4), oct = octet<BI>(t, tid, wave);
                 u32x4 out[4];
@@ -178,9 +218,9 @@ struct Gemm {
                     float v[2][4];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const unsigned x = as[t][2 * e + h];
-                        const float s = __builtin_bit_cast(float, x == 255u ? 0x7fc00000u : x << 23);
-                        const unsigned u = aw[t][2 * e + h] ^ 0x80808080u;  // q + 128
+                        const unsigned ex = 2 * e + h < left ? x[t][2 * e + h] : 0;
+                        const float s = __builtin_bit_cast(float, ex == 255u ? 0x7fc00000u : ex << 23);
+                        const unsigned u = w[t][2 * e + h] ^ 0x80808080u;  // q + 128
 #pragma unroll
                         for (int j = 0; j < 4; ++j) v[h][j] = __builtin_fmaf((float)((u >> (8 * j)) & 255u), s, -128.0f * s);
                     }
@@ -188,78 +228,39 @@ struct Gemm {
                     for (int j = 0; j < 4; ++j) out[j][e] = A_::pack_exact(v[0][j], v[1][j]);
                 }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) lds[lds_chunk(4 * quad + j, oct)] = out[j];
+                for (int j = 0; j < 4; ++j) write_lds(lds + lds_chunk(4 * quad + j, oct), out[j]);
             }
         }
     }
+};
 
-    __device__ __forceinline__ void load_b(const GemmParams& p, int64_t j0, int c, int tid, int wave) {
-        const bool full = c + kStep <= p.C;
+// A step of B from memory to LDS: a wave's instruction takes 64 chunks of 16 bytes, eight rows; lane l writes
+// chunk l of them, so it reads the chunk that belongs there.
+using lds_ptr = __attribute__((address_space(3))) void*;
+using global_ptr = const __attribute__((address_space(1))) void*;
+template <int BJ, int WAVES>
+struct DirectB {
+    static constexpr int N = BJ / 8 / WAVES;
+    static_assert(N >= 1 && BJ % (8 * WAVES) == 0, "B pieces");
+    unsigned off[N];  // bytes from the tile's first row
+    int col;          // the lane's first column
+    __device__ __forceinline__ void init(const GemmParams& p, int64_t j0, int lane, int wave) {
+        const int last = (int)min(p.J - 1 - j0, (int64_t)BJ - 1);
 #pragma unroll
-        for (int t = 0; t < PB; ++t) {
-            const int id = t * NT + tid;
-            if constexpr (!kCheckpoint) {  // rows j, 8 neighbours along c
-                const int r = id >> 3, ch = id & 7, c0 = c + 8 * ch;
-                const uint16_t* row = (const uint16_t*)p.B + c + (min(j0 + r, p.J - 1) * p.ldb + 8 * ch);
-                if (full) {
-                    __builtin_memcpy(bv[t], row, 16);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const unsigned lo = c0 + 2 * e < p.C ? row[2 * e] : 0u;
-                        const unsigned hi = c0 + 2 * e + 1 < p.C ? row[2 * e + 1] : 0u;
-                        bv[t][e] = lo | (hi << 16);
-                    }
-                }
-            } else {  // 8 rows along c, four neighbours along j
-                const int oct = octet<BJ>(t, tid, wave), quad = id % (BJ / 4), m = c + 8 * oct;
-                const int n = (int)j0 + 4 * quad, J = (int)p.J;
-                if (J >= 4) {  // four that lie inside, moved down to column n
-                    const int n1 = min(n, J - 4), shift = 16 * min(n - n1, 3);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int64_t row = full ? m + e : min(m + e, (int)p.C - 1);
-                        uint64_t v;
-                        __builtin_memcpy(&v, (const char*)((const uint16_t*)p.B + row * p.ldb) + 2u * (unsigned)n1, 8);
-                        if (j0 + BJ > J) v >>= shift;
-                        if (!full && m + e >= p.C) v = 0;
-                        bv[t][2 * e] = (unsigned)v;
-                        bv[t][2 * e + 1] = (unsigned)(v >> 32);
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const uint16_t* row = (const uint16_t*)p.B + (int64_t)min(m + e, (int)p.C - 1) * p.ldb;
-                        unsigned h[4];
-#pragma unroll
-                        for (int f = 0; f < 4; ++f) h[f] = m + e < p.C ? row[min(n + f, J - 1)] : 0u;
-                        bv[t][2 * e] = h[0] | (h[1] << 16);
-                        bv[t][2 * e + 1] = h[2] | (h[3] << 16);
-                    }
-                }
-            }
+        for (int t = 0; t < N; ++t) {
+            const int r = (t * WAVES + wave) * 8 + (lane >> 3), ch = (lane & 7) ^ swizzle(r);
+            off[t] = (unsigned)min(r, last) * (unsigned)(2 * p.ldb) + 16 * ch;
         }
+        col = 8 * ((lane & 7) ^ swizzle(wave * 8 + (lane >> 3)));  // (rows 64 apart have the same)
+        static_assert(N == 1 || WAVES % 4 == 0, "the rows of a lane agree in their swizzle");
     }
-
-    __device__ __forceinline__ void store_b(u32x4* lds, int tid, int wave) const {
+    __device__ __forceinline__ void load(const GemmParams& p, int64_t j0, int c, u32x4* lds, int lane, int wave) const {
+        const char* base = (const char*)p.B + (j0 * p.ldb + c) * 2;
 #pragma unroll
-        for (int t = 0; t < PB; ++t) {
-            const int id = t * NT + tid;
-            if constexpr (!kCheckpoint) {
-                const int r = id >> 3, ch = id & 7;
-                lds[lds_chunk(r, ch)] = u32x4{bv[t][0], bv[t][1], bv[t][2], bv[t][3]};
-            } else {
-                const int quad = id % (BJ / 4), oct = octet<BJ>(t, tid, wave);
-#pragma unroll
-                for (int f = 0; f < 4; ++f) {
-                    u32x4 o;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        o[e] = __builtin_amdgcn_perm(bv[t][2 * (2 * e + 1) + (f >> 1)], bv[t][2 * (2 * e) + (f >> 1)],
-                                                     (f & 1) ? 0x07060302u : 0x05040100u);
-                    lds[lds_chunk(4 * quad + f, oct)] = o;
-                }
-            }
+        for (int t = 0; t < N; ++t) {
+            u32x4* to = lds + (t * WAVES + wave) * 64;
+            if (c + col < p.C) __builtin_amdgcn_global_load_lds((global_ptr)(base + off[t]), (lds_ptr)to, 16, 0, 0);
+            else to[lane] = u32x4{0, 0, 0, 0};
         }
     }
 };
@@ -273,13 +274,20 @@ __device__ __forceinline__ int xcd_tile(int b, int count) {
 
 template <bool BF, bool LUT, int MODE, int BI, int BJ, int WI, int WJ>
 __global__ __launch_bounds__(64 * WI * WJ) void group_gemm_kernel(const GemmParams p) {
-    using G = Gemm<BF, LUT, MODE, BI, BJ, WI, WJ>;
-    constexpr int MI = G::MI, MJ = G::MJ;
-    __shared__ u32x4 s_buf[2][(BI + BJ) * 8];
+    using G = StageA<BF, LUT, MODE, BI, BJ, WI, WJ>;
+    constexpr int MI = G::MI, MJ = G::MJ, WAVES = WI * WJ;
+    // (arrays of their own, so that the compiler can tell the direct loads' target from what is read and written beside them)
+    __shared__ u32x4 s_a0[BI * 8];
+    __shared__ u32x4 s_a1[BI * 8];
+    __shared__ u32x4 s_b0[BJ * 8];
+    __shared__ u32x4 s_b1[BJ * 8];
+    __shared__ unsigned s_touched[64 * WAVES];  // never read
+    static_assert(BJ + G::kLines <= 64 * WAVES, "a thread touches one line");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave % WI, wj = wave / WI;
     const int tile = xcd_tile(blockIdx.x, p.itiles * p.jtiles);
-    const int i0 = tile % p.itiles * BI, j0 = tile / p.itiles * BJ;
+    const int i0 = tile % p.itiles * BI;
+    const int64_t j0 = (int64_t)(tile / p.itiles) * BJ;
     typename G::L levels;
     if constexpr (LUT) levels.init(p.w.levels);
 
@@ -291,51 +299,112 @@ __global__ __launch_bounds__(64 * WI * WJ) void group_gemm_kernel(const GemmPara
 
     const int s_begin = blockIdx.y * p.steps_per_split;
     const int s_end = min(s_begin + p.steps_per_split, (int)((p.C + kStep - 1) / kStep));
-    G st;
-    auto load = [&](int s) {
-        st.load_a(p, i0, s * kStep, tid, wave);
-        st.load_b(p, j0, s * kStep, tid, wave);
-    };
-    auto store = [&](int buf) {
-        st.store_a(s_buf[buf], tid, wave, levels);
-        st.store_b(s_buf[buf] + BI * 8, tid, wave);
-    };
-    auto compute = [&](int buf) {
-        const u32x4* s_a = s_buf[buf];
-        const u32x4* s_b = s_buf[buf] + BI * 8;
+    // fragment (tile a, half kk) starts at chunk frag[(kk ^ a) & 1] + 128 a of the wave's rows: 16 rows further
+    // the swizzle differs in the bit that kk sets
+    const int r16 = lane & 15, sw = swizzle(r16);
+    const int frag0 = r16 * 8 + ((lane >> 4) ^ sw), frag1 = r16 * 8 + ((4 + (lane >> 4)) ^ sw);
+    static_assert(MI % 2 == 0 && MJ % 2 == 0, "a wave's rows start at a multiple of 32");
+    auto compute = [&](const u32x4* a_rows, const u32x4* b_rows) {
+        a_rows += wi * MI * 128;
+        b_rows += wj * MJ * 128;
+        // Two rows of tiles at a time, their fragments read two turns ahead: left alone, the compiler reads each
+        // one just before its use and waits for LDS every time.
+        constexpr int kTurns = MI;
+        u32x4 af[3][2], bf[2][MJ];
+        auto read = [&](int t) {
+            const int kk = t / (MI / 2), a0 = t % (MI / 2) * 2;
+            if (a0 == 0) {
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            u32x4 af[MI], bf[MJ];
+                for (int b = 0; b < MJ; ++b) bf[kk][b] = b_rows[b * 128 + (((kk ^ b) & 1) ? frag1 : frag0)];
+            }
 #pragma unroll
-            for (int b = 0; b < MJ; ++b) bf[b] = s_b[lds_chunk((wj * MJ + b) * 16 + (lane & 15), kk * 4 + (lane >> 4))];
+            for (int a = 0; a < 2; ++a) af[t % 3][a] = a_rows[(a0 + a) * 128 + (((kk ^ a) & 1) ? frag1 : frag0)];
+        };
+        read(0);
+        read(1);
 #pragma unroll
-            for (int a = 0; a < MI; ++a) af[a] = s_a[lds_chunk((wi * MI + a) * 16 + (lane & 15), kk * 4 + (lane >> 4))];
+        for (int t = 0; t < kTurns; ++t) {
+            const int kk = t / (MI / 2), a0 = t % (MI / 2) * 2;
+            if (t + 2 < kTurns) read(t + 2);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int a = 0; a < MI; ++a)
+            for (int a = 0; a < 2; ++a)
 #pragma unroll
-                for (int b = 0; b < MJ; ++b) acc[a][b] = Act<BF>::mfma(af[a], bf[b], acc[a][b]);
+                for (int b = 0; b < MJ; ++b) acc[a0 + a][b] = Act<BF>::mfma(af[t % 3][a], bf[kk][b], acc[a0 + a][b]);
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
+    // Step s is multiplied while B of step s + 1 is on its way to LDS, A of step s + 1 is turned into LDS, and
+    // A of step s + 2 is on its way to registers.  Two waves share a SIMD: one stages while the other multiplies,
+    // then they change places.  What is in flight has half a step to arrive, which the L2 cache keeps and memory
+    // does not (about 3000 clocks, half as long again as a step's matrix work): each thread also touches one cache
+    // line of step s + kAhead, with a load that nobody waits for before the step after.
+    constexpr int kAhead = 4;
+    unsigned touch_stride = 2 * kStep;
+    const uint8_t* touch_at = (const uint8_t*)p.B + min(j0 + (tid < BJ ? tid : 0), p.J - 1) * p.ldb * 2;
+    if (tid >= BJ && tid < BJ + G::kLines) touch_at = G::line(p, i0, tid - BJ, touch_stride);
+    const bool stage_first = wave < WAVES / 2;
+    DirectB<BJ, WAVES> db;
+    G st;
+    auto step = [&](int s, const u32x4* a_now, u32x4* a_next, const u32x4* b_now, u32x4* b_next) {
+        const bool touched = s + kAhead < s_end && (int64_t)(s + kAhead + 1) * kStep <= p.C;
+        auto stage = [&]() {
+            if (s + 1 < s_end) st.store(a_next, p.C, (s + 1) * kStep, tid, wave, levels);
+            if (s + 2 < s_end) st.load(p, i0, (s + 2) * kStep, tid, wave);
+        };
+        // The touching load follows the direct ones, so these have arrived when at most one load is left of
+        // what was issued up to it.
+        auto direct = [&]() {
+            if (s + 1 < s_end) db.load(p, j0, (s + 1) * kStep, b_next, lane, wave);
+            __builtin_amdgcn_sched_barrier(0);
+            if (touched)
+                __builtin_amdgcn_global_load_lds((global_ptr)(touch_at + (uint64_t)(s + kAhead) * touch_stride),
+                                                 (lds_ptr)(s_touched + 64 * wave), 1, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto arrived = [&]() {
+            __builtin_amdgcn_sched_barrier(0);
+            if (touched) __builtin_amdgcn_s_waitcnt(0x0f71);  // vmcnt(1)
+            else __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0)
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        if (stage_first) stage();
+        direct();
+        compute(a_now, b_now);
+        arrived();
+        if (!stage_first) stage();
+        __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+        // (__syncthreads() would wait for the loads in flight too)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
     if (s_begin < s_end) {
-        load(s_begin);
-        store(0);
-        if (s_begin + 1 < s_end) load(s_begin + 1);
+        db.init(p, j0, lane, wave);
+        db.load(p, j0, s_begin * kStep, s_b0, lane, wave);
+        st.load(p, i0, s_begin * kStep, tid, wave);
+        st.store(s_a0, p.C, s_begin * kStep, tid, wave, levels);
+        if (s_begin + 1 < s_end) st.load(p, i0, (s_begin + 1) * kStep, tid, wave);
+        __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
         __syncthreads();
-        // Two waves share a SIMD: one stages the next step while the other computes, then they change places.
-        const bool stage_first = wave < WI * WJ / 2;
-        for (int s = s_begin; s < s_end; ++s) {
-            const int buf = (s - s_begin) & 1;
-            if (!stage_first) compute(buf);
-            if (s + 1 < s_end) store(buf ^ 1);
-            if (s + 2 < s_end) load(s + 2);
-            if (stage_first) compute(buf);
-            __syncthreads();
+        for (int s = s_begin; s < s_end; s += 2) {
+            step(s, s_a0, s_a1, s_b0, s_b1);
+            if (s + 1 < s_end) step(s + 1, s_a1, s_a0, s_b1, s_b0);
         }
     }
 
     // lane holds out[j][i .. i + 3], j = its column of the 16 x 16 tile
-    const int64_t jl = (int64_t)j0 + wj * MJ * 16 + (lane & 15);
+    const int64_t jl = j0 + wj * MJ * 16 + (lane & 15);
     const int il = i0 + wi * MI * 16 + 4 * (lane >> 4);
+    if constexpr (MODE >= (int)Product::GradWeight) {  // the partial column sums of dY, once
+        if (p.dbias && i0 == 0 && blockIdx.y == 0) {
+            for (int64_t j = j0 + tid; j < min(j0 + BJ, p.J); j += 64 * WAVES) {
+                float v = 0.0f;
+                for (int t = 0; t < p.bias_parts; ++t) v += p.bias_part[(int64_t)t * p.J + j];
+                p.dbias[j] = v;
+            }
+        }
+    }
     if constexpr (MODE == (int)Product::GradScales) {
         static_assert(BI / WI == 128, "a wave holds whole groups");
 #pragma unroll
@@ -421,7 +490,89 @@ __global__ __launch_bounds__(64 * WI * WJ) void group_gemm_kernel(const GemmPara
     }
 }
 
-GemmPlan gemm_plan(Product mode, int64_t I, int64_t J, int64_t C, int groups) {
+// ---- B in aligned rows along the contraction -------------------------------------------------------------
+// out[j][c], rows of p.pitch values (a multiple of 64, zeros from the contraction's end).
+// Transposed (dY): a workgroup takes 32 columns of 256 rows, through LDS; column sums of its rows on the way.
+__global__ __launch_bounds__(256) void transpose_grad_kernel(const StageBParams p, bool bf16) {
+    constexpr int kPitch = 264;  // 16-bit values of an LDS row: 16 bytes over 512
+    __shared__ __attribute__((aligned(16))) uint16_t s_t[32 * kPitch];
+    __shared__ float s_sum[4][32];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, cl = tid & 3, rl = tid >> 2;
+    const int64_t m0 = (int64_t)blockIdx.y * 256;
+    const int n0 = blockIdx.x * 32 + 8 * cl;
+    unsigned v[4][4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const int64_t m = m0 + 64 * t + rl;
+        const uint16_t* at = (const uint16_t*)p.in + (m < p.C ? m * p.ld : 0) + n0;
+        if (m < p.C && n0 + 8 <= p.J) {
+            __builtin_memcpy(v[t], at, 16);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const unsigned lo = m < p.C && n0 + 2 * e < p.J ? at[2 * e] : 0u;
+                const unsigned hi = m < p.C && n0 + 2 * e + 1 < p.J ? at[2 * e + 1] : 0u;
+                v[t][e] = lo | (hi << 16);
+            }
+        }
+    }
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int r = 64 * t + rl;
+            s_t[(8 * cl + 2 * e) * kPitch + r] = (uint16_t)v[t][e];
+            s_t[(8 * cl + 2 * e + 1) * kPitch + r] = (uint16_t)(v[t][e] >> 16);
+            sum[2 * e] += bf16 ? Act<true>::lo(v[t][e]) : Act<false>::lo(v[t][e]);
+            sum[2 * e + 1] += bf16 ? Act<true>::hi(v[t][e]) : Act<false>::hi(v[t][e]);
+        }
+    }
+    if (p.bias_part) {
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+#pragma unroll
+            for (int off = 4; off < 64; off <<= 1) sum[t] += __shfl_xor(sum[t], off);
+            if (lane < 4) s_sum[wave][8 * lane + t] = sum[t];
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {  // 32 rows of 512 bytes
+        const int id = t * 256 + tid, r = id >> 5, ch = id & 31;
+        const int64_t j = (int64_t)blockIdx.x * 32 + r, c = m0 + 8 * ch;
+        if (j < p.J && c < p.pitch) *(u32x4*)((uint16_t*)p.out + j * p.pitch + c) = *(const u32x4*)(s_t + r * kPitch + 8 * ch);
+    }
+    const int64_t j = (int64_t)blockIdx.x * 32 + tid;
+    if (p.bias_part && tid < 32 && j < p.J)
+        p.bias_part[blockIdx.y * p.J + j] = ((s_sum[0][tid] + s_sum[1][tid]) + s_sum[2][tid]) + s_sum[3][tid];
+}
+
+// Copied: eight neighbours a thread.
+__global__ __launch_bounds__(256) void align_rows_kernel(const StageBParams p) {
+    const int64_t per_row = p.pitch >> 3, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t j = id / per_row, c = (id - j * per_row) * 8;
+    if (j >= p.J) return;
+    const uint16_t* at = (const uint16_t*)p.in + j * p.ld + c;
+    u32x4 v;
+    if (c + 8 <= p.C) {
+        __builtin_memcpy(&v, at, 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const unsigned lo = c + 2 * e < p.C ? at[2 * e] : 0u;
+            const unsigned hi = c + 2 * e + 1 < p.C ? at[2 * e + 1] : 0u;
+            v[e] = lo | (hi << 16);
+        }
+    }
+    *(u32x4*)((uint16_t*)p.out + j * p.pitch + c) = v;
+}
+
+static bool rows_are_aligned(const void* B, int64_t ldb, int64_t C) {
+    return ((uintptr_t)B & 15) == 0 && (ldb & 7) == 0 && (C & 7) == 0 && ldb < (int64_t(1) << 22);
+}
+
+GemmPlan gemm_plan(Product mode, const void* B, int64_t ldb, int64_t I, int64_t J, int64_t C, int groups) {
     GemmPlan g;
     const int64_t steps = ceil_div64(C, kStep);
     auto tiles = [&](int bi, int bj) { return ceil_div64(I, bi) * ceil_div64(J, bj); };
@@ -434,12 +585,22 @@ GemmPlan gemm_plan(Product mode, int64_t I, int64_t J, int64_t C, int groups) {
     int64_t splits = 1;
     const int64_t t = tiles(g.bi, g.bj);
     if (t < 256) splits = 512 / t < steps / 4 ? 512 / t : steps / 4;
+#ifdef KQ_PROBE
+    if (getenv("KQ_T")) { g.bi = atoi(getenv("KQ_T")) / 1000; g.bj = atoi(getenv("KQ_T")) % 1000; }
+    if (getenv("KQ_S")) splits = atoi(getenv("KQ_S"));
+#endif
     if (splits < 1) splits = 1;
     g.steps_per_split = (int)ceil_div64(steps, splits);
     if (g.steps_per_split < 1) g.steps_per_split = 1;
     g.splits = steps ? (int)ceil_div64(steps, g.steps_per_split) : 1;
     const int64_t values = mode == Product::GradScales ? J * groups : I * J;
-    g.ws_bytes = g.splits > 1 ? (size_t)g.splits * (size_t)values * sizeof(float) : 0;
+    auto region = [](size_t bytes) { return (bytes + 255) & ~size_t(255); };
+    g.part_bytes = g.splits > 1 ? region((size_t)g.splits * (size_t)values * sizeof(float)) : 0;
+    g.stage_b = !rows || !rows_are_aligned(B, ldb, C);
+    g.pitch = ceil_div64(C, kStep) * kStep;
+    g.b_bytes = g.stage_b ? region((size_t)J * (size_t)g.pitch * 2) : 0;
+    g.bias_parts = rows ? 0 : (int)ceil_div64(C, 256);
+    g.ws_bytes = g.part_bytes + g.b_bytes + (rows ? 0 : region((size_t)g.bias_parts * (size_t)J * sizeof(float)));
     return g;
 }
 
@@ -468,12 +629,24 @@ static hipError_t launch_mode(bool bf16, const GemmPlan& g, const GemmParams& p,
     return launch_tile<MODE, 128, 128, MODE == (int)Product::GradScales ? 1 : 2, MODE == (int)Product::GradScales ? 4 : 2>(bf16, p, s);
 }
 
-hipError_t launch_gemm(Product mode, bool bf16, const GemmPlan& plan, GemmParams p, hipStream_t s) {
+hipError_t launch_gemm(Product mode, bool bf16, const GemmPlan& plan, GemmParams p, void* ws, hipStream_t s) {
+    const bool rows = mode == Product::Linear || mode == Product::GradInput;
     p.itiles = (int)ceil_div64(p.I, plan.bi);
     p.jtiles = (int)ceil_div64(p.J, plan.bj);
     p.splits = plan.splits;
     p.steps_per_split = plan.steps_per_split;
-    if (plan.splits == 1) p.part = nullptr;
+    p.part = plan.splits > 1 ? (float*)ws : nullptr;
+    p.bias_parts = plan.bias_parts;
+    p.bias_part = p.dbias ? (float*)((char*)ws + plan.part_bytes + plan.b_bytes) : nullptr;
+    if (plan.stage_b && p.C > 0) {
+        const StageBParams b = {p.B, p.ldb, p.J, p.C, (char*)ws + plan.part_bytes, plan.pitch, p.bias_part};
+        if (rows) align_rows_kernel<<<dim3((unsigned)ceil_div64(p.J * (plan.pitch >> 3), 256)), dim3(256), 0, s>>>(b);
+        else transpose_grad_kernel<<<dim3((unsigned)ceil_div64(p.J, 32), (unsigned)plan.bias_parts), dim3(256), 0, s>>>(b, bf16);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        p.B = b.out;
+        p.ldb = plan.pitch;
+    }
     hipError_t e;
     switch (mode) {
         case Product::Linear: e = launch_mode<0>(bf16, plan, p, s); break;
@@ -482,7 +655,6 @@ hipError_t launch_gemm(Product mode, bool bf16, const GemmPlan& plan, GemmParams
         default: e = launch_mode<3>(bf16, plan, p, s);
     }
     if (e != hipSuccess || plan.splits == 1) return e;
-    const bool rows = mode == Product::Linear || mode == Product::GradInput;
     const JoinParams j = {p.part, p.splits, p.J, mode == Product::GradScales ? p.w.groups : p.I, p.bias, p.out, p.ldo,
                           rows ? (bf16 ? KQ_T_BF16 : KQ_T_F16) : KQ_T_F32};
     return launch_join(j, s);

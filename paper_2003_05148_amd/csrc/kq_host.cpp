@@ -351,7 +351,7 @@ PyObject* group_linear(PyObject*, PyObject* const* a, Py_ssize_t count) {
         }
         void* const s = c.stream();
         if (!c.ok) return nullptr;
-        const at::Tensor ws = c.scratch(g_lib.linear_ws(m, n, k));
+        const at::Tensor ws = c.scratch(g_lib.linear_ws(X.data_ptr(), ldx, m, n, k));
         if (!Y.defined()) {
             Y = c.make({m, n}, X.scalar_type());
             ldy = n;
@@ -380,7 +380,7 @@ PyObject* grad_input(PyObject*, PyObject* const* a, Py_ssize_t count) {
         }
         void* const s = c.stream();
         if (!c.ok) return nullptr;
-        const at::Tensor ws = c.scratch(g_lib.grad_input_ws(m, n, k));
+        const at::Tensor ws = c.scratch(g_lib.grad_input_ws(dY.data_ptr(), ldy, m, n, k));
         if (!dX.defined()) {
             dX = c.make({m, k}, dY.scalar_type());
             ldx = k;
