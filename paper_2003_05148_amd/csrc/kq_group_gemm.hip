@@ -15,10 +15,6 @@
 // about half of them are exact); checkpoints and activations are exact, sums are fp32.
 #include "kq_group.h"
 
-#ifdef KQ_PROBE
-#include <stdlib.h>
-#endif
-
 namespace kq {
 
 constexpr int kStep = 64;  // contraction per step
@@ -89,31 +85,6 @@ struct StageA {
     static_assert(kATasks % NT == 0 && PA >= 1, "A tasks");
     unsigned w[PA][kWeightRows ? 2 : 8];
     unsigned short x[PA][kWeightRows ? 2 : 8];  // scales (bf16 bits) or checkpoint exponents
-
-    // Cache lines of a step's A: where line `id` of step 0 lies, and how far on it is a step later.
-    static constexpr int kLines = kWeightRows ? BI / 4 : kWeightCols ? BI / 4 + 64 : BI / 2 + 64;
-    static __device__ __forceinline__ const uint8_t* line(const GemmParams& p, int i0, int id, unsigned& stride) {
-        if constexpr (kWeightRows) {  // four lines a tile of codes and step (scales: a line holds many steps' worth)
-            const int nt = min((i0 >> 4) + (id >> 2), p.w.ntiles - 1);
-            stride = kTileBytes / 2;
-            return p.w.codes + (int64_t)nt * p.w.ktiles * kTileBytes + (id & 3) * 128;
-        } else if constexpr (kWeightCols) {
-            if (id < BI / 4) {  // 4 tiles of rows, BI / 128 of columns, eight lines each
-                const int kt = min((i0 >> 7) + (id >> 3) % (BI / 128), p.w.ktiles - 1);
-                stride = 4u * p.w.ktiles * kTileBytes;
-                return p.w.codes + ((int64_t)(id / (BI / 16)) * p.w.ktiles + kt) * kTileBytes + (id & 7) * 128;
-            }
-            stride = 2u * kStep * p.w.groups;
-            return (const uint8_t*)(p.w.scales + (int64_t)(id - BI / 4) * p.w.groups + (i0 >> p.w.log_group));
-        } else {
-            if (id < BI / 2) {
-                stride = (unsigned)kStep * p.kq;
-                return (const uint8_t*)p.q + (int64_t)(id / (BI / 128)) * p.kq + min(i0 + id % (BI / 128) * 128, p.kq - 1);
-            }
-            stride = (unsigned)kStep * (p.kq >> 5);
-            return p.exps + (int64_t)(id - BI / 2) * (p.kq >> 5) + (i0 >> 5);
-        }
-    }
 
     // Which rows of the contraction a thread's transposed tasks take: octet t * kOctets + ...; with 256
     // rows of output a wave has one octet, and its row addresses are scalar.
@@ -281,8 +252,6 @@ __global__ __launch_bounds__(64 * WI * WJ) void group_gemm_kernel(const GemmPara
     __shared__ u32x4 s_a1[BI * 8];
     __shared__ u32x4 s_b0[BJ * 8];
     __shared__ u32x4 s_b1[BJ * 8];
-    __shared__ unsigned s_touched[64 * WAVES];  // never read
-    static_assert(BJ + G::kLines <= 64 * WAVES, "a thread touches one line");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave % WI, wj = wave / WI;
     const int tile = xcd_tile(blockIdx.x, p.itiles * p.jtiles);
@@ -336,45 +305,24 @@ __global__ __launch_bounds__(64 * WI * WJ) void group_gemm_kernel(const GemmPara
     };
     // Step s is multiplied while B of step s + 1 is on its way to LDS, A of step s + 1 is turned into LDS, and
     // A of step s + 2 is on its way to registers.  Two waves share a SIMD: one stages while the other multiplies,
-    // then they change places.  What is in flight has half a step to arrive, which the L2 cache keeps and memory
-    // does not (about 3000 clocks, half as long again as a step's matrix work): each thread also touches one cache
-    // line of step s + kAhead, with a load that nobody waits for before the step after.
-    constexpr int kAhead = 4;
-    unsigned touch_stride = 2 * kStep;
-    const uint8_t* touch_at = (const uint8_t*)p.B + min(j0 + (tid < BJ ? tid : 0), p.J - 1) * p.ldb * 2;
-    if (tid >= BJ && tid < BJ + G::kLines) touch_at = G::line(p, i0, tid - BJ, touch_stride);
+    // then they change places.
     const bool stage_first = wave < WAVES / 2;
     DirectB<BJ, WAVES> db;
     G st;
     auto step = [&](int s, const u32x4* a_now, u32x4* a_next, const u32x4* b_now, u32x4* b_next) {
-        const bool touched = s + kAhead < s_end && (int64_t)(s + kAhead + 1) * kStep <= p.C;
         auto stage = [&]() {
             if (s + 1 < s_end) st.store(a_next, p.C, (s + 1) * kStep, tid, wave, levels);
             if (s + 2 < s_end) st.load(p, i0, (s + 2) * kStep, tid, wave);
         };
-        // The touching load follows the direct ones, so these have arrived when at most one load is left of
-        // what was issued up to it.
-        auto direct = [&]() {
-            if (s + 1 < s_end) db.load(p, j0, (s + 1) * kStep, b_next, lane, wave);
-            __builtin_amdgcn_sched_barrier(0);
-            if (touched)
-                __builtin_amdgcn_global_load_lds((global_ptr)(touch_at + (uint64_t)(s + kAhead) * touch_stride),
-                                                 (lds_ptr)(s_touched + 64 * wave), 1, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
-        };
-        auto arrived = [&]() {
-            __builtin_amdgcn_sched_barrier(0);
-            if (touched) __builtin_amdgcn_s_waitcnt(0x0f71);  // vmcnt(1)
-            else __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0)
-            __builtin_amdgcn_sched_barrier(0);
-        };
         if (stage_first) stage();
-        direct();
+        if (s + 1 < s_end) db.load(p, j0, (s + 1) * kStep, b_next, lane, wave);
+        __builtin_amdgcn_sched_barrier(0);
         compute(a_now, b_now);
-        arrived();
+        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the direct loads (A's come after them, or were waited for)
+        __builtin_amdgcn_sched_barrier(0);
         if (!stage_first) stage();
         __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
-        // (__syncthreads() would wait for the loads in flight too)
+        // (__syncthreads() would wait for the loads of A too)
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -572,24 +520,48 @@ static bool rows_are_aligned(const void* B, int64_t ldb, int64_t C) {
     return ((uintptr_t)B & 15) == 0 && (ldb & 7) == 0 && (C & 7) == 0 && ldb < (int64_t(1) << 22);
 }
 
+// The tile and the splits with the shortest modelled time.  A workgroup's step takes `alone` us while it has a CU
+// to itself, and a CU with n workgroups at hand takes n times `shared`; a split contraction pays the joining
+// launch and its partial sums, written and read at about 6 MB a us.  The figures are fitted to sweeps of all
+// tiles and 1 to 16 splits (us; modelled times are within a fifth of them, and what is picked is within a tenth
+// of the best): X 512 x 4096 by W 4096 x 4096, 128x128 tiles 62 40 36 45 for 1 2 4 8 splits, 256x128 80 49 35
+// 46, 256x256 120 71 48 42; 64 rows of X, 128x32 52 30 19 17, 128x128 61 36 23 19; 1024 rows, 256x128 81
+// 58, 256x256 121 76 56; dX of 512 rows, 128x128 91 55 60, 256x128 99 61 41; scales' gradient 2048 x 4096 x
+// 1024, 128x128 62 46 51, 256x256 76 50 39.
+struct TileTime {
+    int bi, bj;
+    float alone[3], shared[3];  // Linear, GradInput, the gradients from a checkpoint
+};
+constexpr TileTime kTiles[] = {
+    {128, 32, {0.62f, 1.10f, 0.0f}, {0.33f, 0.42f, 0.0f}},
+    {128, 64, {0.70f, 1.00f, 0.0f}, {0.50f, 0.60f, 0.0f}},
+    {128, 128, {0.92f, 1.30f, 1.50f}, {0.60f, 1.00f, 0.95f}},
+    {256, 128, {1.15f, 1.37f, 0.0f}, {1.15f, 1.37f, 0.0f}},
+    {256, 256, {1.75f, 1.80f, 2.00f}, {1.75f, 1.80f, 2.00f}},
+};
+
 GemmPlan gemm_plan(Product mode, const void* B, int64_t ldb, int64_t I, int64_t J, int64_t C, int groups) {
-    GemmPlan g;
+    GemmPlan g = {};
     const int64_t steps = ceil_div64(C, kStep);
-    auto tiles = [&](int bi, int bj) { return ceil_div64(I, bi) * ceil_div64(J, bj); };
     const bool rows = mode == Product::Linear || mode == Product::GradInput;
-    if (tiles(256, 256) >= 192) g.bi = g.bj = 256;
-    else if (rows && J <= 32) g.bi = 128, g.bj = 32;
-    else if (rows && J <= 64) g.bi = 128, g.bj = 64;
-    else if (rows && tiles(256, 128) >= 192) g.bi = 256, g.bj = 128;
-    else g.bi = g.bj = 128;
+    const int column = mode == Product::Linear ? 0 : mode == Product::GradInput ? 1 : 2;
+    const float value_us = (mode == Product::GradScales ? (float)J * groups : (float)I * J) * 8.0f / 6e6f;
+    float best = 0.0f;
     int64_t splits = 1;
-    const int64_t t = tiles(g.bi, g.bj);
-    if (t < 256) splits = 512 / t < steps / 4 ? 512 / t : steps / 4;
-#ifdef KQ_PROBE
-    if (getenv("KQ_T")) { g.bi = atoi(getenv("KQ_T")) / 1000; g.bj = atoi(getenv("KQ_T")) % 1000; }
-    if (getenv("KQ_S")) splits = atoi(getenv("KQ_S"));
-#endif
-    if (splits < 1) splits = 1;
+    for (const TileTime& t : kTiles) {
+        if (t.alone[column] == 0.0f) continue;
+        const int64_t tiles = ceil_div64(I, t.bi) * ceil_div64(J, t.bj);
+        for (int s = 1; s <= 32 && (s == 1 || (s * 2 <= steps && s * tiles <= 1024)); s = s < 4 ? s + 1 : s * 3 / 2) {  // 1 2 3 4 6 9 13 ..
+            const float n = (float)ceil_div64(tiles * s, 256), step = n * t.shared[column] > t.alone[column] ? n * t.shared[column] : t.alone[column];
+            const float us = (float)ceil_div64(steps, s) * step + (s > 1 ? 2.5f + s * value_us : 0.0f);
+            if (g.bi == 0 || us < best) {
+                best = us;
+                g.bi = t.bi;
+                g.bj = t.bj;
+                splits = s;
+            }
+        }
+    }
     g.steps_per_split = (int)ceil_div64(steps, splits);
     if (g.steps_per_split < 1) g.steps_per_split = 1;
     g.splits = steps ? (int)ceil_div64(steps, g.steps_per_split) : 1;
