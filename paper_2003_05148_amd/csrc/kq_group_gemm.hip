@@ -190,7 +190,7 @@ struct StageA {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const unsigned ex = 2 * e + h < left ? x[t][2 * e + h] : 0;
-                        const float s = __builtin_bit_cast(float, ex == 255u ? 0x7fc00000u : ex << 23);
+                        const float s = __builtin_bit_cast(float, ex << 23);  // 255: infinity, and inf - inf below
                         const unsigned u = w[t][2 * e + h] ^ 0x80808080u;  // q + 128
 #pragma unroll
                         for (int j = 0; j < 4; ++j) v[h][j] = __builtin_fmaf((float)((u >> (8 * j)) & 255u), s, -128.0f * s);
