@@ -1205,3 +1205,46 @@ def kq_checkpoint_grad_weight(dY, q, exps, in_features: int, bias: bool = False,
     _check(lib.kq_checkpoint_grad_weight(dy.data_ptr(), ty, ldy, m, n, k, q.data_ptr(), exps.data_ptr(), out.data_ptr(),
                                          ldw, _ptr(dbias), wp, wn, _stream(dev)), "kq_checkpoint_grad_weight")
     return dW, dbias
+
+
+class GroupLinear:
+    """A fully-connected layer in 4 bits: codes, bf16 group scales (with an fp32 master copy for retraining), a
+    level table or None, and an fp32 bias or None, on the weight's device.
+
+    ``layer(X)`` is the serving call.  ``layer.forward(X)`` also returns the 8-bit checkpoint of X that
+    ``layer.backward(dY, checkpoint)`` takes the gradients of the scales and of the bias from; ``layer.step``
+    moves both against them, as Eq. (2) moves a codebook's entries: a shared value follows the gradients of what
+    it stands for, and the codes stay."""
+
+    def __init__(self, W, group: int = 128, levels=None, bias=None):
+        self.group, self.levels = int(group), levels
+        self.codes, self.scales = kq_quantize_groups(W, self.group, levels)
+        self.out_features, self.in_features = W.shape
+        self.master = self.scales.float()
+        self.bias = None if bias is None else _dev(bias, torch.float32, "bias", (self.out_features,)).clone()
+
+    def __call__(self, X):
+        return kq_group_linear(X, self.codes, self.scales, self.group, self.levels, self.bias)
+
+    def forward(self, X):
+        """(Y, checkpoint of X)."""
+        return self(X), kq_checkpoint_pack(X)
+
+    def backward(self, dY, checkpoint, input_grad: bool = True):
+        """(dX or None, dscales fp32, dbias fp32 or None)."""
+        dX = kq_group_linear_grad_input(dY, self.codes, self.scales, self.in_features, self.group,
+                                        self.levels) if input_grad else None
+        ds, db = kq_checkpoint_grad_scales(dY, *checkpoint, self.codes, self.in_features, self.group, self.levels,
+                                           self.bias is not None)
+        return dX, ds, db
+
+    def step(self, dscales, dbias, gamma: float):
+        """scales -= gamma * dscales (in the fp32 master, then rounded to bf16), bias -= gamma * dbias."""
+        self.master.sub_(dscales, alpha=float(gamma))
+        self.scales.copy_(self.master)
+        if self.bias is not None and dbias is not None:
+            self.bias.sub_(dbias, alpha=float(gamma))
+
+    def weight(self, dtype=torch.float32):
+        """The weights that the layer stands for."""
+        return kq_reconstruct_groups(self.codes, self.scales, self.in_features, self.group, self.levels, dtype)

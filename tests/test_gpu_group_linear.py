@@ -647,3 +647,35 @@ def test_the_general_path_gives_the_same(monkeypatch):
     monkeypatch.setattr(kq, "_fast", None)
     for a, b in zip(want, step()):
         assert a.dtype == b.dtype and a.shape == b.shape and torch.equal(a, b)
+
+
+# ---- the layer and the example ---------------------------------------------------------------------------------------
+
+def test_layer_class_is_its_calls():
+    W = torch.randn(70, 200, generator=gen(1)).to(DEV)
+    b = torch.randn(70, generator=gen(2)).to(DEV)
+    lv = table(3).to(DEV)
+    layer = kq.GroupLinear(W, 32, lv, b)
+    X, dY = acts(24, 200, BF, seed=4).to(DEV), acts(24, 70, BF, seed=5).to(DEV)
+    Y, ck = layer.forward(X)
+    assert torch.equal(Y, kq.kq_group_linear(X, layer.codes, layer.scales, 32, lv, b)) and torch.equal(layer(X), Y)
+    dX, ds, db = layer.backward(dY, ck)
+    assert torch.equal(dX, kq.kq_group_linear_grad_input(dY, layer.codes, layer.scales, 200, 32, lv))
+    assert torch.equal(ds, kq.kq_checkpoint_grad_scales(dY, *ck, layer.codes, 200, 32, lv)[0])
+    before = layer.master.clone()
+    layer.step(ds, db, 0.5)
+    assert torch.equal(layer.master, before - 0.5 * ds) and torch.equal(layer.scales, layer.master.to(BF))
+    assert torch.equal(layer.bias, b - 0.5 * db)
+    assert layer.weight(BF).dtype == BF and layer.backward(dY, ck, input_grad=False)[0] is None
+
+
+def test_retraining_example_lowers_the_error():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "fc4_retrain.py")
+    spec = importlib.util.spec_from_file_location("fc4_retrain", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    losses, _ = mod.retrain(n_in=512, n_hidden=500, n_out=100, batch=128, steps=25, group=64)
+    assert all(math.isfinite(v) for v in losses)
+    assert sum(losses[-5:]) < 0.9 * sum(losses[:5])
