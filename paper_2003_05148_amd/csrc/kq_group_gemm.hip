@@ -306,7 +306,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void group_gemm_kernel(const GemmPara
     // Step s is multiplied while B of step s + 1 is on its way to LDS, A of step s + 1 is turned into LDS, and
     // A of step s + 2 is on its way to registers.  Two waves share a SIMD: one stages while the other multiplies,
     // then they change places.
-    const bool stage_first = wave < WAVES / 2;
+    const bool stage_first = MODE == (int)Product::Linear || wave < WAVES / 2;
     DirectB<BJ, WAVES> db;
     G st;
     auto step = [&](int s, const u32x4* a_now, u32x4* a_next, const u32x4* b_now, u32x4* b_next) {
@@ -589,16 +589,20 @@ static hipError_t launch_tile(bool bf16, const GemmParams& p, hipStream_t s) {
     return hipGetLastError();
 }
 
+// (a tile that a product has no kernel for is refused: a kernel must have the plan's tile)
 template <int MODE>
 static hipError_t launch_mode(bool bf16, const GemmPlan& g, const GemmParams& p, hipStream_t s) {
+    const int tile = g.bi * 1000 + g.bj;
     if constexpr (MODE == (int)Product::Linear || MODE == (int)Product::GradInput) {
-        if (g.bj == 32) return launch_tile<MODE, 128, 32, 4, 1>(bf16, p, s);
-        if (g.bj == 64) return launch_tile<MODE, 128, 64, 2, 2>(bf16, p, s);
-        if (g.bi == 256 && g.bj == 128) return launch_tile<MODE, 256, 128, 4, 2>(bf16, p, s);
+        if (tile == 128032) return launch_tile<MODE, 128, 32, 4, 1>(bf16, p, s);
+        if (tile == 128064) return launch_tile<MODE, 128, 64, 2, 2>(bf16, p, s);
+        if (tile == 256128) return launch_tile<MODE, 256, 128, 4, 2>(bf16, p, s);
     }
-    if (g.bi == 256) return launch_tile<MODE, 256, 256, 2, 4>(bf16, p, s);
+    if (tile == 256256) return launch_tile<MODE, 256, 256, 2, 4>(bf16, p, s);
     // (a wave of the scales' gradient holds whole groups)
-    return launch_tile<MODE, 128, 128, MODE == (int)Product::GradScales ? 1 : 2, MODE == (int)Product::GradScales ? 4 : 2>(bf16, p, s);
+    if (tile == 128128)
+        return launch_tile<MODE, 128, 128, MODE == (int)Product::GradScales ? 1 : 2, MODE == (int)Product::GradScales ? 4 : 2>(bf16, p, s);
+    return hipErrorInvalidValue;
 }
 
 hipError_t launch_gemm(Product mode, bool bf16, const GemmPlan& plan, GemmParams p, void* ws, hipStream_t s) {
