@@ -91,7 +91,7 @@ __device__ __forceinline__ unsigned max_bits(const float (&v)[8]) {
 }
 
 // ---- quantizer -----------------------------------------------------------------------------------------
-// Sixteen lanes a row of a 16 x 128 tile, 8 neighbouring columns and one dword of codes a lane, four rows a
+// A workgroup a 16 x 128 tile, sixteen lanes a row, 8 neighbouring columns and one dword of codes a lane, four rows a
 // wave: a row's lanes read contiguous memory, and a group's columns lie in 4, 8 or 16 neighbouring lanes.
 // Per group: a = max |w| (a non-finite value is larger than every other), s = bf16(a / top) with top = 7 or
 // the largest |level| (zero below the normal range, NaN where a is not finite), and per weight t = w / s in
@@ -117,9 +117,8 @@ __device__ __forceinline__ unsigned nearest_level_code(float t, const float* mid
 template <int TYPE, bool LUT>
 __global__ __launch_bounds__(256) void quantize_groups_kernel(const QuantizeParams p) {
     const int lane = threadIdx.x & 63, l16 = lane & 15;
-    const int64_t id = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);  // row of a tile: tile * 16 + row
-    const int64_t tile = id >> 4;
-    const int64_t tiles = (int64_t)ceil_div(p.n, kTileRows) * p.ktiles;
+    const unsigned tile = blockIdx.x;
+    const int64_t id = (int64_t)tile * 16 + (threadIdx.x >> 4);  // row of a tile
     __shared__ float s_mid[17];
     float top = 7.0f;
     if constexpr (LUT) {
@@ -131,8 +130,7 @@ __global__ __launch_bounds__(256) void quantize_groups_kernel(const QuantizePara
         for (int j = 0; j < 16; ++j) top = __builtin_fmaxf(top, __builtin_fabsf(bf16_bits_to_f32(p.levels[j])));
         __syncthreads();
     }
-    if (tile >= tiles) return;  // (all lanes of a row, and of the workgroup's rows of the tile)
-    const int nt = (int)(tile / p.ktiles), kt = (int)(tile - (int64_t)nt * p.ktiles);
+    const int nt = (int)(tile / (unsigned)p.ktiles), kt = (int)(tile - (unsigned)nt * p.ktiles);
     const int row = nt * kTileRows + (int)(id & 15);
     const bool live = row < p.n;
     const int limit = live ? p.k : 0;
@@ -203,16 +201,16 @@ hipError_t launch_quantize_groups(const QuantizeParams& p, hipStream_t s) {
 template <int TYPE, bool LUT>
 __global__ __launch_bounds__(256) void reconstruct_groups_kernel(const ReconstructGroupsParams p) {
     const int l16 = threadIdx.x & 15;
-    const int64_t tile = blockIdx.x;
+    const unsigned tile = blockIdx.x;
     __shared__ float s_level[16];
     if constexpr (LUT) {
         if (threadIdx.x < 16) s_level[threadIdx.x] = bf16_bits_to_f32(p.w.levels[threadIdx.x]);
         __syncthreads();
     }
-    const int nt = (int)(tile / p.w.ktiles), kt = (int)(tile - (int64_t)nt * p.w.ktiles);
+    const int nt = (int)(tile / (unsigned)p.w.ktiles), kt = (int)(tile - (unsigned)nt * p.w.ktiles);
     const int r = threadIdx.x >> 4, row = nt * kTileRows + r;
     if (row >= p.w.n) return;
-    const unsigned* codes = (const unsigned*)(p.w.codes + tile * kTileBytes + r * 64);
+    const unsigned* codes = (const unsigned*)(p.w.codes + (int64_t)tile * kTileBytes + r * 64);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int cc = 64 * h + 4 * l16, c0 = kt * kTileCols + cc;  // dword 4 q + i of columns 32 i + 8 q
@@ -254,10 +252,10 @@ hipError_t launch_reconstruct_groups(const ReconstructGroupsParams& p, hipStream
 template <int TYPE>
 __global__ __launch_bounds__(256) void checkpoint_pack_kernel(const CheckpointParams p) {
     const int per_row = p.kq >> 3;  // 8-column pieces
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t row = id / per_row;
+    const unsigned id = blockIdx.x * 256u + threadIdx.x;  // (at most 2^34 values: fewer than 2^32 threads)
+    const int64_t row = id / (unsigned)per_row;
     const bool live = row < p.m;     // (groups are whole: the four lanes of one agree)
-    const int c0 = live ? (int)(id - row * per_row) * 8 : 0;
+    const int c0 = live ? (int)(id - (unsigned)row * per_row) * 8 : 0;
     float v[8];
     load_columns<TYPE>(p.X, live ? row * p.ldx : 0, c0, live ? p.k : 0, v);
     unsigned a = max_bits(v);
@@ -292,10 +290,10 @@ __device__ __forceinline__ float checkpoint_step(unsigned e) {
 template <int TYPE>
 __global__ __launch_bounds__(256) void checkpoint_restore_kernel(const CheckpointParams p) {
     const int per_row = p.kq >> 3;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t row = id / per_row;
+    const unsigned id = blockIdx.x * 256u + threadIdx.x;
+    const int64_t row = id / (unsigned)per_row;
     if (row >= p.m) return;
-    const int c0 = (int)(id - row * per_row) * 8;
+    const int c0 = (int)(id - (unsigned)row * per_row) * 8;
     if (c0 >= p.k) return;
     const u32x2 w = *(const u32x2*)(p.q + row * p.kq + c0);
     const float step = checkpoint_step(p.exps[row * (p.kq >> 5) + (c0 >> 5)]);
@@ -325,14 +323,26 @@ hipError_t launch_checkpoint_restore(const CheckpointParams& p, hipStream_t s) {
 // ---- partial sums of a split contraction -------------------------------------------------------------------------
 template <int TYPE>
 __global__ __launch_bounds__(256) void join_kernel(const JoinParams p) {
-    const int64_t per_row = (p.cols + 3) >> 2, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t r = id / per_row, c = (id - r * per_row) * 4, total = p.rows * p.cols;
+    const unsigned per_row = (unsigned)((p.cols + 3) >> 2), id = blockIdx.x * 256u + threadIdx.x;  // (fewer than 2^32 threads)
+    const int64_t r = id / per_row, c = (int64_t)(id - (unsigned)r * per_row) * 4, total = p.rows * p.cols;
     if (r >= p.rows) return;
     float v[4] = {0, 0, 0, 0};
     const float* part = p.part + r * p.cols + c;
     const int count = (int)min((int64_t)4, p.cols - c);
+    // (four splits' loads in flight at a time; the sums stay in order)
     if (count == 4) {
-        for (int s = 0; s < p.splits; ++s, part += total) {
+        int s = 0;
+        for (; s + 4 <= p.splits; s += 4, part += 4 * total) {
+            float x[4][4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) __builtin_memcpy(x[u], part + u * total, 16);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) v[t] += x[u][t];
+        }
+#pragma unroll 3
+        for (; s < p.splits; ++s, part += total) {
             float x[4];
             __builtin_memcpy(x, part, 16);
 #pragma unroll

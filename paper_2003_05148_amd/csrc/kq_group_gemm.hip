@@ -498,8 +498,8 @@ __global__ __launch_bounds__(256) void transpose_grad_kernel(const StageBParams 
 
 // Copied: eight neighbours a thread.
 __global__ __launch_bounds__(256) void align_rows_kernel(const StageBParams p) {
-    const int64_t per_row = p.pitch >> 3, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t j = id / per_row, c = (id - j * per_row) * 8;
+    const unsigned per_row = (unsigned)(p.pitch >> 3), id = blockIdx.x * 256u + threadIdx.x;  // (fewer than 2^32 threads)
+    const int64_t j = id / per_row, c = (int64_t)(id - (unsigned)j * per_row) * 8;
     if (j >= p.J) return;
     const uint16_t* at = (const uint16_t*)p.in + j * p.ld + c;
     u32x4 v;
@@ -523,11 +523,11 @@ static bool rows_are_aligned(const void* B, int64_t ldb, int64_t C) {
 // The tile and the splits with the shortest modelled time.  A workgroup's step takes `alone` us while it has a CU
 // to itself, and a CU with n workgroups at hand takes n times `shared`; a split contraction pays the joining
 // launch and its partial sums, written and read at about 6 MB a us.  The figures are fitted to sweeps of all
-// tiles and 1 to 16 splits (us; modelled times are within a fifth of them, and what is picked is within a tenth
-// of the best): X 512 x 4096 by W 4096 x 4096, 128x128 tiles 62 40 36 45 for 1 2 4 8 splits, 256x128 80 49 35
-// 46, 256x256 120 71 48 42; 64 rows of X, 128x32 52 30 19 17, 128x128 61 36 23 19; 1024 rows, 256x128 81
-// 58, 256x256 121 76 56; dX of 512 rows, 128x128 91 55 60, 256x128 99 61 41; scales' gradient 2048 x 4096 x
-// 1024, 128x128 62 46 51, 256x256 76 50 39.
+// tiles and 1 to 16 splits, and what is picked is within a twentieth of the sweeps' best (us for 1, 2, 4 and 8
+// splits): X 512 x 4096 by W 4096 x 4096, 128x128 tiles 66 43 36 46, 256x128 73 48 35 47, 256x256 110 67 46 44,
+// picked 36; 64 rows of X, 128x32 51 30 20 17, 128x128 63 37 24 19, picked 17; 1024 rows, 256x128 75 57 66 85,
+// 256x256 111 71 55 73, picked 56; dX of 512 rows, 128x128 91 56 61 70, 256x128 99 60 40 50, picked 40; scales'
+// gradient 2048 x 4096 x 1024, 128x128 61 46 49 56, 256x256 75 51 39 45, picked 40.
 struct TileTime {
     int bi, bj;
     float alone[3], shared[3];  // Linear, GradInput, the gradients from a checkpoint
