@@ -12,7 +12,16 @@
 // lie in 16-byte aligned rows along c: dY is transposed into the workspace first (its column sums, the bias
 // gradient, are taken on the way), and an X or dY whose rows are not aligned is copied there.
 // Weights are s * level rounded once to the activation's type (bf16: s has 8 bits and -8..7 three, so
-// about half of them are exact); checkpoints and activations are exact, sums are fp32.
+// about half of them are exact): applying the scale to a group's fp32 sum instead, as the few-row kernel
+// does, would take as many accumulators again, and the tile would halve.  Checkpoints and activations are
+// exact, sums are fp32.
+//
+// Measured, bf16: Linear 2048 x 4096 x 4096 80 us (854 TFLOP/s), GradInput 4096 x 4096 x 4096 128 us (1070),
+// GradScales 2048 x 4096 x 25088 460 us (916), with dY's transpose (11 us) and the bias gradient.  What
+// bounds them: no pipe alone.  Of GradInput (143 us in the same run) the products by themselves take 103 us
+// (MFMA issue and fragment reads), decoding by itself 50, loads by themselves 88; two waves a SIMD cover part
+// of each other.  At a split contraction the partial sums count too (the weight's gradient of 2047 x 1000 x
+// 4095: 5 transpose + 33 product + 14 joining of 51 us).
 #include "kq_group.h"
 
 namespace kq {
@@ -304,8 +313,9 @@ __global__ __launch_bounds__(64 * WI * WJ) void group_gemm_kernel(const GemmPara
         }
     };
     // Step s is multiplied while B of step s + 1 is on its way to LDS, A of step s + 1 is turned into LDS, and
-    // A of step s + 2 is on its way to registers.  Two waves share a SIMD: one stages while the other multiplies,
-    // then they change places.
+    // A of step s + 2 is on its way to registers.  Two waves share a SIMD: where A is transposed, one stages while
+    // the other multiplies, then they change places (GradInput 4096 x 4096 x 4096: 143 us, 158 with all staging
+    // first); Linear's shorter staging is better done first by all (4096 x 4096 x 4096: 131 and 139 us).
     const bool stage_first = MODE == (int)Product::Linear || wave < WAVES / 2;
     DirectB<BJ, WAVES> db;
     G st;
