@@ -16,9 +16,9 @@
 // does, would take as many accumulators again, and the tile would halve.  Checkpoints and activations are
 // exact, sums are fp32.
 //
-// Measured, bf16: Linear 2048 x 4096 x 4096 80 us (854 TFLOP/s), GradInput 4096 x 4096 x 4096 128 us (1070),
-// GradScales 2048 x 4096 x 25088 460 us (916), with dY's transpose (11 us) and the bias gradient.  What
-// bounds them: no pipe alone.  Of GradInput (143 us in the same run) the products by themselves take 103 us
+// Measured, bf16: Linear 2048 x 4096 x 4096 80 to 82 us (838 to 854 TFLOP/s), GradInput 4096 x 4096 x 4096 128 to
+// 133 us (1036 to 1070), GradScales 2048 x 4096 x 25088 460 to 462 us (911 to 916), with dY's transpose (11 us) and the bias gradient.  What
+// bounds them: no pipe alone.  Of an earlier GradInput (143 us in that run) the products by themselves take 103 us
 // (MFMA issue and fragment reads), decoding by itself 50, loads by themselves 88; two waves a SIMD cover part
 // of each other.  At a split contraction the partial sums count too (the weight's gradient of 2047 x 1000 x
 // 4095: 5 transpose + 33 product + 14 joining of 51 us).
