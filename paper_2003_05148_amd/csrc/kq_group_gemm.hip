@@ -87,8 +87,8 @@ struct StageA {
     using A_ = Act<BF>;
     using L = Levels<LUT>;
 
-    // A thread's pieces of a step.  Rows past the output's edge repeat the last one (what they give is not
-    // stored); past the contraction's edge B is zero, and so are A's scales.
+    // A thread's pieces of a step.  Rows past the output's edge repeat the last ones (what they give is not
+    // stored, or cleared before a group's sum); past the contraction's edge B is zero, and so are A's scales.
     static constexpr int kATasks = kWeightRows ? BI * 4 : BI * 2;
     static constexpr int PA = kATasks / NT;
     static_assert(kATasks % NT == 0 && PA >= 1, "A tasks");
@@ -365,6 +365,19 @@ __global__ __launch_bounds__(64 * WI * WJ) void group_gemm_kernel(const GemmPara
     }
     if constexpr (MODE == (int)Product::GradScales) {
         static_assert(BI / WI == 128, "a wave holds whole groups");
+        // A matrix may end inside a group.  Past it the accumulators hold repeated columns, or 0 * inf where dY is not
+        // finite, and the codes' level need not be zero: they are cleared.  (In a branch of the edge's workgroups:
+        // a select beside each product took 25 of 459 us at 2048 x 4096 x 25088.)
+        if (i0 + BI > p.w.k) {
+#pragma unroll
+            for (int a = 0; a < MI; ++a)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const bool past = il + 16 * a + r >= p.w.k;
+#pragma unroll
+                    for (int b = 0; b < MJ; ++b) acc[a][b][r] = past ? 0.0f : acc[a][b][r];
+                }
+        }
 #pragma unroll
         for (int b = 0; b < MJ; ++b) {
             const int n = (int)jl + 16 * b;
@@ -372,7 +385,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void group_gemm_kernel(const GemmPara
             float sum[MI / 2];  // per 32 columns
 #pragma unroll
             for (int a = 0; a < MI; ++a) {
-                // columns past the matrix repeat codes of the last tile: the checkpoint is zero there, or the group is not stored
+                // (past the last tile its codes again: their accumulators are zero)
                 const int k = il + 16 * a, kk = k & 127;
                 const unsigned d = *(const unsigned*)(p.w.codes + ((int64_t)(min(n, p.w.n - 1) >> 4) * p.w.ktiles + min(k >> 7, p.w.ktiles - 1)) * kTileBytes +
                                                       (n & 15) * 64 + ((kk >> 3) & 3) * 16 + (kk >> 5) * 4);

@@ -1,0 +1,88 @@
+"""The 4-bit fully-connected layer and the 8-bit checkpoints at the edges of their matrices and of their numbers, on
+the GPU against plain forms in 64 bits.  Tolerances and helpers are those of test_gpu_group_linear.py."""
+import pytest
+import torch
+
+from test_gpu_group_linear import BF, DEV, F32, HF, Layer, acts, check, grad_inputs, pack, table, values
+
+pytestmark = pytest.mark.gpu
+
+kq = pytest.importorskip("paper_2003_05148_amd")
+
+
+def group_sums(v, group):
+    """Sums over groups of columns."""
+    n, k = v.shape
+    G = -(-k // group)
+    return torch.zeros(n, G, dtype=torch.float64, device=v.device).index_add_(1, torch.arange(k, device=v.device) // group, v)
+
+
+# ---- groups that the matrix ends in ------------------------------------------------------------------
+
+@pytest.mark.parametrize("k", [32, 64, 93, 95, 96, 160, 192, 576, 960, 2208])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("dtype,lut", [(BF, False), (BF, True), (HF, False), (HF, True)])
+@pytest.mark.parametrize("m", [1, 200])
+def test_scale_gradient_of_a_partial_last_group(m, k, group, dtype, lut):
+    """Widths whose last group is not whole: what lies past the matrix adds nothing to it."""
+    n = 37
+    L = Layer(n, k, group, table(k) if lut else None, seed=k + group)
+    dY, q, exps, xh = grad_inputs(m, n, k, dtype)
+    ds, _ = kq.kq_checkpoint_grad_scales(dY.to(DEV), q, exps, L.packed, k, **L.kw())
+    lv = values(L.levels)[L.codes.long()]
+    d = dY.double()
+    check(ds, group_sums((d.T @ xh) * lv, group), group_sums((d.abs().T @ xh.abs()) * lv.abs(), group), F32, m + group, False, False,
+          norm=False)
+
+
+@pytest.mark.parametrize("m,n,k,group,lut", [(130, 3500, 4128, 128, True), (130, 3500, 4128, 64, False), (1111, 2100, 2144, 128, False),
+                                             (5000, 300, 544, 128, True), (5000, 300, 544, 64, False)])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_partial_last_group_in_larger_tiles_and_splits(m, n, k, group, lut, dtype):
+    """The same through the larger tile and through split contractions (the reference in 64 bits on the GPU)."""
+    L = Layer(n, k, group, table(k) if lut else None, seed=n + k)
+    dY = acts(m, n, dtype, seed=m + 1, scale=0.05).to(DEV)
+    q, exps = kq.kq_checkpoint_pack(acts(m, k, dtype, seed=m + 2).to(DEV))
+    ds, _ = kq.kq_checkpoint_grad_scales(dY, q, exps, L.packed, k, **L.kw())
+    xh, d = kq.kq_checkpoint_restore(q, exps, k).double(), dY.double()
+    lv = values(L.levels).to(DEV)[L.codes.long().to(DEV)]
+    want, S = (d.T.contiguous() @ xh) * lv, (d.abs().T.contiguous() @ xh.abs()) * lv.abs()
+    check(ds, group_sums(want, group).cpu(), group_sums(S, group).cpu(), F32, m + group, False, False, norm=False)
+
+
+@pytest.mark.parametrize("k,group", [(96, 64), (160, 128), (95, 128)])
+def test_partial_last_group_against_differences(k, group):
+    """The loss is linear in the scales: its central difference is the last group's gradient."""
+    m, n = 40, 9
+    L = Layer(n, k, group, table(k), seed=k)
+    dY, q, exps, xh = grad_inputs(m, n, k, BF)
+    ds, _ = kq.kq_checkpoint_grad_scales(dY.to(DEV), q, exps, L.packed, k, **L.kw())
+    lv = values(L.levels)[L.codes.long()]
+    which = torch.arange(k) // group
+
+    def loss(s):
+        return float((dY.double() * (xh @ (lv * s[:, which]).T)).sum())
+
+    s0 = L.scales.double()
+    S = group_sums((dY.double().abs().T @ xh.abs()) * lv.abs(), group)
+    for r in range(n):
+        h = torch.zeros_like(s0)
+        h[r, -1] = 2.0 ** -6
+        num = (loss(s0 + h) - loss(s0 - h)) / 2.0 ** -5
+        assert abs(num - float(ds[r, -1])) <= (m + group + 16) * 2.0 ** -24 * float(S[r, -1]) + 1e-7
+
+
+@pytest.mark.parametrize("k", [40, 64, 70])
+@pytest.mark.parametrize("lut", [False, True])
+def test_infinite_gradient_of_a_partial_last_group(k, lut):
+    """Every term of the last group is positive, one infinite: so is its sum, whatever lies past the matrix."""
+    m, n, group = 3, 20, 128
+    L = Layer(n, k, group, torch.arange(-8, 8).to(BF) if lut else None, seed=k)
+    L.packed = pack(torch.full((n, k), 12, dtype=torch.uint8)).to(DEV)      # level 4
+    q, exps = kq.kq_checkpoint_pack(torch.ones(m, k, dtype=BF, device=DEV))
+    dY = torch.ones(m, n, dtype=BF, device=DEV)
+    dY[1, 7] = float("inf")
+    ds, _ = kq.kq_checkpoint_grad_scales(dY, q, exps, L.packed, k, **L.kw())
+    want = torch.full((n, 1), 4.0 * m * k, device=DEV)
+    want[7] = float("inf")
+    assert torch.equal(ds, want)
