@@ -543,6 +543,13 @@ static bool rows_are_aligned(const void* B, int64_t ldb, int64_t C) {
     return ((uintptr_t)B & 15) == 0 && (ldb & 7) == 0 && (C & 7) == 0 && ldb < (int64_t(1) << 22);
 }
 
+// DirectB's 32-bit byte offsets reach the last chunk of bj rows (a staged operand's pitch is the contraction
+// itself, up to KQ_GROUP_MAX_FEATURES: 256 rows reach to 8.42 million columns, 128 rows to all).
+static bool row_offsets_fit(int bj, int64_t pitch) {
+    return (int64_t)(bj - 1) * 2 * pitch + 2 * kStep <= int64_t(UINT32_MAX);
+}
+static_assert(127 * 2 * (int64_t)KQ_GROUP_MAX_FEATURES + 2 * kStep <= int64_t(UINT32_MAX), "every pitch has a tile");
+
 // The tile and the splits with the shortest modelled time.  A workgroup's step takes `alone` us while it has a CU
 // to itself, and a CU with n workgroups at hand takes n times `shared`; a split contraction pays the joining
 // launch and its partial sums, written and read at about 6 MB a us.  The figures are fitted to sweeps of all
@@ -569,10 +576,13 @@ GemmPlan gemm_plan(Product mode, const void* B, int64_t ldb, int64_t I, int64_t 
     const bool rows = mode == Product::Linear || mode == Product::GradInput;
     const int column = mode == Product::Linear ? 0 : mode == Product::GradInput ? 1 : 2;
     const float value_us = (mode == Product::GradScales ? (float)J * groups : (float)I * J) * 8.0f / 6e6f;
+    g.stage_b = !rows || !rows_are_aligned(B, ldb, C);
+    g.pitch = ceil_div64(C, kStep) * kStep;
     float best = 0.0f;
     int64_t splits = 1;
     for (const TileTime& t : kTiles) {
         if (t.alone[column] == 0.0f) continue;
+        if (!row_offsets_fit(t.bj, g.stage_b ? g.pitch : ldb)) continue;  // (of 128 rows and fewer all do)
         const int64_t tiles = ceil_div64(I, t.bi) * ceil_div64(J, t.bj);
         for (int s = 1; s <= 32 && (s == 1 || (s * 2 <= steps && s * tiles <= 1024)); s = s < 4 ? s + 1 : s * 3 / 2) {  // 1 2 3 4 6 9 13 ..
             const float n = (float)ceil_div64(tiles * s, 256), step = n * t.shared[column] > t.alone[column] ? n * t.shared[column] : t.alone[column];
@@ -591,8 +601,6 @@ GemmPlan gemm_plan(Product mode, const void* B, int64_t ldb, int64_t I, int64_t 
     const int64_t values = mode == Product::GradScales ? J * groups : I * J;
     auto region = [](size_t bytes) { return (bytes + 255) & ~size_t(255); };
     g.part_bytes = g.splits > 1 ? region((size_t)g.splits * (size_t)values * sizeof(float)) : 0;
-    g.stage_b = !rows || !rows_are_aligned(B, ldb, C);
-    g.pitch = ceil_div64(C, kStep) * kStep;
     g.b_bytes = g.stage_b ? region((size_t)J * (size_t)g.pitch * 2) : 0;
     g.bias_parts = rows ? 0 : (int)ceil_div64(C, 256);
     g.ws_bytes = g.part_bytes + g.b_bytes + (rows ? 0 : region((size_t)g.bias_parts * (size_t)J * sizeof(float)));
