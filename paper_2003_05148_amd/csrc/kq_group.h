@@ -35,6 +35,11 @@ using u32x2 = __attribute__((ext_vector_type(2))) unsigned;
 
 __device__ __forceinline__ float bf16_bits_to_f32(unsigned h) { return __builtin_bit_cast(float, h << 16); }
 
+// A checkpoint group's step from its exponent; 0 gives 0, and 255 NaN.
+__device__ __forceinline__ float checkpoint_step(unsigned e) {
+    return __builtin_bit_cast(float, e == 255u ? 0x7fc00000u : e << 23);
+}
+
 // The two 16-bit activation types.
 template <bool BF>
 struct Act {

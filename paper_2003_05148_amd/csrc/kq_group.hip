@@ -287,10 +287,6 @@ __global__ __launch_bounds__(256) void checkpoint_pack_kernel(const CheckpointPa
     if ((threadIdx.x & 3) == 0) p.exps[row * (p.kq >> 5) + (c0 >> 5)] = (uint8_t)(bad ? 255 : e);
 }
 
-__device__ __forceinline__ float checkpoint_step(unsigned e) {
-    return __builtin_bit_cast(float, e == 255u ? 0x7fc00000u : e << 23);
-}
-
 template <int TYPE>
 __global__ __launch_bounds__(256) void checkpoint_restore_kernel(const CheckpointParams p) {
     const int per_row = p.kq >> 3;

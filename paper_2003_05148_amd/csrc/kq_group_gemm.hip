@@ -199,10 +199,9 @@ struct StageA {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const unsigned ex = 2 * e + h < left ? x[t][2 * e + h] : 0;
-                        const float s = __builtin_bit_cast(float, ex << 23);  // 255: infinity, and inf - inf below
-                        const unsigned u = w[t][2 * e + h] ^ 0x80808080u;  // q + 128
+                        const float s = checkpoint_step(ex);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) v[h][j] = __builtin_fmaf((float)((u >> (8 * j)) & 255u), s, -128.0f * s);
+                        for (int j = 0; j < 4; ++j) v[h][j] = (float)((int)(w[t][2 * e + h] << (24 - 8 * j)) >> 24) * s;
                     }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) out[j][e] = A_::pack_exact(v[0][j], v[1][j]);

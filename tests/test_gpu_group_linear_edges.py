@@ -86,3 +86,24 @@ def test_infinite_gradient_of_a_partial_last_group(k, lut):
     want = torch.full((n, 1), 4.0 * m * k, device=DEV)
     want[7] = float("inf")
     assert torch.equal(ds, want)
+
+
+# ---- the largest numbers -----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("m,n,k", [(3, 20, 40), (130, 40, 257), (1000, 2049, 1026)])
+@pytest.mark.parametrize("lut", [False, True])
+def test_gradients_from_the_largest_checkpoints(m, n, k, lut):
+    """Values up to bf16's largest number (steps of 2^121): finite gradients of finite values."""
+    X = 0.2 * acts(m, k, BF, seed=m + k).clamp(-5, 5) * 3.3e38
+    X[:, ::7] = 3.3895314e38
+    q, exps = kq.kq_checkpoint_pack(X.to(DEV))
+    assert int(exps.max()) == 121 + 127
+    dY = acts(m, n, BF, seed=m + n, scale=1e-36)
+    L = Layer(n, k, 64, table(k) if lut else None, seed=n)
+    xh, d = kq.kq_checkpoint_restore(q, exps, k).double(), dY.to(DEV).double()
+    want, S = d.T.contiguous() @ xh, d.abs().T.contiguous() @ xh.abs()
+    dW, _ = kq.kq_checkpoint_grad_weight(dY.to(DEV), q, exps, k)
+    check(dW, want.cpu(), S.cpu(), F32, m, False, False)
+    ds, _ = kq.kq_checkpoint_grad_scales(dY.to(DEV), q, exps, L.packed, k, **L.kw())
+    lv = values(L.levels).to(DEV)[L.codes.long().to(DEV)]
+    check(ds, group_sums(want * lv, 64).cpu(), group_sums(S * lv.abs(), 64).cpu(), F32, m + 64, False, False, norm=False)
