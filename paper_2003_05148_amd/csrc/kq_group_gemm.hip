@@ -40,17 +40,19 @@ __device__ __forceinline__ void write_lds(u32x4* at, u32x4 v) {
     asm volatile("ds_write_b128 %0, %1" ::"v"((unsigned)(uintptr_t)(__attribute__((address_space(3))) u32x4*)at), "v"(v) : "memory");
 }
 
-// The bytes of four codes, 0..15 each, as fp32 s * level.
+// Four codes as fp32 s * level (scaled: the even or the odd nibbles of w) or as levels (plain: the bytes of b, 0..15).
 template <bool LUT>
 struct Levels;
 template <>
 struct Levels<false> {
     __device__ __forceinline__ void init(const uint16_t*) {}
-    // levels -8 .. 7: s * (q - 8) = fma(q, s, -8 s), exact
-    static __device__ __forceinline__ void scaled(const Levels&, unsigned b, const float (&s)[4], float (&v)[4]) {
-        asm("" : "+v"(b));  // (unknown bytes: a byte conversion each, with no extraction before it)
+    // levels -8 .. 7: a nibble with its top bit turned, in the upper half of a byte, is 16 (q - 8) as a signed byte.
+    // (fma(q, s, -8 s) would overflow for scales from 2^125 on, of which the largest weights have some.)
+    template <int ODD>
+    static __device__ __forceinline__ void scaled(const Levels&, unsigned w, const float (&s)[4], float (&v)[4]) {
+        const unsigned b = ((ODD ? w : w << 4) & 0xf0f0f0f0u) ^ 0x80808080u;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = __builtin_fmaf((float)((b >> (8 * j)) & 255u), s[j], -8.0f * s[j]);
+        for (int j = 0; j < 4; ++j) v[j] = (float)((int)(b << (24 - 8 * j)) >> 24) * (0.0625f * s[j]);
     }
     static __device__ __forceinline__ void plain(const Levels&, unsigned b, float (&v)[4]) {
 #pragma unroll
@@ -70,8 +72,9 @@ struct Levels<true> {
         v[2] = __builtin_bit_cast(float, __builtin_amdgcn_perm(hi, lo, 0x06020c0cu));
         v[3] = __builtin_bit_cast(float, __builtin_amdgcn_perm(hi, lo, 0x07030c0cu));
     }
-    static __device__ __forceinline__ void scaled(const Levels& l, unsigned b, const float (&s)[4], float (&v)[4]) {
-        plain(l, b, v);
+    template <int ODD>
+    static __device__ __forceinline__ void scaled(const Levels& l, unsigned w, const float (&s)[4], float (&v)[4]) {
+        plain(l, (ODD ? w >> 4 : w) & 0x0f0f0f0fu, v);
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] *= s[j];
     }
@@ -167,8 +170,8 @@ struct StageA {
                     const float s1 = bf16_bits_to_f32(x[t][h]);
                     const float s[4] = {s1, s1, s1, s1};
                     float e[4], o[4];  // nibbles 0 2 4 6 are columns 0 4 1 5, nibbles 1 3 5 7 columns 2 6 3 7
-                    L::scaled(lv, w[t][h] & 0x0f0f0f0fu, s, e);
-                    L::scaled(lv, (w[t][h] >> 4) & 0x0f0f0f0fu, s, o);
+                    L::template scaled<0>(lv, w[t][h], s, e);
+                    L::template scaled<1>(lv, w[t][h], s, o);
                     write_lds(lds + lds_chunk(r, 4 * h + q), u32x4{A_::pack(e[0], e[2]), A_::pack(o[0], o[2]), A_::pack(e[1], e[3]), A_::pack(o[1], o[3])});
                 }
             } else if constexpr (kWeightCols) {
@@ -181,8 +184,8 @@ struct StageA {
                     const float s0 = bf16_bits_to_f32(2 * e < left ? x[t][2 * e] : 0), s1 = bf16_bits_to_f32(2 * e + 1 < left ? x[t][2 * e + 1] : 0);
                     const float s[4] = {s0, s0, s1, s1};
                     float ev[4], od[4];  // columns 0, 2 of both rows; columns 1, 3
-                    L::scaled(lv, pairw & 0x0f0f0f0fu, s, ev);
-                    L::scaled(lv, (pairw >> 4) & 0x0f0f0f0fu, s, od);
+                    L::template scaled<0>(lv, pairw, s, ev);
+                    L::template scaled<1>(lv, pairw, s, od);
                     out[0][e] = A_::pack(ev[0], ev[2]);
                     out[1][e] = A_::pack(od[0], od[2]);
                     out[2][e] = A_::pack(ev[1], ev[3]);

@@ -107,3 +107,28 @@ def test_gradients_from_the_largest_checkpoints(m, n, k, lut):
     ds, _ = kq.kq_checkpoint_grad_scales(dY.to(DEV), q, exps, L.packed, k, **L.kw())
     lv = values(L.levels).to(DEV)[L.codes.long().to(DEV)]
     check(ds, group_sums(want * lv, 64).cpu(), group_sums(S * lv.abs(), 64).cpu(), F32, m + 64, False, False, norm=False)
+
+
+def of_scale(n, k, group, levels, scale, seed):
+    """A layer with one scale, whose codes are 1 .. 15: the lowest level stands past the matrix alone."""
+    L = Layer(n, k, group, levels, seed=seed)
+    L.codes.clamp_(min=1)
+    L.packed = pack(L.codes).to(DEV)
+    L.scales.fill_(scale)
+    L.dscales = L.scales.to(DEV)
+    return L
+
+
+@pytest.mark.parametrize("m", [1, 16, 17, 64, 300])
+def test_products_with_the_largest_scales(m):
+    """Scales of 2^125 and more, as weights near bf16's largest number have: 7 of them is still finite."""
+    n, k = 192, 256
+    for scale in (2.0 ** 125, 2.0 ** 125 * (1 + 17 / 128)):
+        L = of_scale(n, k, 128, None, scale, seed=m)
+        X, dY = acts(m, k, BF, seed=m, scale=1e-30), acts(m, n, BF, seed=m + 1, scale=1e-30)
+        W = L.W
+        assert float(W.abs().max()) <= 3.3895314e38
+        Y = kq.kq_group_linear(X.to(DEV), L.packed, L.dscales, **L.kw())
+        check(Y, X.double() @ W.T, X.double().abs() @ W.abs().T, BF, k, m > 16, True)
+        dX = kq.kq_group_linear_grad_input(dY.to(DEV), L.packed, L.dscales, k, **L.kw())
+        check(dX, dY.double() @ W, dY.double().abs() @ W.abs(), BF, n, True, False)
