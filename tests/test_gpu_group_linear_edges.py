@@ -132,3 +132,17 @@ def test_products_with_the_largest_scales(m):
         check(Y, X.double() @ W.T, X.double().abs() @ W.abs().T, BF, k, m > 16, True)
         dX = kq.kq_group_linear_grad_input(dY.to(DEV), L.packed, L.dscales, k, **L.kw())
         check(dX, dY.double() @ W, dY.double().abs() @ W.abs(), BF, n, True, False)
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 40, 70), (17, 40, 70), (64, 33, 1000), (300, 515, 1030), (2048, 2100, 300)])
+@pytest.mark.parametrize("dtype,lut", [(HF, False), (HF, True), (BF, False), (BF, True)])
+def test_weights_past_the_matrix_may_overflow(m, n, k, dtype, lut):
+    """Scales at which the lowest level, that of the codes past the matrix, is beyond the activations' type, and no
+    level that the matrix has."""
+    levels = torch.tensor([-2.0] + [-0.9 + 0.12 * i for i in range(15)]).to(BF) if lut else None
+    scale = {(HF, False): 2.0 ** 13, (HF, True): 2.0 ** 15 * 1.5, (BF, False): 2.0 ** 125, (BF, True): 2.0 ** 127}[dtype, lut]
+    L = of_scale(n, k, 32, levels, scale, seed=k)
+    X = acts(m, k, dtype, seed=m, scale=1e-3 if dtype == HF else 1e-30)
+    Y = kq.kq_group_linear(X.to(DEV), L.packed, L.dscales, **L.kw())
+    W = L.W
+    check(Y, X.double() @ W.T, X.double().abs() @ W.abs().T, dtype, k, m > 16, not lut, xsum=X.double().abs().sum(1, keepdim=True))
