@@ -613,8 +613,9 @@ kq_status kq_fit_layer_noalloc(const float* X, int64_t n, int32_t dim, int32_t k
  * kq_reconstruct_groups -- W_hat in any KQ_T_* type, fp32 products rounded once.
  * kq_group_linear -- Y[m][n] = X[m][k] W_hat^T + bias (fp32 [n], or NULL).  Sums in fp32.  For up to 16
  *   rows of X the levels multiply X exactly and a group's fp32 sum takes the scale; beyond, the weights
- *   are rounded to the type of X first.  An infinity in X makes its row of Y infinite or NaN, as do
- *   values of 2^122 and more.  A row of Y depends on its row of X and on m alone, not on other rows.
+ *   are rounded to the type of X first.  An infinity in X makes its row of Y infinite or NaN, as may a
+ *   group of X whose magnitudes add up to 2^127 or more.  A row of Y depends on its row of X and on m
+ *   alone, not on other rows.
  * kq_group_linear_grad_input -- dX[m][k] = dY[m][n] W_hat, the weights rounded to the type of dY.
  *   workspaces: the *_workspace_bytes of the same arguments (may be 0: ws may be NULL then).  Above 16 rows,
  *   an X or dY that is not 16-byte aligned, or whose columns or pitch are not multiples of 8, is copied there.

@@ -3,10 +3,12 @@
 //
 // A wave multiplies 16 rows of W by 16 rows of X, 128 columns at a time: 16 bytes of codes a lane are one
 // contiguous kilobyte and four operands of the 16 x 16 x 32 matrix instruction, so the codes go from memory
-// to the matrix cores through registers alone.  A code q becomes 16 + q in one shift and one masked OR a pair
-// (the four bits are the top of the mantissa of 16); a product of X with the constant -24 starts the
-// accumulator, and so the sum is that of x (q - 8).  Tables of levels are looked up with byte permutes.
-// Every product is exact; a group's fp32 sum takes the group's scale in fp32.
+// to the matrix cores through registers alone.  A code q becomes 1 + q / 16 in one shift and one masked OR a pair
+// (the four bits are the top of the mantissa of 1); a product of X with the constant -1.5 is added, and so the sum
+// is that of x (q - 8) / 16.  (Products and sums stay below 2 |x|: with 16 + q and -24 they overflowed for finite X.)
+// Its fp32 rounding is that of terms of up to 31 |x| where the direct sum's are of up to 8 |x|.  Tables of levels
+// are looked up with byte permutes.  Every product is exact (fp16 takes table levels below 2^-14 rounded to its
+// subnormals' 2^-24); a group's fp32 sum takes the group's scale in fp32, and the row's sum the factor 16 at the end.
 // The waves of a workgroup take the 128-column blocks of its rows in turn and add their sums through LDS in
 // order.  Where there are few rows of W the columns are also split over workgroups, joined by a second kernel.
 //
@@ -21,7 +23,7 @@ namespace kq {
 
 // ---- codes to 16-bit values -------------------------------------------------------------------------------
 
-// the 8 columns of a dword of codes, in order: levels, or 16 + q without a table
+// the 8 columns of a dword of codes, in order: levels, or 1 + q / 16 without a table
 template <bool BF, bool LUT>
 __device__ __forceinline__ u32x4 decode(unsigned d, const LevelTable& t) {
     u32x4 o;
@@ -35,15 +37,15 @@ __device__ __forceinline__ u32x4 decode(unsigned d, const LevelTable& t) {
             o[2 + h] = __builtin_amdgcn_perm(hi, lo, 0x07030501u);
         }
     } else if constexpr (BF) {
-        o[0] = ((d << 3) & 0x00780078u) | 0x41804180u;
-        o[1] = ((d >> 1) & 0x00780078u) | 0x41804180u;
-        o[2] = ((d >> 5) & 0x00780078u) | 0x41804180u;
-        o[3] = ((d >> 9) & 0x00780078u) | 0x41804180u;
+        o[0] = ((d << 3) & 0x00780078u) | 0x3f803f80u;
+        o[1] = ((d >> 1) & 0x00780078u) | 0x3f803f80u;
+        o[2] = ((d >> 5) & 0x00780078u) | 0x3f803f80u;
+        o[3] = ((d >> 9) & 0x00780078u) | 0x3f803f80u;
     } else {
-        o[0] = ((d << 6) & 0x03c003c0u) | 0x4c004c00u;
-        o[1] = ((d << 2) & 0x03c003c0u) | 0x4c004c00u;
-        o[2] = ((d >> 2) & 0x03c003c0u) | 0x4c004c00u;
-        o[3] = ((d >> 6) & 0x03c003c0u) | 0x4c004c00u;
+        o[0] = ((d << 6) & 0x03c003c0u) | 0x3c003c00u;
+        o[1] = ((d << 2) & 0x03c003c0u) | 0x3c003c00u;
+        o[2] = ((d >> 2) & 0x03c003c0u) | 0x3c003c00u;
+        o[3] = ((d >> 6) & 0x03c003c0u) | 0x3c003c00u;
     }
     return o;
 }
@@ -89,7 +91,7 @@ __global__ __launch_bounds__(64 * WAVES) void group_matvec_kernel(const MatvecPa
     const unsigned code_off = r16 * 64 + q * 16;
     const uint16_t* xrow = (const uint16_t*)p.X + (int64_t)min(r16, p.m - 1) * p.ldx;
 
-    const unsigned offset_bits = BF ? 0xc1c0c1c0u : 0xce00ce00u;  // a pair of -24
+    const unsigned offset_bits = BF ? 0xbfc0bfc0u : 0xbe00be00u;  // a pair of -1.5
     const u32x4 offset = {offset_bits, offset_bits, offset_bits, offset_bits};
     LevelTable table;
     f32x4 y[RT];
@@ -164,7 +166,7 @@ __global__ __launch_bounds__(64 * WAVES) void group_matvec_kernel(const MatvecPa
     if constexpr (XLDS) __syncthreads();
     f32x4* s_sum = (f32x4*)s_buf;
 #pragma unroll
-    for (int t = 0; t < RT; ++t) s_sum[(t * WAVES + wave) * 64 + lane] = y[t];
+    for (int t = 0; t < RT; ++t) s_sum[(t * WAVES + wave) * 64 + lane] = LUT ? y[t] : y[t] * 16.0f;
     __syncthreads();
     if (wave < RT) {
         f32x4 v = s_sum[wave * WAVES * 64 + lane];

@@ -146,3 +146,18 @@ def test_weights_past_the_matrix_may_overflow(m, n, k, dtype, lut):
     Y = kq.kq_group_linear(X.to(DEV), L.packed, L.dscales, **L.kw())
     W = L.W
     check(Y, X.double() @ W.T, X.double().abs() @ W.abs().T, dtype, k, m > 16, not lut, xsum=X.double().abs().sum(1, keepdim=True))
+
+
+@pytest.mark.parametrize("m", [1, 4, 5, 16, 17])
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("size", [2.0 ** 122, 2.0 ** 124])
+def test_linear_of_large_activations(m, group, size):
+    """One value in a group near bf16's largest number, the others ordinary: the level's product is taken off nothing
+    that overflows."""
+    n, k = 70, 300
+    L = Layer(n, k, group, None, seed=m, scale=2.0 ** -100)
+    X = acts(m, k, BF, seed=m)
+    X[:, 5::group] = size
+    X[m // 2] *= -1
+    Y = kq.kq_group_linear(X.to(DEV), L.packed, L.dscales, **L.kw())
+    check(Y, X.double() @ L.W.T, X.double().abs() @ L.W.abs().T, BF, k, m > 16, True)
