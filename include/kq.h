@@ -657,7 +657,8 @@ kq_status kq_group_linear_grad_input(const void* dY, int32_t type, int64_t ldy, 
  * kq_checkpoint_grad_scales -- dscales[o][g] = sum over the group's columns of L[code] dW, fp32
  *   [n][ceil(k / group)]; dW is never written.
  *   dbias (fp32 [n], or NULL): sum_m dY[m][o].  dY bf16 or fp16; an fp16 dY needs a checkpoint
- *   whose values fp16 can hold.  Sums in fp32, in an order that the sizes alone decide.
+ *   whose values fp16 can hold (of larger ones infinities are taken, smaller ones are rounded).
+ *   Sums in fp32, in an order that the sizes alone decide.
  *   workspace: kq_checkpoint_grad_workspace_bytes(m, n, k, group), group 0 for the weight's; it holds dY
  *   transposed, and the partial sums of a split contraction.
  */

@@ -55,12 +55,12 @@ struct Act {
         if constexpr (BF) return __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2));
         else return __builtin_bit_cast(unsigned, __builtin_convertvector(v, f16x2));
     }
-    // the same for values that the type holds exactly
-    static __device__ __forceinline__ unsigned pack_exact(float lo, float hi) {
+    // the same for values that bf16 holds exactly (to fp16 they are rounded, beyond its range to infinity)
+    static __device__ __forceinline__ unsigned pack_bf16_value(float lo, float hi) {
         if constexpr (BF)
             return __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, hi), __builtin_bit_cast(unsigned, lo), 0x07060302u);
         else
-            return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_pkrtz(lo, hi));
+            return pack(lo, hi);
     }
     static __device__ __forceinline__ float lo(unsigned v) {
         if constexpr (BF) return __builtin_bit_cast(float, v << 16);

@@ -220,7 +220,7 @@ struct StageA {
                         for (int j = 0; j < 4; ++j) v[h][j] = (float)((int)(w[t][2 * e + h] << (24 - 8 * j)) >> 24) * s;
                     }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) out[j][e] = A_::pack_exact(v[0][j], v[1][j]);
+                    for (int j = 0; j < 4; ++j) out[j][e] = A_::pack_bf16_value(v[0][j], v[1][j]);
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) write_lds(lds + lds_chunk(4 * quad + j, oct), out[j]);

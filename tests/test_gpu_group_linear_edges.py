@@ -161,3 +161,19 @@ def test_linear_of_large_activations(m, group, size):
     X[m // 2] *= -1
     Y = kq.kq_group_linear(X.to(DEV), L.packed, L.dscales, **L.kw())
     check(Y, X.double() @ L.W.T, X.double().abs() @ L.W.abs().T, BF, k, m > 16, True)
+
+
+@pytest.mark.parametrize("m", [1, 90])
+def test_checkpoint_beyond_the_gradients_type_is_not_clipped(m):
+    """An fp16 dY with a checkpoint of larger values: infinities or NaN, not the gradient of other values."""
+    n, k = 20, 64
+    X = torch.ones(m, k, dtype=BF)
+    X[m // 2, 32:] = 1e5
+    q, exps = kq.kq_checkpoint_pack(X.to(DEV))
+    dY = torch.ones(m, n, dtype=HF, device=DEV)
+    dW, _ = kq.kq_checkpoint_grad_weight(dY, q, exps, k)
+    assert torch.all(dW[:, :32] == m) and not torch.isfinite(dW[:, 32:]).any()
+    L = Layer(n, k, 32, None, seed=1)
+    L.packed = pack(torch.full((n, k), 9, dtype=torch.uint8)).to(DEV)       # level 1
+    ds, _ = kq.kq_checkpoint_grad_scales(dY, q, exps, L.packed, k, **L.kw())
+    assert torch.all(ds[:, 0] == 32 * m) and not torch.isfinite(ds[:, 1]).any()
