@@ -593,7 +593,7 @@ kq_status kq_fit_layer_noalloc(const float* X, int64_t n, int32_t dim, int32_t k
  *   scales device [n][ceil(k / group)] bf16; group 32, 64 or 128 (else KQ_ERR_UNSUPPORTED).
  *   L: levels == NULL for the integers -8 .. 7, or a device table of 16 bf16 levels in
  *   ascending order (for instance those kq_quantize_scalars finds with 4 bits), finite, one of
- *   them not zero.  Levels have to lie in fp16's range where the activations are fp16.
+ *   them not zero.
  *   codes: kq_group_code_bytes(n, k) bytes, 16-byte aligned: tiles of 16 rows by 128 columns of
  *   1 KB, [ceil(n / 16)][ceil(k / 128)][16][64].  In a row's 64 bytes, dword 4 q + i (little
  *   endian) holds columns 32 i + 8 q + 0 .. 7, column j of them in bits 4 b .. 4 b + 3 with
@@ -612,8 +612,9 @@ kq_status kq_fit_layer_noalloc(const float* X, int64_t n, int32_t dim, int32_t k
  *   A group with an infinity or NaN gets a NaN scale: all of it reconstructs to NaN.
  * kq_reconstruct_groups -- W_hat in any KQ_T_* type, fp32 products rounded once.
  * kq_group_linear -- Y[m][n] = X[m][k] W_hat^T + bias (fp32 [n], or NULL).  Sums in fp32.  For up to 16
- *   rows of X the levels multiply X exactly and a group's fp32 sum takes the scale; beyond, the weights
- *   are rounded to the type of X first.  An infinity in X makes its row of Y infinite or NaN, as may a
+ *   rows of X the levels multiply X exactly (fp16: those above 2^-31 of the largest, smaller ones are off by
+ *   at most 2^-39 of it) and a group's fp32 sum takes the scale; beyond, the weights are rounded to the type
+ *   of X first.  An infinity in X makes its row of Y infinite or NaN, as may a
  *   group of X whose magnitudes add up to 2^127 or more.  A row of Y depends on its row of X and on m
  *   alone, not on other rows.
  * kq_group_linear_grad_input -- dX[m][k] = dY[m][n] W_hat, the weights rounded to the type of dY.

@@ -74,22 +74,33 @@ struct Act {
 };
 
 // 16 levels as two byte tables of 16 entries in registers; a look-up is four byte permutes.
+// In fp16 they are levels 2^shift, with the largest in [2^14, 2^15): every bf16 level down to 2^-31 of it is exact
+// and what lies below is off by at most 2^-39 of it (fp16's subnormals), whatever the table's own range is.
 struct LevelTable {
     unsigned lo[4], hi[4];  // low and high bytes of the 16-bit levels, four a register
+    int shift;
 };
 
 template <bool BF>
 __device__ __forceinline__ LevelTable load_levels(const uint16_t* levels) {
     LevelTable t;
+    t.shift = 0;
+    if constexpr (!BF) {
+        unsigned top = 1u << 7;  // (at least the smallest normal number)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) top = max(top, (unsigned)levels[j] & 0x7fffu);
+        t.shift = 14 + 127 - (int)(top >> 7);
+    }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         unsigned a, b;  // levels 4 r .. 4 r + 3 in two registers
         if constexpr (BF) {
             a = (unsigned)levels[4 * r] | (unsigned)levels[4 * r + 1] << 16;
             b = (unsigned)levels[4 * r + 2] | (unsigned)levels[4 * r + 3] << 16;
-        } else {  // fp16 holds a bf16 level exactly from 2^-14 on, and to 2^-25 below
-            a = Act<false>::pack(bf16_bits_to_f32(levels[4 * r]), bf16_bits_to_f32(levels[4 * r + 1]));
-            b = Act<false>::pack(bf16_bits_to_f32(levels[4 * r + 2]), bf16_bits_to_f32(levels[4 * r + 3]));
+        } else {
+            auto level = [&](int j) { return __builtin_ldexpf(bf16_bits_to_f32(levels[j]), t.shift); };
+            a = Act<false>::pack(level(4 * r), level(4 * r + 1));
+            b = Act<false>::pack(level(4 * r + 2), level(4 * r + 3));
         }
         t.lo[r] = __builtin_amdgcn_perm(b, a, 0x06040200u);
         t.hi[r] = __builtin_amdgcn_perm(b, a, 0x07050301u);

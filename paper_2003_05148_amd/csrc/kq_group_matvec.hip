@@ -7,8 +7,9 @@
 // (the four bits are the top of the mantissa of 1); a product of X with the constant -1.5 is added, and so the sum
 // is that of x (q - 8) / 16.  (Products and sums stay below 2 |x|: with 16 + q and -24 they overflowed for finite X.)
 // Its fp32 rounding is that of terms of up to 31 |x| where the direct sum's are of up to 8 |x|.  Tables of levels
-// are looked up with byte permutes.  Every product is exact (fp16 takes table levels below 2^-14 rounded to its
-// subnormals' 2^-24); a group's fp32 sum takes the group's scale in fp32, and the row's sum the factor 16 at the end.
+// are looked up with byte permutes.  Every product is exact (in fp16 a table's levels are brought into its range by a
+// power of two, which the scales take off); a group's fp32 sum takes the group's scale in fp32, and without a table
+// the row's sum the factor 16 at the end.
 // The waves of a workgroup take the 128-column blocks of its rows in turn and add their sums through LDS in
 // order.  Where there are few rows of W the columns are also split over workgroups, joined by a second kernel.
 //
@@ -153,7 +154,8 @@ __global__ __launch_bounds__(64 * WAVES) void group_matvec_kernel(const MatvecPa
                     acc[t] = Act<BF>::mfma(x, w, acc[t]);
                     if ((i + 1) % kPieces == 0) {  // the group's last piece
                         if constexpr (!LUT) acc[t] += base;
-                        const float s = bf16_bits_to_f32(cur.s[t][i / kPieces]);
+                        float s = bf16_bits_to_f32(cur.s[t][i / kPieces]);
+                        if constexpr (LUT && !BF) s = __builtin_ldexpf(s, -table.shift);
 #pragma unroll
                         for (int r = 0; r < 4; ++r) y[t][r] = __builtin_fmaf(s, acc[t][r], y[t][r]);
                     }

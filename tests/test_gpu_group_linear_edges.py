@@ -177,3 +177,16 @@ def test_checkpoint_beyond_the_gradients_type_is_not_clipped(m):
     L.packed = pack(torch.full((n, k), 9, dtype=torch.uint8)).to(DEV)       # level 1
     ds, _ = kq.kq_checkpoint_grad_scales(dY, q, exps, L.packed, k, **L.kw())
     assert torch.all(ds[:, 0] == 32 * m) and not torch.isfinite(ds[:, 1]).any()
+
+
+@pytest.mark.parametrize("m", [1, 4, 5, 16, 17])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("size", [2.0 ** -120, 2.0 ** -20, 2.0 ** 20, 2.0 ** 110])
+def test_level_tables_outside_of_fp16(m, group, size):
+    """fp16 activations and levels that fp16 does not hold, with scales that bring the weights into its range."""
+    n, k = 70, 300
+    levels = (table(m).double() * size).to(BF)
+    L = Layer(n, k, group, levels, seed=m, scale=0.02 / size)
+    X = acts(m, k, HF, seed=m + 1)
+    Y = kq.kq_group_linear(X.to(DEV), L.packed, L.dscales, **L.kw())
+    check(Y, X.double() @ L.W.T, X.double().abs() @ L.W.abs().T, HF, k, m > 16, False, xsum=X.double().abs().sum(1, keepdim=True))
