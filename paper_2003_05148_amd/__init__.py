@@ -1214,7 +1214,8 @@ class GroupLinear:
     ``layer(X)`` is the serving call.  ``layer.forward(X)`` also returns the 8-bit checkpoint of X that
     ``layer.backward(dY, checkpoint)`` takes the gradients of the scales and of the bias from; ``layer.step``
     moves both against them, as Eq. (2) moves a codebook's entries: a shared value follows the gradients of what
-    it stands for, and the codes stay."""
+    it stands for, and the codes stay.  Not an autograd function: an X that requires a gradient gets it from
+    ``layer.backward``.  X and dY are bf16 or fp16."""
 
     def __init__(self, W, group: int = 128, levels=None, bias=None):
         self.group, self.levels = int(group), levels

@@ -114,7 +114,7 @@ __device__ __forceinline__ unsigned nearest_level_code(float t, const float* mid
     return code;
 }
 
-// Measured: 4096 x 25088 fp32 weights 87 to 99 us (463 MB, 4.7 to 5.3 TB/s: memory), 1000 x 1023 bf16 with a table
+// Measured: 4096 x 25088 fp32 weights 86 to 99 us (463 MB, 4.7 to 5.4 TB/s: memory), 1000 x 1023 bf16 with a table
 // 5.5 us (latency of one round of loads, a division and the table's search).
 template <int TYPE, bool LUT>
 __global__ __launch_bounds__(256) void quantize_groups_kernel(const QuantizeParams p) {
@@ -199,8 +199,8 @@ hipError_t launch_quantize_groups(const QuantizeParams& p, hipStream_t s) {
 
 // ---- reconstruction: W_hat[n][k] = scale * level -----------------------------------------------------------
 // A workgroup a tile, 16 lanes a row.  A lane writes four neighbouring columns at a time, 4 l + 64 h, so a
-// row's lanes write contiguous memory; two lanes share a dword of codes.  4096 x 25088 fp32: 76 to 80 us (463 MB,
-// 5.8 to 6.1 TB/s: memory).
+// row's lanes write contiguous memory; two lanes share a dword of codes.  4096 x 25088 fp32: 71 to 80 us (463 MB,
+// 5.8 to 6.5 TB/s: memory).
 template <int TYPE, bool LUT>
 __global__ __launch_bounds__(256) void reconstruct_groups_kernel(const ReconstructGroupsParams p) {
     const int l16 = threadIdx.x & 15;
@@ -250,8 +250,8 @@ hipError_t launch_reconstruct_groups(const ReconstructGroupsParams& p, hipStream
 // [-127, 127].  So |q| is at most 127 however large x is, q 2^e has seven significant bits (bf16 holds it
 // exactly, and fp16 does for fp16 inputs), and the error is at most half a step, one step where rint gives 128.
 // A group with an infinity or a NaN gets exponent 255: all of it is NaN when it is read.
-// Four lanes a group, 8 columns a lane: 16-byte loads for 16-bit types.  8192 x 25088 bf16: pack 107 to 112 us, restore
-// 103 to 105 us (623 MB each, 5.6 to 6.0 TB/s: memory).
+// Four lanes a group, 8 columns a lane: 16-byte loads for 16-bit types.  8192 x 25088 bf16: pack 107 to 113 us, restore
+// 100 to 105 us (623 MB each, 5.5 to 6.2 TB/s: memory).
 
 template <int TYPE>
 __global__ __launch_bounds__(256) void checkpoint_pack_kernel(const CheckpointParams p) {

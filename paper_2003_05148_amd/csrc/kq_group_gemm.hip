@@ -16,8 +16,8 @@
 // does, would take as many accumulators again, and the tile would halve.  Checkpoints and activations are
 // exact, sums are fp32.
 //
-// Measured, bf16: Linear 2048 x 4096 x 4096 80 to 82 us (838 to 854 TFLOP/s), GradInput 4096 x 4096 x 4096 128 to
-// 133 us (1036 to 1070), GradScales 2048 x 4096 x 25088 460 to 462 us (911 to 916), with dY's transpose (11 us) and the bias gradient.  What
+// Measured, bf16: Linear 2048 x 4096 x 4096 82 us (837 TFLOP/s; 80 to 86 on several machines), GradInput 4096 x 4096 x
+// 4096 131 us (1050; 127 to 140), GradScales 2048 x 4096 x 25088 463 us (909), with dY's transpose (11 us) and the bias gradient.  What
 // bounds them: no pipe alone.  Of an earlier GradInput (143 us in that run) the products by themselves take 103 us
 // (MFMA issue and fragment reads), decoding by itself 50, loads by themselves 88; two waves a SIMD cover part
 // of each other.  At a split contraction the partial sums count too (the weight's gradient of 2047 x 1000 x
@@ -30,7 +30,9 @@ constexpr int kStep = 64;  // contraction per step
 
 // LDS rows of 128 bytes in eight 16-byte chunks; chunk ch of row r lies at ch ^ swizzle(r).  Eight
 // consecutive rows of one chunk (fragment reads), rows 4 l + t (transposed writes of four columns) and rows
-// 8 d + 2 t + par (transposed writes of a dword's even or odd columns) all fall on eight different chunks.
+// 8 d + 2 t + par (transposed writes of a dword's even or odd columns) all fall on eight different chunks.  Linear's
+// writes do not: eight lanes write chunks 4 h + 0 .. 3 of two neighbouring rows, two to a bank (8 more cycles a
+// write, a quarter of the kernel's LDS cycles).
 __device__ __forceinline__ int swizzle(int r) { return (r ^ (r >> 2)) & 7; }
 __device__ __forceinline__ int lds_chunk(int r, int ch) { return r * 8 + (ch ^ swizzle(r)); }
 

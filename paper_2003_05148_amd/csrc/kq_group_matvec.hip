@@ -13,10 +13,10 @@
 // The waves of a workgroup take the 128-column blocks of its rows in turn and add their sums through LDS in
 // order.  Where there are few rows of W the columns are also split over workgroups, joined by a second kernel.
 //
-// Measured: one token through 4096 x 25088, 128 columns a group, 11.0 us a call (4.8 TB/s, the rate of a large
-// copy): bound by memory.  Without a table a kilobyte of codes takes about 60 vector instructions, a fifth of the
-// time that memory leaves; with a table about 140.  One token through 1000 x 512: 4.3 to 4.9 us a call, kernel 2.9: the
-// launch.  13 rows of fp16 through 4096 x 4096 with a table, 32 columns a group: 7.1 us; X's fragments from L2 (four
+// Measured: one token through 4096 x 25088, 128 columns a group, 10.8 to 11.1 us a call (4.8 to 4.9 TB/s: memory, at the
+// rate of a large copy; the streaming passes reach 6 TB/s, which would be 9 us).  Without a table a kilobyte of codes takes about 60 vector instructions, a fifth of the
+// time that memory leaves; with a table about 140.  One token through 1000 x 512: 4.5 to 4.9 us a call, kernel 3.0: the
+// launch.  13 rows of fp16 through 4096 x 4096 with a table, 32 columns a group: 7.2 us; X's fragments from L2 (four
 // loads beside each load of codes) and the load latency of four dependent rounds.
 #include "kq_group.h"
 
