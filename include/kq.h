@@ -614,7 +614,7 @@ kq_status kq_fit_layer_noalloc(const float* X, int64_t n, int32_t dim, int32_t k
  * kq_group_linear -- Y[m][n] = X[m][k] W_hat^T + bias (fp32 [n], or NULL).  Sums in fp32.  For up to 16
  *   rows of X the levels multiply X exactly (fp16: those above 2^-31 of the largest, smaller ones are off by
  *   at most 2^-39 of it) and a group's fp32 sum takes the scale; beyond, the weights are rounded to the type
- *   of X first.  An infinity in X makes its row of Y infinite or NaN, as may a
+ *   of X first (equal codes of a group alike).  An infinity in X makes its row of Y infinite or NaN, as may a
  *   group of X whose magnitudes add up to 2^127 or more.  A row of Y depends on its row of X and on m
  *   alone, not on other rows.
  * kq_group_linear_grad_input -- dX[m][k] = dY[m][n] W_hat, the weights rounded to the type of dY.

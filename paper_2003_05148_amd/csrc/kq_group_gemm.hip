@@ -12,9 +12,11 @@
 // lie in 16-byte aligned rows along c: dY is transposed into the workspace first (its column sums, the bias
 // gradient, are taken on the way), and an X or dY whose rows are not aligned is copied there.
 // Weights are s * level rounded once to the activation's type (bf16: s has 8 bits and -8..7 three, so
-// about half of them are exact): applying the scale to a group's fp32 sum instead, as the few-row kernel
-// does, would take as many accumulators again, and the tile would halve.  Checkpoints and activations are
-// exact, sums are fp32.
+// about half of them are exact; fp16 holds all of these in its range): applying the scale to a group's fp32 sum
+// instead, as the few-row kernel does, would take as many accumulators again, and the tile would halve.  Equal
+// codes of a group round alike, so where X has one sign their errors add up: of the result's norm 0.0022 for random
+// X and up to 0.0041 for positive X with a level table, where rounding the result alone gives 0.0017 (fp16: 2.1e-4
+// with -8 .. 7, 2.9e-4 and 4.3e-4 with a table, and 2.1e-4).  Checkpoints and activations are exact, sums are fp32.
 //
 // Measured, bf16: Linear 2048 x 4096 x 4096 82 us (837 TFLOP/s; 80 to 86 on several machines), GradInput 4096 x 4096 x
 // 4096 131 us (1050; 127 to 140), GradScales 2048 x 4096 x 25088 463 us (909), with dY's transpose (11 us) and the bias gradient.  What
