@@ -1,0 +1,392 @@
+"""Timed calls of the fully-connected layer in 8-bit floating point with a scale for each block of 128, and of
+distillation from a teacher's top logits.
+
+A case is a dict of plain values; ``op`` names the operator:
+
+  quantize     kq_quantize_blocks, then kq_reconstruct_blocks: e4m3 values and a power of two for each block of
+               ``rows`` rows by 128 columns (1: an activation, 128: a weight), and what they stand for
+  linear       kq_block_linear: Y = X W^T + b, X quantized on the way or (``x8``) before
+  grad_input   kq_block_linear_grad_input: dX = dY W
+  grad_weight  kq_block_linear_grad_weight: dW = dY^T X from the 8-bit values of X that the forward call used
+  distill      kq_distill: the loss of every row and the gradient of the logits in one call, or (``fused`` false)
+               kq_distill_loss, then kq_distill_grad with the loss' own gradient
+
+``m`` rows (tokens, images), ``n`` output features, ``k`` input features; ``v`` classes, ``top`` logits kept of the
+teacher, ``ragged`` whether rows keep only what makes up 99 % of the teacher's probability.  Sizes are those of
+VGG-16's fully-connected layers (25088 -> 4096 -> 4096 -> 1000) and ResNet-18's classifier (512 -> 1000), and
+vocabularies of language models in round and odd sizes.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+_DTYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+_BYTES = {"bf16": 2, "f16": 2, "f32": 4}
+_BLOCK = 128
+_MOST = 2 * 4096 * 4096 * 25088   # operations of the largest listed product
+_MOST_LOGITS = 4096 * 50001       # logits of the largest listed batch
+
+
+def listed():
+    return [
+        # a small ragged activation of an fp32 model
+        {"name": "quantize_33x1000", "op": "quantize", "m": 33, "k": 1000, "rows": 1, "dtype": "f32"},
+        # compressing VGG-16's largest layer
+        {"name": "quantize_4096x25088_weight", "op": "quantize", "m": 4096, "k": 25088, "rows": 128, "dtype": "f32"},
+        # a few requests through a small classifier of odd width: latency
+        {"name": "linear_13_1000x511", "op": "linear", "m": 13, "n": 1000, "k": 511, "dtype": "f16", "bias": True, "x8": False},
+        # one token through the largest layer: the stream of the weights
+        {"name": "linear_1_4096x25088", "op": "linear", "m": 1, "n": 4096, "k": 25088, "dtype": "bf16", "bias": False, "x8": False},
+        # a training batch, its input quantized before: the backward pass takes it again
+        {"name": "linear_4096_4096x4096", "op": "linear", "m": 4096, "n": 4096, "k": 4096, "dtype": "bf16", "bias": True, "x8": True},
+        # the gradient of a ragged small batch
+        {"name": "grad_input_37_1000x1023", "op": "grad_input", "m": 37, "n": 1000, "k": 1023, "dtype": "f16"},
+        # the gradient of a training batch
+        {"name": "grad_input_4096_4096x4096", "op": "grad_input", "m": 4096, "n": 4096, "k": 4096, "dtype": "bf16"},
+        # retraining a classifier on a ragged batch: odd sizes everywhere
+        {"name": "grad_weight_2047_1000x4095", "op": "grad_weight", "m": 2047, "n": 1000, "k": 4095, "dtype": "f16", "bias": True},
+        # retraining VGG-16's largest layer
+        {"name": "grad_weight_4096_4096x25088", "op": "grad_weight", "m": 4096, "n": 4096, "k": 25088, "dtype": "bf16", "bias": False},
+        # an image classifier's batch with labels
+        {"name": "distill_64x1000", "op": "distill", "m": 64, "v": 1000, "top": 10, "dtype": "bf16", "temperature": 2.0, "alpha": 0.3, "ragged": False, "fused": True},
+        # a few tokens of a large vocabulary, loss and gradient in calls of their own
+        {"name": "distill_16x131071", "op": "distill", "m": 16, "v": 131071, "top": 100, "dtype": "f32", "temperature": 1.5, "alpha": 0.25, "ragged": True, "fused": False},
+        # a training batch of tokens over an odd vocabulary
+        {"name": "distill_4096x50001", "op": "distill", "m": 4096, "v": 50001, "top": 64, "dtype": "bf16", "temperature": 1.0, "alpha": 0.0, "ragged": True, "fused": True},
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _size(rng, lo, hi):
+    """A size of the range: round (a multiple of 64) or not."""
+    v = _log_int(rng, lo, hi)
+    return max(64, v // 64 * 64) if rng.random() < 0.5 else v
+
+
+def draw(rng):
+    op = rng.choice(["quantize", "linear", "linear", "linear", "grad_input", "grad_weight", "distill", "distill"])
+    dtype = rng.choice(["bf16", "f16", "bf16", "f16", "f32"])
+    if op == "distill":
+        v = _log_int(rng, 10, 131072)
+        m = max(1, min(_log_int(rng, 1, 8192), _MOST_LOGITS // v))
+        mix = rng.random() < 0.5
+        return {"op": op, "m": m, "v": v, "top": _log_int(rng, 1, min(v, 128)), "dtype": dtype,
+                "temperature": 1.0 if rng.random() < 0.3 else round(rng.uniform(1.0, 5.0), 2),
+                "alpha": round(rng.uniform(0.05, 0.95), 2) if mix else 0.0, "ragged": rng.random() < 0.5, "fused": rng.random() < 0.6}
+    if op == "quantize":
+        return {"op": op, "m": _log_int(rng, 1, 4096), "k": _size(rng, 33, 25088), "rows": rng.choice([1, 128]), "dtype": dtype}
+    n, k = _size(rng, 65, 8192), _size(rng, 65, 25088)
+    m = rng.choice([1, _log_int(rng, 1, 16), _log_int(rng, 1, 4096)]) if op == "linear" else _log_int(rng, 1, 4096)
+    m = max(1, min(m, _MOST // (2 * n * k)))
+    case = {"op": op, "m": m, "n": n, "k": k, "dtype": dtype}
+    if op != "grad_input":
+        case["bias"] = rng.random() < 0.5
+    if op == "linear":
+        case["x8"] = rng.random() < 0.3
+    return case
+
+
+# ---- inputs ------------------------------------------------------------------------------------
+
+def _activation(m, k, dtype, gen):
+    """After a ReLU: half of it zero, a long tail, some rows much larger than others."""
+    x = torch.randn(m, k, device="cuda", generator=gen).relu_()
+    return (x * torch.exp(torch.randn(m, 1, device="cuda", generator=gen))).to(dtype)
+
+
+def _weights(case, gen):
+    """Values and exponents of Gaussian weights of variance 1/k, as the quantizer leaves them."""
+    return _stored(torch.randn(case["n"], case["k"], device="cuda", generator=gen) / math.sqrt(case["k"]), 128)
+
+
+def _stored(x, rows):
+    exps, v = _quantize(x, rows)
+    return v.to(torch.float8_e4m3fn), exps
+
+
+def _logits(case, gen):
+    """(student's logits, the teacher's top logits and where they stand, labels): the student is the teacher with
+    noise; the label is the teacher's first choice, but for one row in eight, and one row in sixteen has none."""
+    m, v, top, dtype = case["m"], case["v"], case["top"], _DTYPES[case["dtype"]]
+    t = torch.randn(m, v, device="cuda", generator=gen)
+    t.mul_(1.0 + t.relu())   # a long upper tail
+    values, idx = t.topk(top, dim=1)
+    Z = (0.8 * t + 0.5 * torch.randn(m, v, device="cuda", generator=gen)).to(dtype)
+    if case["ragged"]:   # what makes up 99 % of the kept probability stays, at least the first
+        p = torch.softmax(values.double(), 1)
+        idx = torch.where(p.cumsum(1) - p <= 0.99, idx, torch.full_like(idx, -1))
+    labels = None
+    if case["alpha"] > 0:
+        u = torch.rand(m, device="cuda", generator=gen)
+        other = torch.randint(0, v, (m,), device="cuda", generator=gen)
+        labels = torch.where(u < 1 / 8, other, idx[:, 0])
+        labels = torch.where(u > 15 / 16, torch.full_like(labels, -100), labels)
+    return Z, values, idx, labels
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    op, dtype = case["op"], _DTYPES[case["dtype"]]
+    state = {"case": case}
+    if op == "quantize":
+        if case["rows"] == 1:
+            state["X"] = _activation(case["m"], case["k"], dtype, gen)
+        else:
+            state["X"] = (torch.randn(case["m"], case["k"], device="cuda", generator=gen) / math.sqrt(case["k"])).to(dtype)
+        return state
+    if op == "distill":
+        state["Z"], state["top_values"], state["top_idx"], state["labels"] = _logits(case, gen)
+        state["dloss"] = torch.full((case["m"],), 1.0 / case["m"], device="cuda")   # of the mean over the rows
+        return state
+    if op != "grad_weight":
+        state["W"], state["W_exps"] = _weights(case, gen)
+    if op == "linear":
+        X = _activation(case["m"], case["k"], dtype, gen)
+        state["X"], state["X_exps"] = _stored(X.float(), 1) if case["x8"] else (X, None)
+        state["bias"] = 0.1 * torch.randn(case["n"], device="cuda", generator=gen) if case["bias"] else None
+        return state
+    # rows of very different size, as the gradients of a loss have them
+    dY = 0.01 * torch.randn(case["m"], case["n"], device="cuda", generator=gen)
+    state["dY"] = (dY * torch.exp(torch.randn(case["m"], 1, device="cuda", generator=gen))).to(dtype)
+    if op == "grad_weight":
+        state["X"], state["X_exps"] = _stored(_activation(case["m"], case["k"], dtype, gen).float(), 1)
+    return state
+
+
+# ---- the plain forms ----------------------------------------------------------------------------
+
+def _power(exps):
+    """2^(exps - 127) from its bits, 255 NaN."""
+    return torch.where(exps == 255, torch.full((), math.nan, device=exps.device), (exps.int() << 23).view(torch.float32))
+
+
+def _spread(exps, rows, m, cols):
+    """One value a block to one an element."""
+    return exps.repeat_interleave(_BLOCK, 1)[:, :cols].repeat_interleave(rows, 0)[:m]
+
+
+def _quantize(x, rows):
+    """x fp32 [m, k] -> (exps uint8 [ceil(m / rows), ceil(k / 128)], v fp32 [m, k rounded up to 128]): the power of two
+    takes the block's largest magnitude to at most 448, e4m3's largest number, and above 224; v is nearest, ties to even."""
+    m, k = x.shape
+    kb, mb = -(-k // _BLOCK), -(-m // rows)
+    x = torch.nn.functional.pad(x, (0, kb * _BLOCK - k, 0, mb * rows - m))
+    a = x.abs().view(mb, rows, kb, _BLOCK).amax((1, 3))
+    f, e = torch.frexp(a)                                    # a = f 2^e, 1/2 <= f < 1
+    e = (e - 9 + (f > 0.875).int()).clamp(min=-126)
+    e = torch.where(a > 0, e, torch.full_like(e, -126))
+    exps = torch.where(torch.isfinite(a), e + 127, torch.full_like(e, 255)).to(torch.uint8)
+    v = x / _spread(_power(exps), rows, mb * rows, kb * _BLOCK)
+    step = torch.exp2((torch.frexp(v)[1] - 4).clamp(min=-9).float())   # 3 bits behind the first, down to 2^-9
+    return exps, (torch.round(v / step) * step)[:m]
+
+
+def _restore(values, exps, rows):
+    return values.float() * _spread(_power(exps), rows, *values.shape)
+
+
+def _again(x, rows):
+    """What x is after the quantizer."""
+    exps, v = _quantize(x, rows)
+    return (v * _spread(_power(exps), rows, *v.shape))[:, :x.shape[1]]
+
+
+def run(state):
+    return _run_own(state) if own else _run_plain(state)
+
+
+def _run_plain(state):
+    case = state["case"]
+    op, dtype = case["op"], _DTYPES[case["dtype"]]
+    if op == "distill":
+        return _distill_plain(state)
+    if op == "quantize":
+        exps, v = _quantize(state["X"].float(), case["rows"])
+        return {"exps": exps, "X_hat": _restore(v, exps, case["rows"])[:, :case["k"]]}
+    if op == "linear":
+        X = _restore(state["X"], state["X_exps"], 1)[:, :case["k"]] if case["x8"] else _again(state["X"].float(), 1)
+        Y = X @ _restore(state["W"], state["W_exps"], 128)[:, :case["k"]].t()
+        if state["bias"] is not None:
+            Y += state["bias"]
+        return {"Y": Y.to(dtype)}
+    dY = state["dY"].float()
+    if op == "grad_input":
+        return {"dX": (_again(dY, 1) @ _restore(state["W"], state["W_exps"], 128)[:, :case["k"]]).to(dtype)}
+    X = _restore(state["X"], state["X_exps"], 1)[:, :case["k"]]
+    out = {"dW": _again(dY.t(), 1) @ _again(X.t(), 1).t()}   # blocks of 128 rows
+    if case["bias"]:
+        out["dbias"] = dY.sum(0)
+    return out
+
+
+def _distill_plain(state):
+    case = state["case"]
+    T, alpha, v = case["temperature"], case["alpha"], case["v"]
+    Z, idx = state["Z"].float(), state["top_idx"]
+    here = (idx >= 0) & (idx < v)
+    at = torch.where(here, idx, torch.zeros_like(idx))
+    t = torch.where(here, state["top_values"].float() / T, torch.full((), -math.inf, device=Z.device))
+    t = t - t.amax(1, keepdim=True)
+    et = torch.exp(t)
+    total = et.sum(1, keepdim=True)
+    p = torch.where(here, et / total, torch.zeros_like(et))
+    z = (Z - Z.amax(1, keepdim=True)) / T
+    ez = torch.exp(z)
+    sz = ez.sum(1, keepdim=True)
+    diff = (t - torch.log(total)) - (z.gather(1, at) - torch.log(sz))
+    loss = (1 - alpha) * T * T * torch.where(p > 0, p * diff, torch.zeros_like(p)).sum(1)
+    d = state["dloss"][:, None]
+    some = here.any(1, keepdim=True).float()
+    dZ = (ez / sz * some).scatter_add_(1, at, -p) * ((1 - alpha) * T * d)
+    if alpha > 0:
+        y = state["labels"][:, None]
+        has = (y >= 0) & (y < v)
+        y = torch.where(has, y, torch.zeros_like(y))
+        z = Z - Z.amax(1, keepdim=True)
+        ez = torch.exp(z)
+        sz = ez.sum(1, keepdim=True)
+        loss += torch.where(has, alpha * (torch.log(sz) - z.gather(1, y)), torch.zeros_like(sz))[:, 0]
+        dZ += (ez / sz).scatter_add_(1, y, -torch.ones_like(sz)) * (alpha * d * has.float())
+    return {"loss": loss, "dZ": dZ.to(state["Z"].dtype)}
+
+
+def _run_own(state):
+    import paper_2003_05148_amd as kq
+    case = state["case"]
+    op, dtype = case["op"], _DTYPES[case["dtype"]]
+    if op == "quantize":
+        values, exps = kq.kq_quantize_blocks(state["X"], rows=case["rows"])
+        return {"exps": exps, "X_hat": kq.kq_reconstruct_blocks(values, exps, case["k"], rows=case["rows"])}
+    if op == "linear":
+        return {"Y": kq.kq_block_linear(state["X"], state["W"], state["W_exps"], bias=state["bias"],
+                                        x_exps=state["X_exps"], dtype=dtype)}
+    if op == "grad_input":
+        return {"dX": kq.kq_block_linear_grad_input(state["dY"], state["W"], state["W_exps"], case["k"])}
+    if op == "grad_weight":
+        dW, dbias = kq.kq_block_linear_grad_weight(state["dY"], state["X"], state["X_exps"], case["k"], bias=case["bias"])
+        return {"dW": dW, "dbias": dbias} if case["bias"] else {"dW": dW}
+    how = dict(temperature=case["temperature"], labels=state["labels"], alpha=case["alpha"])
+    if case["fused"]:
+        loss, dZ = kq.kq_distill(state["Z"], state["top_values"], state["top_idx"], scale=1.0 / case["m"], **how)
+    else:
+        loss, stats = kq.kq_distill_loss(state["Z"], state["top_values"], state["top_idx"], **how)
+        dZ = kq.kq_distill_grad(state["Z"], state["top_values"], state["top_idx"], stats, state["dloss"], **how)
+    return {"loss": loss, "dZ": dZ}
+
+
+# ---- what a pass cannot do without ---------------------------------------------------------------
+
+def work(case):
+    op, size = case["op"], _BYTES[case["dtype"]]
+    m = case["m"]
+    if op == "distill":      # logits in, gradient out (fused or not: the loss' gradient is known before), top logits and indices
+        v = case["v"]
+        labels = 8 * m if case["alpha"] > 0 else 0
+        return {"bytes": m * (2 * v * size + 12 * case["top"] + 8) + labels, "flops": 8 * m * v}
+    k = case["k"]
+    kp = -(-k // _BLOCK) * _BLOCK
+    if op == "quantize":     # X in, values and exponents out and in again, X_hat (fp32) out
+        exps = -(-m // case["rows"]) * kp // _BLOCK
+        return {"bytes": m * k * (size + 4) + 2 * (m * kp + exps), "flops": 4 * m * k}
+    n = case["n"]
+    weight, flops = n * kp + -(-n // 128) * kp // _BLOCK, 2 * m * n * k
+    x8 = m * (kp + kp // _BLOCK)
+    bias = 4 * n if case.get("bias") else 0
+    if op == "grad_weight":
+        return {"bytes": m * n * size + x8 + 4 * n * k + bias, "flops": flops}
+    if op == "linear":
+        return {"bytes": weight + (x8 if case["x8"] else m * k * size) + m * n * size + bias, "flops": flops}
+    return {"bytes": weight + m * (n + k) * size, "flops": flops}
+
+
+# ---- the definitions in 64 bits -------------------------------------------------------------------
+
+def _exact_quantized(x, rows):
+    """x (64 bits) -> (exps, x_hat): block by block of columns."""
+    m, k = x.shape
+    exps, parts = [], []
+    for c in range(0, k, _BLOCK):
+        b = x[:, c:c + _BLOCK]
+        a = b.abs().max(1).values
+        if rows > 1:
+            a = torch.stack([piece.max() for piece in a.split(rows)])
+        top = torch.where(a > 0, a, torch.full_like(a, 2.0 ** -140))
+        E = torch.floor(torch.log2(top))
+        e = torch.where(top > 1.75 * torch.exp2(E), E - 7, E - 8).clamp(min=-126)
+        scale = torch.exp2(e).repeat_interleave(rows)[:m, None]
+        v = b / scale
+        mag = v.abs().clamp(min=2.0 ** -6)
+        ulp = torch.exp2(torch.floor(torch.log2(mag)) - 3)
+        parts.append((v / ulp).round() * ulp * scale)
+        exps.append(e + 127)
+    return torch.stack(exps, 1), torch.cat(parts, 1)
+
+
+def _exact_stored(values, exps, rows, k):
+    m = values.shape[0]
+    r, c = torch.arange(m, device="cuda") // rows, torch.arange(k, device="cuda") // _BLOCK
+    return values[:, :k].double() * torch.exp2(exps.double() - 127)[r][:, c]
+
+
+def _exact_distill(case, state):
+    T, alpha, m, v = case["temperature"], case["alpha"], case["m"], case["v"]
+    losses, grads = [], []
+    rows = max(1, (1 << 27) // v)
+    for r in range(0, m, rows):     # in pieces: 64 bits of a large batch are many
+        z, idx = state["Z"][r:r + rows].double(), state["top_idx"][r:r + rows]
+        here = (idx >= 0) & (idx < v)
+        logp = torch.log_softmax(torch.where(here, state["top_values"][r:r + rows].double() / T, -math.inf), 1)
+        p_rows = torch.zeros_like(z)
+        loss = torch.zeros(z.shape[0], dtype=torch.float64, device="cuda")
+        logq = torch.log_softmax(z / T, 1)
+        line = torch.arange(z.shape[0], device="cuda")
+        for j in range(case["top"]):
+            ok = here[:, j]
+            rr, at, lp = line[ok], idx[ok, j], logp[ok, j]
+            p_rows[rr, at] += torch.exp(lp)
+            loss[rr] += torch.exp(lp) * (lp - logq[rr, at])
+        loss *= (1 - alpha) * T * T
+        g = (torch.exp(logq) * here.any(1)[:, None] - p_rows) * ((1 - alpha) * T)
+        if alpha > 0:
+            y = state["labels"][r:r + rows]
+            ok = (y >= 0) & (y < v)
+            logs = torch.log_softmax(z, 1)
+            loss[ok] -= alpha * logs[line[ok], y[ok]]
+            h = torch.exp(logs)
+            h[line[ok], y[ok]] -= 1
+            g += alpha * h * ok[:, None]
+        losses.append(loss)
+        grads.append(g / m)
+    return {"loss": torch.cat(losses), "dZ": torch.cat(grads)}
+
+
+def exact(case, seed):
+    state = prepare(case, seed)
+    op, k = case["op"], case.get("k")
+    if op == "distill":
+        return _exact_distill(case, state)
+    if op == "quantize":
+        exps, x_hat = _exact_quantized(state["X"].double(), case["rows"])
+        return {"exps": exps, "X_hat": x_hat}
+    if op == "grad_weight":
+        dY = state["dY"].double()
+        X = _exact_stored(state["X"], state["X_exps"], 1, k)
+        dY_t = _exact_quantized(dY.t().contiguous(), 1)[1]
+        X_t = _exact_quantized(X.t().contiguous(), 1)[1]
+        out = {"dW": torch.matmul(dY_t, X_t.t().contiguous())}
+        if case["bias"]:
+            out["dbias"] = dY.sum(0)
+        return out
+    W = _exact_stored(state["W"], state["W_exps"], 128, k)
+    if op == "grad_input":
+        return {"dX": torch.matmul(_exact_quantized(state["dY"].double(), 1)[1], W)}
+    X = _exact_stored(state["X"], state["X_exps"], 1, k) if case["x8"] else _exact_quantized(state["X"].double(), 1)[1]
+    Y = torch.matmul(X, W.t().contiguous())
+    return {"Y": Y + state["bias"].double() if state["bias"] is not None else Y}
