@@ -7,7 +7,8 @@ A case is a dict of plain values; ``op`` names the operator:
                ``rows`` rows by 128 columns (1: an activation, 128: a weight), and what they stand for
   linear       kq_block_linear: Y = X W^T + b, X quantized on the way or (``x8``) before
   grad_input   kq_block_linear_grad_input: dX = dY W
-  grad_weight  kq_block_linear_grad_weight: dW = dY^T X from the 8-bit values of X that the forward call used
+  grad_weight  kq_block_linear_grad_weight: dW = dY^T X (of type ``out``) from the 8-bit values of X that the forward
+               call used
   distill      kq_distill: the loss of every row and the gradient of the logits in one call, or (``fused`` false)
                kq_distill_loss, then kq_distill_grad with the loss' own gradient
 
@@ -47,10 +48,10 @@ def listed():
         {"name": "grad_input_37_1000x1023", "op": "grad_input", "m": 37, "n": 1000, "k": 1023, "dtype": "f16"},
         # the gradient of a training batch
         {"name": "grad_input_4096_4096x4096", "op": "grad_input", "m": 4096, "n": 4096, "k": 4096, "dtype": "bf16"},
-        # retraining a classifier on a ragged batch: odd sizes everywhere
-        {"name": "grad_weight_2047_1000x4095", "op": "grad_weight", "m": 2047, "n": 1000, "k": 4095, "dtype": "f16", "bias": True},
-        # retraining VGG-16's largest layer
-        {"name": "grad_weight_4096_4096x25088", "op": "grad_weight", "m": 4096, "n": 4096, "k": 25088, "dtype": "bf16", "bias": False},
+        # retraining a classifier with fp32 master weights on a ragged batch: odd sizes everywhere
+        {"name": "grad_weight_2047_1000x4095", "op": "grad_weight", "m": 2047, "n": 1000, "k": 4095, "dtype": "f16", "out": "f32", "bias": True},
+        # retraining VGG-16's largest layer, held in bf16
+        {"name": "grad_weight_4096_4096x25088", "op": "grad_weight", "m": 4096, "n": 4096, "k": 25088, "dtype": "bf16", "out": "bf16", "bias": False},
         # an image classifier's batch with labels
         {"name": "distill_64x1000", "op": "distill", "m": 64, "v": 1000, "top": 10, "dtype": "bf16", "temperature": 2.0, "alpha": 0.3, "ragged": False, "fused": True},
         # a few tokens of a large vocabulary, loss and gradient in calls of their own
@@ -90,6 +91,8 @@ def draw(rng):
         case["bias"] = rng.random() < 0.5
     if op == "linear":
         case["x8"] = rng.random() < 0.3
+    if op == "grad_weight":
+        case["out"] = rng.choice(["f32", dtype])
     return case
 
 
@@ -220,7 +223,7 @@ def _run_plain(state):
     if op == "grad_input":
         return {"dX": (_again(dY, 1) @ _restore(state["W"], state["W_exps"], 128)[:, :case["k"]]).to(dtype)}
     X = _restore(state["X"], state["X_exps"], 1)[:, :case["k"]]
-    out = {"dW": _again(dY.t(), 1) @ _again(X.t(), 1).t()}   # blocks of 128 rows
+    out = {"dW": (_again(dY.t(), 1) @ _again(X.t(), 1).t()).to(_DTYPES[case["out"]])}   # blocks of 128 rows
     if case["bias"]:
         out["dbias"] = dY.sum(0)
     return out
@@ -270,7 +273,8 @@ def _run_own(state):
     if op == "grad_input":
         return {"dX": kq.kq_block_linear_grad_input(state["dY"], state["W"], state["W_exps"], case["k"])}
     if op == "grad_weight":
-        dW, dbias = kq.kq_block_linear_grad_weight(state["dY"], state["X"], state["X_exps"], case["k"], bias=case["bias"])
+        dW, dbias = kq.kq_block_linear_grad_weight(state["dY"], state["X"], state["X_exps"], case["k"], bias=case["bias"],
+                                                   dtype=_DTYPES[case["out"]])
         return {"dW": dW, "dbias": dbias} if case["bias"] else {"dW": dW}
     how = dict(temperature=case["temperature"], labels=state["labels"], alpha=case["alpha"])
     if case["fused"]:
@@ -300,7 +304,7 @@ def work(case):
     x8 = m * (kp + kp // _BLOCK)
     bias = 4 * n if case.get("bias") else 0
     if op == "grad_weight":
-        return {"bytes": m * n * size + x8 + 4 * n * k + bias, "flops": flops}
+        return {"bytes": m * n * size + x8 + n * k * _BYTES[case["out"]] + bias, "flops": flops}
     if op == "linear":
         return {"bytes": weight + (x8 if case["x8"] else m * k * size) + m * n * size + bias, "flops": flops}
     return {"bytes": weight + m * (n + k) * size, "flops": flops}
