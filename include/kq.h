@@ -30,6 +30,11 @@
  *                        kq_checkpoint_grad_scales and kq_checkpoint_grad_weight take the
  *                        gradients of the group scales (Eq. 2's idea: a shared value moves with
  *                        the gradients of what it stands for) or of the whole weight from it.
+ *   kq_quantize_blocks   a fully-connected layer (or its input) in 8-bit floats with a power of two for each
+ *                        block of 128; kq_block_linear, kq_block_linear_grad_input and
+ *                        kq_block_linear_grad_weight run and train it.
+ *   kq_distill           the loss that a compressed classifier is retrained with: against the top logits
+ *                        of the uncompressed one, with its gradient.
  *   kq_accounting        Eq. (4), (6), (7): storage bits, compression ratio, bits per parameter.
  *
  * Conventions shared by every call
@@ -676,6 +681,104 @@ kq_status kq_checkpoint_grad_scales(const void* dY, int32_t type, int64_t ldy, i
 kq_status kq_checkpoint_grad_weight(const void* dY, int32_t type, int64_t ldy, int64_t m, int64_t n, int64_t k,
                                     const int8_t* q, const uint8_t* exps, float* dW, int64_t lddw, float* dbias,
                                     void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Fully-connected layers in 8-bit floating point with a power of two for each block of 128.
+ *
+ *   x_hat = v 2^e, v an e4m3 number (4 exponent bits, 3 mantissa bits, largest 448), e shared by a block: KQ_BLOCK
+ *   neighbouring columns of 1 row (an activation, a gradient) or of 128 rows (a weight).  With a the
+ *   block's largest magnitude and E = floor(log2 a): e = E - 8 where a <= 1.75 2^E and E - 7 otherwise, so
+ *   that a 2^-e is in (224, 448], and e is at least -126; v is the nearest number to x 2^-e, ties to even.  A
+ *   block with an infinity or NaN is NaN when it is read.
+ *   values device [m][kp] bytes, 16-byte aligned, kp = k rounded up to KQ_BLOCK (zeros past k);
+ *   exps device [ceil(m / rows)][kp / KQ_BLOCK] uint8: e + 127 (1 .. 254), or 255 for NaN (0 does not occur).
+ *   Types are KQ_T_*; KQ_T_E4M3 stands for such a pair where an input may be one.  Matrices are row-major with a row
+ *   pitch in elements, aligned to their type; a KQ_T_E4M3 matrix has the pitch kp.  Sizes are limited as for the
+ *   4-bit layers; m = 0 writes nothing (gradients of parameters are zero then).
+ *   Products whose magnitude is below 2^-126 may be taken as zero.
+ *
+ * kq_quantize_blocks, kq_reconstruct_blocks -- X [m][k] of any KQ_T_* type but KQ_T_E4M3; rows 1 or 128 (else
+ *   KQ_ERR_UNSUPPORTED).
+ * kq_block_linear -- Y[m][n] = X_hat[m][k] W_hat^T + bias (fp32 [n], or NULL).  X of type KQ_T_F32, KQ_T_BF16 or KQ_T_F16 (x_exps
+ *   is NULL) is quantized on the way, in blocks of 1 row: the same values as from kq_quantize_blocks.  X of type
+ *   KQ_T_E4M3 comes with x_exps.  values and exps: the weight [n][k], rows = 128.  y_type is any but KQ_T_E4M3.
+ * kq_block_linear_grad_input -- dX[m][k] = dY_hat W_hat, dY [m][n] quantized in blocks of 1 row along n; dX in
+ *   the type of dY.
+ * kq_block_linear_grad_weight -- dW[o][c] = sum_m dY^[m][o] X^[m][c] from X's values (rows = 1): both are quantized along m, in
+ *   blocks of 128 rows by 1 column (X's values again: a power of two changes them only where they become
+ *   subnormal).  dw_type is any but KQ_T_E4M3.  dbias (fp32 [n], or NULL): sum_m dY[m][o], not quantized.
+ *   Sums.  Where the output is fp32, and in kq_block_linear of up to 16 rows, products are exact and sums are fp32.
+ *   Otherwise the 8-bit matrix instruction adds them: eight products at a time, each cut off 13 bits below the
+ *   largest of the eight (on random operands 1.5e-5 of the result's norm, where rounding to bf16 is 1.7e-3 and to
+ *   fp16 2.1e-4), and the eights in fp32.  The order of a sum goes by the sizes alone.
+ *   workspaces: the *_workspace_bytes of the same arguments (may be 0: ws may be NULL then).
+ */
+#define KQ_T_E4M3 3
+#define KQ_BLOCK 128
+kq_status kq_quantize_blocks(const void* X, int32_t type, int64_t ldx, int64_t m, int64_t k, int32_t rows, uint8_t* values,
+                             uint8_t* exps, void* stream);
+kq_status kq_reconstruct_blocks(const uint8_t* values, const uint8_t* exps, int64_t m, int64_t k, int32_t rows,
+                                int32_t type, void* X_hat, int64_t ldx, void* stream);
+size_t kq_block_linear_workspace_bytes(int32_t x_type, int32_t y_type, int64_t m, int64_t n, int64_t k);
+kq_status kq_block_linear(const void* X, int32_t x_type, int64_t ldx, const uint8_t* x_exps, int64_t m, int64_t n, int64_t k,
+                          const uint8_t* values, const uint8_t* exps, const float* bias, void* Y, int32_t y_type,
+                          int64_t ldy, void* ws, size_t ws_bytes, void* stream);
+size_t kq_block_linear_grad_input_workspace_bytes(int32_t type, int64_t m, int64_t n, int64_t k);
+kq_status kq_block_linear_grad_input(const void* dY, int32_t type, int64_t ldy, int64_t m, int64_t n, int64_t k,
+                                     const uint8_t* values, const uint8_t* exps, void* dX, int64_t ldx, void* ws,
+                                     size_t ws_bytes, void* stream);
+size_t kq_block_linear_grad_weight_workspace_bytes(int32_t dw_type, int64_t m, int64_t n, int64_t k);
+kq_status kq_block_linear_grad_weight(const void* dY, int32_t type, int64_t ldy, int64_t m, int64_t n, int64_t k,
+                                      const uint8_t* x_values, const uint8_t* x_exps, void* dW, int32_t dw_type,
+                                      int64_t lddw, float* dbias, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Distillation from a teacher's top logits.
+ *
+ *   Z device [m][v], logits of the network that is trained (fp32, bf16 or fp16, row pitch ldz); of every row the
+ *   teacher's `top` largest logits: top_values device [m][top] (any KQ_T_* type but KQ_T_E4M3) at top_idx device
+ *   [m][top] (int32 or int64: idx_bytes 4 or 8).  Entries whose index is outside [0, v) or whose logit is -infinity are
+ *   absent (rows may keep different numbers of them); an index that stands twice counts twice.  labels device [m] (int32
+ *   or int64: label_bytes) or NULL; a label outside [0, v) is absent.  With p the softmax of a row's present
+ *   teacher logits / T, q the softmax of z / T and s the softmax of z,
+ *     loss = (1 - alpha) T^2 sum_j p_j (log p_j - log q_idx[j])  +  alpha (-log s_label),
+ *     dz_c = d [ (1 - alpha) T (q_c - sum of p_j with idx[j] = c)  +  alpha (s_c - [c = label]) ];
+ *   a row without a present entry (or label) has no first (second) term in either.  d is dloss[row], or `scale` for
+ *   all rows where dloss is NULL.  A term with a weight of zero (alpha 0 or 1) is not computed.
+ *   A NaN or +infinity in a row makes its loss and gradient NaN; -infinity in Z is a class that is masked out (gradient
+ *   0, or the teacher's share: its loss is infinite then).
+ *   1 <= v <= KQ_DISTILL_MAX_CLASSES, 1 <= top <= KQ_DISTILL_MAX_TOP, 0 <= m <= KQ_GROUP_MAX_ROWS,
+ *   2^-10 <= temperature <= 2^20 (else KQ_ERR_UNSUPPORTED), 0 <= alpha <= 1; alpha > 0 needs labels.
+ *
+ * kq_distill -- loss device [m] fp32 and dZ [m][v] (Z's type, pitch lddz; dZ may be Z).
+ * kq_distill_loss -- loss, and stats device [m][3] fp32 for the gradient: the row's largest logit, the sum of
+ *   exp((z - largest) / T) and that of exp(z - largest) (0 where it is not needed).
+ * kq_distill_grad -- dZ (may be Z) from the same inputs, stats and dloss (device [m] fp32, or NULL for `scale`).
+ *   Sums in fp32, in an order that the sizes alone decide.
+ *   workspace: kq_distill_workspace_bytes(m, v, top) (may be 0).
+ */
+#define KQ_DISTILL_MAX_CLASSES (1 << 24)
+#define KQ_DISTILL_MAX_TOP 256
+typedef struct kq_distill_args {
+    const void* Z;
+    int32_t type;
+    int64_t ldz, m, v;
+    const void* top_values;
+    int32_t top_type;
+    const void* top_idx;
+    int32_t idx_bytes;
+    int32_t top;
+    const void* labels;
+    int32_t label_bytes;
+    float temperature, alpha;
+} kq_distill_args;
+size_t kq_distill_workspace_bytes(int64_t m, int64_t v, int32_t top);
+kq_status kq_distill(const kq_distill_args* args /* host */, const float* dloss, float scale, float* loss, void* dZ,
+                     int64_t lddz, void* ws, size_t ws_bytes, void* stream);
+kq_status kq_distill_loss(const kq_distill_args* args /* host */, float* loss, float* stats, void* ws, size_t ws_bytes,
+                          void* stream);
+kq_status kq_distill_grad(const kq_distill_args* args /* host */, const float* stats, const float* dloss, float scale,
+                          void* dZ, int64_t lddz, void* stream);
 
 #ifdef __cplusplus
 }

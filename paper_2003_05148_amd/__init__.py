@@ -15,7 +15,11 @@ Entry points (same names as the C ABI):
   kq_reconstruct, kq_reconstruct_packed;
   fully-connected layers in 4 bits: kq_quantize_groups, kq_reconstruct_groups, kq_group_linear,
   kq_group_linear_grad_input; 8-bit activations: kq_checkpoint_pack, kq_checkpoint_restore,
-  kq_checkpoint_grad_scales, kq_checkpoint_grad_weight; GroupLinear, a layer over them.
+  kq_checkpoint_grad_scales, kq_checkpoint_grad_weight; GroupLinear, a layer over them;
+  fully-connected layers in 8-bit floats with a power of two for each block of 128: kq_quantize_blocks,
+  kq_reconstruct_blocks, kq_block_linear, kq_block_linear_grad_input, kq_block_linear_grad_weight; BlockLinear, a
+  layer over them;
+  retraining against an uncompressed network: kq_distill, kq_distill_loss, kq_distill_grad.
 """
 from __future__ import annotations
 
@@ -64,6 +68,12 @@ class KqCompressLayer(ctypes.Structure):
     _fields_ = [("X", _P), ("n", _I64), ("k", _I32), ("C_init", _P), ("C", _P), ("idx", _P), ("counts", _P),
                 ("distortion", _P), ("codes", _P), ("levels", _P), ("C_hat", _P), ("packed_idx", _P),
                 ("packed_codes", _P), ("W_hat", _P), ("sq_error", _P)]
+
+
+class KqDistillArgs(ctypes.Structure):
+    _fields_ = [("Z", _P), ("type", _I32), ("ldz", _I64), ("m", _I64), ("v", _I64), ("top_values", _P), ("top_type", _I32),
+                ("top_idx", _P), ("idx_bytes", _I32), ("top", _I32), ("labels", _P), ("label_bytes", _I32),
+                ("temperature", ctypes.c_float), ("alpha", ctypes.c_float)]
 
 
 def _load():
@@ -122,6 +132,18 @@ def _load():
         "kq_checkpoint_grad_scales": ([_P, _I32, _I64, _I64, _I64, _I64, _P, _P, _P, _P, _I32, _P, _P, _P, _SZ, _P],
                                       _I32),
         "kq_checkpoint_grad_weight": ([_P, _I32, _I64, _I64, _I64, _I64, _P, _P, _P, _I64, _P, _P, _SZ, _P], _I32),
+        "kq_quantize_blocks": ([_P, _I32, _I64, _I64, _I64, _I32, _P, _P, _P], _I32),
+        "kq_reconstruct_blocks": ([_P, _P, _I64, _I64, _I32, _I32, _P, _I64, _P], _I32),
+        "kq_block_linear_workspace_bytes": ([_I32, _I32, _I64, _I64, _I64], _SZ),
+        "kq_block_linear": ([_P, _I32, _I64, _P, _I64, _I64, _I64, _P, _P, _P, _P, _I32, _I64, _P, _SZ, _P], _I32),
+        "kq_block_linear_grad_input_workspace_bytes": ([_I32, _I64, _I64, _I64], _SZ),
+        "kq_block_linear_grad_input": ([_P, _I32, _I64, _I64, _I64, _I64, _P, _P, _P, _I64, _P, _SZ, _P], _I32),
+        "kq_block_linear_grad_weight_workspace_bytes": ([_I32, _I64, _I64, _I64], _SZ),
+        "kq_block_linear_grad_weight": ([_P, _I32, _I64, _I64, _I64, _I64, _P, _P, _P, _I32, _I64, _P, _P, _SZ, _P], _I32),
+        "kq_distill_workspace_bytes": ([_I64, _I64, _I32], _SZ),
+        "kq_distill": ([_P, _P, ctypes.c_float, _P, _P, _I64, _P, _SZ, _P], _I32),
+        "kq_distill_loss": ([_P, _P, _P, _P, _SZ, _P], _I32),
+        "kq_distill_grad": ([_P, _P, _P, ctypes.c_float, _P, _I64, _P], _I32),
         "kq_fit_layer_noalloc_max_bytes": ([], _SZ),
         "kq_fit_layer_noalloc": ([_P, _I64, _I32, _I32, _P, _I32, _P, _P, _P, _P, _U32, _P], _I32),
     }
@@ -163,10 +185,15 @@ EXPORTED = ["kq_status_string", "kq_abi_version", "kq_workspace_bytes", "kq_stac
             "kq_group_code_bytes", "kq_quantize_groups", "kq_reconstruct_groups", "kq_group_linear_workspace_bytes",
             "kq_group_linear", "kq_group_linear_grad_input_workspace_bytes", "kq_group_linear_grad_input",
             "kq_checkpoint_pack", "kq_checkpoint_restore", "kq_checkpoint_grad_workspace_bytes",
-            "kq_checkpoint_grad_scales", "kq_checkpoint_grad_weight"]
+            "kq_checkpoint_grad_scales", "kq_checkpoint_grad_weight", "kq_quantize_blocks", "kq_reconstruct_blocks",
+            "kq_block_linear_workspace_bytes", "kq_block_linear", "kq_block_linear_grad_input_workspace_bytes",
+            "kq_block_linear_grad_input", "kq_block_linear_grad_weight_workspace_bytes", "kq_block_linear_grad_weight",
+            "kq_distill_workspace_bytes", "kq_distill", "kq_distill_loss", "kq_distill_grad"]
 KQ_MAX_PACK_JOBS = 32
-KQ_T_F32, KQ_T_BF16, KQ_T_F16 = 0, 1, 2
+KQ_T_F32, KQ_T_BF16, KQ_T_F16, KQ_T_E4M3 = 0, 1, 2, 3
 KQ_CHECKPOINT_GROUP = 32
+KQ_BLOCK = 128
+KQ_DISTILL_MAX_TOP = 256
 
 
 class KqError(RuntimeError):
@@ -1249,3 +1276,283 @@ class GroupLinear:
     def weight(self, dtype=torch.float32):
         """The weights that the layer stands for."""
         return kq_reconstruct_groups(self.codes, self.scales, self.in_features, self.group, self.levels, dtype)
+
+
+# ---- fully-connected layers in 8-bit floats ------------------------------------------------------
+
+_E4M3 = torch.float8_e4m3fn
+
+
+def block_shapes(m: int, k: int, rows: int = 1):
+    """Shapes of the values and exponents of an [m, k] matrix in blocks of `rows` (1 or 128) by 128."""
+    if rows not in (1, KQ_BLOCK):
+        raise ValueError(f"rows must be 1 or {KQ_BLOCK}, got {rows}")
+    kb = -(-k // KQ_BLOCK)
+    return (m, kb * KQ_BLOCK), (-(-m // rows), kb)
+
+
+def _type_number(dtype):
+    ty = _TYPES.get(dtype)
+    if ty is None:
+        raise TypeError(f"dtype must be one of {', '.join(str(d) for d in _TYPES)}, got {dtype}")
+    return ty
+
+
+def _blocks(values, exps, k, rows, name):
+    """Checks an 8-bit matrix; returns (m, k)."""
+    if not isinstance(values, torch.Tensor) or values.dim() != 2:
+        raise TypeError(f"{name} must be a [rows, columns] tensor")
+    m = values.shape[0]
+    k = values.shape[1] if k is None else int(k)
+    if k < 1:
+        raise ValueError(f"{name} must have columns")
+    vs, es = block_shapes(m, k, rows)
+    _dev(values, _E4M3, name, vs)
+    _dev(exps, torch.uint8, "the exponents of " + name, es)
+    _same_device(values.device, **{"the exponents of " + name: exps})
+    return m, k
+
+
+def kq_quantize_blocks(X, rows: int = 1, values=None, exps=None):
+    """A matrix [..., k] (fp32, bf16 or fp16; a matrix may have strided rows) in 8-bit floats with a power of two for each
+    block of `rows` rows (1: activations, 128: weights) by 128 columns.  Returns (values float8_e4m3fn [m, k rounded up to
+    128], exps uint8 [ceil(m / rows), ceil(k / 128)]); include/kq.h has the formulas."""
+    x, ty, ld = _rows(X, _TYPES, "X")
+    m, k = x.shape
+    dev = x.device
+    vs, es = block_shapes(m, k, rows)
+    values = torch.empty(vs, dtype=_E4M3, device=dev) if values is None else _dev(values, _E4M3, "values", vs)
+    exps = torch.empty(es, dtype=torch.uint8, device=dev) if exps is None else _dev(exps, torch.uint8, "exps", es)
+    _same_device(dev, values=values, exps=exps)
+    _check(lib.kq_quantize_blocks(x.data_ptr(), ty, ld, m, k, rows, values.data_ptr(), exps.data_ptr(), _stream(dev)),
+           "kq_quantize_blocks")
+    return values, exps
+
+
+def kq_reconstruct_blocks(values, exps, in_features: int, rows: int = 1, dtype=torch.float32, X_hat=None):
+    """What values and exponents stand for, [m, in_features] of `dtype` (or X_hat's)."""
+    m, k = _blocks(values, exps, in_features, rows, "values")
+    dev = values.device
+    if X_hat is None:
+        _type_number(dtype)
+        X_hat = torch.empty(m, k, dtype=dtype, device=dev)
+    out, ty, ld = _rows(X_hat, _TYPES, "X_hat", k)
+    if out.shape[0] != m:
+        raise ValueError(f"X_hat must have {m} rows")
+    _same_device(dev, X_hat=X_hat)
+    _check(lib.kq_reconstruct_blocks(values.data_ptr(), exps.data_ptr(), m, k, rows, ty, out.data_ptr(), ld, _stream(dev)),
+           "kq_reconstruct_blocks")
+    return X_hat
+
+
+def _typed_rows(out, dtype, dev, lead, cols, name):
+    """An output of lead + (cols,) values of a type: given, or allocated.  Returns (out, matrix, type, pitch)."""
+    if out is None:
+        _type_number(dtype)
+        out = torch.empty(*lead, cols, dtype=dtype, device=dev)
+    elif tuple(out.shape) != (*lead, cols):
+        raise ValueError(f"{name} must have shape {(*lead, cols)}, got {tuple(out.shape)}")
+    t, ty, ld = _rows(out, _TYPES, name, cols)
+    _same_device(dev, **{name: out})
+    return out, t, ty, ld
+
+
+def kq_block_linear(X, values, exps, bias=None, x_exps=None, dtype=None, Y=None, workspace=None):
+    """Y = X_hat W_hat^T + bias for a weight [n, k] as kq_quantize_blocks(W, rows=128) leaves it.  X [..., k] is fp32, bf16 or
+    fp16 and quantized on the way, or it is the values of kq_quantize_blocks(X) with x_exps its exponents.  bias fp32 [n] or
+    None; Y [..., n] of `dtype` (X's type, or bf16 for 8-bit values).  From one row (a token) to any number of them."""
+    if x_exps is None:
+        x, xt, ldx = _rows(X, _TYPES, "X")
+        m, k = x.shape
+        lead = X.shape[:-1]
+    else:
+        m, k = _blocks(X, x_exps, None, 1, "X")
+        x, xt, ldx, lead = X, KQ_T_E4M3, k, (m,)
+    dev = x.device
+    n, _ = _blocks(values, exps, k, KQ_BLOCK, "values")
+    if n == 0:
+        raise ValueError("values must have rows")
+    if bias is not None:
+        _dev(bias, torch.float32, "bias", (n,))
+    _same_device(dev, values=values, bias=bias)
+    if dtype is None:
+        dtype = Y.dtype if isinstance(Y, torch.Tensor) else torch.bfloat16 if xt == KQ_T_E4M3 else X.dtype
+    elif Y is not None and Y.dtype != dtype:
+        raise TypeError(f"Y must be {dtype}, got {Y.dtype}")
+    Y, y, yt, ldy = _typed_rows(Y, dtype, dev, lead, n, "Y")
+    wp, wn = _scratch_for(dev, lib.kq_block_linear_workspace_bytes(xt, yt, m, n, k), workspace)
+    _check(lib.kq_block_linear(x.data_ptr(), xt, ldx, _ptr(x_exps), m, n, k, values.data_ptr(), exps.data_ptr(), _ptr(bias),
+                               y.data_ptr(), yt, ldy, wp, wn, _stream(dev)), "kq_block_linear")
+    return Y
+
+
+def kq_block_linear_grad_input(dY, values, exps, in_features: int, dX=None, workspace=None):
+    """dX = dY_hat W_hat: dY [..., n] fp32, bf16 or fp16, quantized on the way in blocks of 128 of its columns; dX
+    [..., in_features] in its type."""
+    dy, ty, ldy = _rows(dY, _TYPES, "dY")
+    m = dy.shape[0]
+    n, k = _blocks(values, exps, in_features, KQ_BLOCK, "values")
+    dev = dy.device
+    if dy.shape[1] != n:
+        raise ValueError(f"dY must have {n} columns, got {dy.shape[1]}")
+    _same_device(dev, values=values)
+    dX, dx, ldx = _out_rows(dX, dY, dY.shape[:-1], k, _TYPES, "dX")
+    wp, wn = _scratch_for(dev, lib.kq_block_linear_grad_input_workspace_bytes(ty, m, n, k), workspace)
+    _check(lib.kq_block_linear_grad_input(dy.data_ptr(), ty, ldy, m, n, k, values.data_ptr(), exps.data_ptr(), dx.data_ptr(),
+                                          ldx, wp, wn, _stream(dev)), "kq_block_linear_grad_input")
+    return dX
+
+
+def kq_block_linear_grad_weight(dY, x_values, x_exps, in_features: int, bias: bool = False, dtype=torch.float32, dW=None,
+                                dbias=None, workspace=None):
+    """Gradient of the weight, dY^T X (`dtype` [n, in_features]), from dY [..., n] (fp32, bf16 or fp16) and the values that
+    kq_quantize_blocks(X) gives: both are quantized along the rows, in blocks of 128 rows by 1 column.  bias: also the
+    column sums of dY (fp32, not quantized).  Returns (dW, dbias or None)."""
+    m, k = _blocks(x_values, x_exps, in_features, 1, "x_values")
+    dy, ty, ldy = _rows(dY, _TYPES, "dY")
+    n, dev = dy.shape[1], dy.device
+    if dy.shape[0] != m:
+        raise ValueError(f"dY must have {m} rows as x_values, got {dy.shape[0]}")
+    _same_device(dev, x_values=x_values)
+    if dW is not None:
+        dtype = dW.dtype
+    dW, dw, wt, ldw = _typed_rows(dW, dtype, dev, (n,), k, "dW")
+    dbias = _bias_out(dev, n, bias, dbias)
+    wp, wn = _scratch_for(dev, lib.kq_block_linear_grad_weight_workspace_bytes(wt, m, n, k), workspace)
+    _check(lib.kq_block_linear_grad_weight(dy.data_ptr(), ty, ldy, m, n, k, x_values.data_ptr(), x_exps.data_ptr(),
+                                           dw.data_ptr(), wt, ldw, _ptr(dbias), wp, wn, _stream(dev)),
+           "kq_block_linear_grad_weight")
+    return dW, dbias
+
+
+class BlockLinear:
+    """A fully-connected layer in 8-bit floats: e4m3 values with a power of two for each 128 x 128 block, an fp32 master
+    copy of the weight for training (master=True) and an fp32 bias or None, on the weight's device.
+
+    ``layer(X)`` is the serving call.  ``layer.forward(X)`` also returns the 8-bit values of X that
+    ``layer.backward(dY, kept)`` takes the weight's gradient from; ``layer.step`` moves the master copy and the bias
+    against them and quantizes the weight again.  Not an autograd function: an X that requires a gradient gets it
+    from ``layer.backward``."""
+
+    def __init__(self, W, bias=None, master: bool = False):
+        self.out_features, self.in_features = W.shape
+        self.values, self.exps = kq_quantize_blocks(W, KQ_BLOCK)
+        self.master = W.float().clone() if master else None
+        self.bias = None if bias is None else _dev(bias, torch.float32, "bias", (self.out_features,)).clone()
+
+    def __call__(self, X, dtype=None):
+        return kq_block_linear(X, self.values, self.exps, self.bias, dtype=dtype)
+
+    def forward(self, X, dtype=None):
+        """(Y, the 8-bit values and exponents of X)."""
+        x = kq_quantize_blocks(X)
+        Y = kq_block_linear(x[0], self.values, self.exps, self.bias, x[1], dtype or X.dtype)
+        return Y.view(*X.shape[:-1], self.out_features), x
+
+    def backward(self, dY, kept, input_grad: bool = True, dtype=torch.float32):
+        """(dX or None, dW of `dtype`, dbias fp32 or None)."""
+        dX = kq_block_linear_grad_input(dY, self.values, self.exps, self.in_features) if input_grad else None
+        dW, db = kq_block_linear_grad_weight(dY, *kept, self.in_features, self.bias is not None, dtype)
+        return dX, dW, db
+
+    def step(self, dW, dbias, gamma: float):
+        """master -= gamma * dW, and quantized into the weight; bias -= gamma * dbias."""
+        if self.master is None:
+            raise ValueError("the layer was made without a master copy of its weight")
+        self.master.sub_(dW, alpha=float(gamma))
+        kq_quantize_blocks(self.master, KQ_BLOCK, self.values, self.exps)
+        if self.bias is not None and dbias is not None:
+            self.bias.sub_(dbias, alpha=float(gamma))
+
+    def weight(self, dtype=torch.float32):
+        """The weights that the layer stands for."""
+        return kq_reconstruct_blocks(self.values, self.exps, self.in_features, KQ_BLOCK, dtype)
+
+
+# ---- distillation from a teacher's top logits ----------------------------------------------------
+
+_INDEX = {torch.int32: 4, torch.int64: 8}
+
+
+def _distill_args(Z, top_values, top_idx, temperature, labels, alpha):
+    """Checks the inputs; returns (the descriptor, matrix of Z, tensors to keep until the call)."""
+    z, ty, ldz = _rows(Z, _TYPES, "Z")
+    m, v = z.shape
+    for name, t, types in (("top_values", top_values, _TYPES), ("top_idx", top_idx, _INDEX)):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+        if t.dtype not in types:
+            raise TypeError(f"{name} must be one of {', '.join(str(d) for d in types)}, got {t.dtype}")
+        if t.dim() == 0 or tuple(t.shape[:-1]) != tuple(Z.shape[:-1]):
+            raise ValueError(f"{name} must have the rows of Z, {tuple(Z.shape[:-1])}, got {tuple(t.shape)}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    if top_values.shape != top_idx.shape:
+        raise ValueError("top_values and top_idx must have one shape")
+    if labels is not None:
+        if not isinstance(labels, torch.Tensor) or not labels.is_cuda or labels.dtype not in _INDEX:
+            raise TypeError("labels must be a CUDA (HIP) tensor of int32 or int64")
+        if tuple(labels.shape) != tuple(Z.shape[:-1]) or not labels.is_contiguous():
+            raise ValueError(f"labels must be contiguous and one for each row of Z, {tuple(Z.shape[:-1])}")
+    elif alpha > 0:
+        raise ValueError("alpha above 0 needs labels")
+    _same_device(z.device, top_values=top_values, top_idx=top_idx, labels=labels)
+    return KqDistillArgs(z.data_ptr(), ty, ldz, m, v, top_values.data_ptr(), _TYPES[top_values.dtype], top_idx.data_ptr(),
+                         _INDEX[top_idx.dtype], top_values.shape[-1], _ptr(labels),
+                         _INDEX[labels.dtype] if labels is not None else 0, temperature, alpha), z
+
+
+def _row_floats(t, dev, m, name):
+    if t is None:
+        return torch.empty(m, dtype=torch.float32, device=dev)
+    _same_device(dev, **{name: t})
+    return _dev(t, torch.float32, name, (m,))
+
+
+def kq_distill(Z, top_values, top_idx, temperature: float = 1.0, labels=None, alpha: float = 0.0, scale: float = 1.0,
+               dloss=None, loss=None, dZ=None, workspace=None):
+    """The loss of every row of logits Z [..., v] against the teacher's top logits (top_values [..., top] of any float
+    type at top_idx, int32 or int64) and, with weight alpha, its labels, and the gradient of sum_row d[row] loss[row]: d is
+    dloss (fp32, one a row) or `scale` for all rows (1 / rows for the mean).  Entries and labels outside [0, v) are absent.
+    Returns (loss fp32 [rows], dZ like Z; dZ may be Z).  include/kq.h has the formulas."""
+    a, z = _distill_args(Z, top_values, top_idx, temperature, labels, alpha)
+    dev, m = z.device, z.shape[0]
+    if dloss is not None:
+        _row_floats(dloss, dev, m, "dloss")
+    loss = _row_floats(loss, dev, m, "loss")
+    dZ, dz, lddz = _out_rows(dZ, Z, Z.shape[:-1], z.shape[1], _TYPES, "dZ")
+    wp, wn = _scratch_for(dev, lib.kq_distill_workspace_bytes(m, z.shape[1], a.top), workspace)
+    _check(lib.kq_distill(ctypes.byref(a), _ptr(dloss), scale, loss.data_ptr(), dz.data_ptr(), lddz, wp, wn, _stream(dev)),
+           "kq_distill")
+    return loss, dZ
+
+
+def kq_distill_loss(Z, top_values, top_idx, temperature: float = 1.0, labels=None, alpha: float = 0.0, loss=None, stats=None,
+                    workspace=None):
+    """The loss alone: (loss fp32 [rows], stats fp32 [rows, 3] for kq_distill_grad)."""
+    a, z = _distill_args(Z, top_values, top_idx, temperature, labels, alpha)
+    dev, m = z.device, z.shape[0]
+    loss = _row_floats(loss, dev, m, "loss")
+    if stats is None:
+        stats = torch.empty(m, 3, dtype=torch.float32, device=dev)
+    _dev(stats, torch.float32, "stats", (m, 3))
+    _same_device(dev, stats=stats)
+    wp, wn = _scratch_for(dev, lib.kq_distill_workspace_bytes(m, z.shape[1], a.top), workspace)
+    _check(lib.kq_distill_loss(ctypes.byref(a), loss.data_ptr(), stats.data_ptr(), wp, wn, _stream(dev)), "kq_distill_loss")
+    return loss, stats
+
+
+def kq_distill_grad(Z, top_values, top_idx, stats, dloss=None, temperature: float = 1.0, labels=None, alpha: float = 0.0,
+                    scale: float = 1.0, dZ=None):
+    """The gradient of the logits from what kq_distill_loss kept: dloss fp32 [rows], or None for `scale` in all of them.
+    dZ may be Z."""
+    a, z = _distill_args(Z, top_values, top_idx, temperature, labels, alpha)
+    dev, m = z.device, z.shape[0]
+    _dev(stats, torch.float32, "stats", (m, 3))
+    _same_device(dev, stats=stats)
+    if dloss is not None:
+        _row_floats(dloss, dev, m, "dloss")
+    dZ, dz, lddz = _out_rows(dZ, Z, Z.shape[:-1], z.shape[1], _TYPES, "dZ")
+    _check(lib.kq_distill_grad(ctypes.byref(a), stats.data_ptr(), _ptr(dloss), scale, dz.data_ptr(), lddz, _stream(dev)),
+           "kq_distill_grad")
+    return dZ

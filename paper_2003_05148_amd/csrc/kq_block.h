@@ -1,0 +1,136 @@
+// Fully-connected layers in 8-bit floats (e4m3) with a power of two for each block of 128: what the translation
+// units share.
+//
+// Every product is out[j][i] = sum_c A[i][c] B[j][c] of two operands held the same way: rows of e4m3 values along the
+// contraction, their pitch a multiple of 128 bytes with zeros past the end, and one exponent byte for 128 of them.  So
+// a kernel has no edges along the contraction, every row is aligned, and a block's exponent is one byte of the scaled
+// matrix instruction (or one factor of a decoded operand).
+//   linear       Y[m][n]   i = n, j = m, c = k   A = W (128 x 128 blocks), B = X
+//   grad input   dX[m][k]  i = k, j = m, c = n   A = W^T (its bytes transposed, the same blocks), B = dY
+//   grad weight  dW[n][k]  i = k, j = n, c = m   A = X^T, B = dY^T, both quantized along m
+#pragma once
+
+#include "kq_group.h"
+
+namespace kq {
+
+constexpr int kBlock = KQ_BLOCK;
+
+inline __host__ __device__ int64_t block_pitch(int64_t k) { return (k + kBlock - 1) / kBlock * kBlock; }
+
+// The biased exponent of a block from the bits of its largest magnitude (255: not finite).
+__device__ __forceinline__ unsigned block_exponent(unsigned a) {
+    if (a >= 0x7f800000u) return 255u;
+    const int e = (int)(a >> 23) - 8 + ((a & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return (unsigned)(e < 1 ? 1 : e);
+}
+// 2^-e, for 1 <= biased <= 254
+__device__ __forceinline__ float block_inverse(unsigned biased) { return __builtin_bit_cast(float, (254u - biased) << 23); }
+
+// Four fp32 values times inv (exact: a power of two) to four bytes.  Their magnitude is at most 448 then.
+__device__ __forceinline__ unsigned encode4(float a, float b, float c, float d, float inv) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
+}
+constexpr unsigned kNaN4 = 0x7f7f7f7fu;
+
+// Eight bytes times a power of two as bf16, which holds them exactly (but for magnitudes below 2^-126).
+__device__ __forceinline__ u32x4 decode8(unsigned lo, unsigned hi, float scale) {
+    return u32x4{__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false)),
+                 __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true)),
+                 __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false)),
+                 __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true))};
+}
+
+// ---- device parameters and launchers (checked by the C entry points before) ------------------------
+
+struct BlockQuantizeParams {
+    const void* X;
+    int64_t ldx;
+    int type;
+    int64_t m;
+    int64_t k, kp;
+    uint8_t* values;
+    uint8_t* exps;
+};
+hipError_t launch_quantize_blocks(const BlockQuantizeParams& p, int rows, hipStream_t s);
+
+struct BlockReconstructParams {
+    const uint8_t* values;
+    const uint8_t* exps;
+    int64_t m, k, kp;
+    int rows;
+    void* X_hat;
+    int64_t ldx;
+    int type;
+};
+hipError_t launch_reconstruct_blocks(const BlockReconstructParams& p, hipStream_t s);
+
+// out[c][r], r along the 128-row blocks of X, pitch rp (a multiple of 128, zeros past m).  Quantized along r again, or
+// (exps NULL: a weight) the same bytes.
+struct BlockTransposeParams {
+    const void* X;        // [m][cols], or bytes of pitch ldx with in_exps [m][ldx / 128]
+    int64_t ldx;
+    int type;             // KQ_T_*
+    const uint8_t* in_exps;
+    int64_t m, cols, rp;
+    uint8_t* values;      // [cols][rp]
+    uint8_t* exps;        // [cols][rp / 128], or NULL
+    float* sums;          // [rp / 128][cols]: sums over each 128 rows, or NULL
+};
+hipError_t launch_transpose_blocks(const BlockTransposeParams& p, hipStream_t s);
+
+struct BlockOperand {
+    const uint8_t* v;
+    int64_t pitch;
+    const uint8_t* e;        // exponent of row r, block b: e[r * e_row + b * e_col], r / 128 for r in the 128 x 128 form
+    int64_t e_row, e_col;
+};
+struct BlockGemmParams {
+    BlockOperand A, B;
+    int64_t I, J;
+    int steps;               // blocks of the contraction
+    const float* bias;       // [I] or NULL
+    void* out;
+    int type;                // of out
+    int64_t ldo;
+    float* part;             // partial sums of a split contraction, or NULL
+    int splits, steps_per_split;
+    int itiles, jtiles;
+};
+struct BlockGemmPlan {
+    int bi, bj;              // output tile
+    int splits, steps_per_split;
+    size_t part_bytes;
+};
+// exact: products on the 16-bit matrix instructions
+BlockGemmPlan block_gemm_plan(bool exact, int64_t I, int64_t J, int64_t C);
+// a_rows: A's blocks are 1 x 128 (else 128 x 128)
+hipError_t launch_block_gemm(bool exact, bool a_rows, const BlockGemmPlan& plan, BlockGemmParams p, void* part, hipStream_t s);
+
+// Y = X W^T for at most kBlockMatvecRows rows of X.
+constexpr int kBlockMatvecRows = 16;
+struct BlockMatvecParams {
+    const uint8_t* values;   // W
+    const uint8_t* exps;
+    int64_t n, k, kp;
+    const void* X;           // of x_type; KQ_T_E4M3 with x_exps
+    int x_type;
+    int64_t ldx;
+    const uint8_t* x_exps;
+    int m;
+    const float* bias;
+    void* Y;
+    int y_type;
+    int64_t ldy;
+    float* part;             // partial sums [splits][m][n], or NULL
+    int splits, blocks_per_split;
+};
+struct BlockMatvecPlan {
+    int row_tiles, waves, splits, blocks_per_split;
+    size_t ws_bytes;
+};
+BlockMatvecPlan block_matvec_plan(int m, int64_t n, int64_t k);
+hipError_t launch_block_matvec(const BlockMatvecPlan& plan, BlockMatvecParams p, hipStream_t s);
+
+}  // namespace kq

@@ -113,6 +113,17 @@ __device__ __forceinline__ unsigned look_up(const unsigned (&t)[4], unsigned low
     return __builtin_amdgcn_perm(__builtin_amdgcn_perm(t[3], t[2], low3), __builtin_amdgcn_perm(t[1], t[0], low3), pick);
 }
 
+// Memory of the two kinds as the direct load to LDS takes it.
+using lds_ptr = __attribute__((address_space(3))) void*;
+using global_ptr = const __attribute__((address_space(1))) void*;
+
+// Workgroups are dealt to the eight XCDs in turn; tile numbers are dealt so that an XCD's workgroups take
+// neighbouring tiles (their operands meet in its L2).  A bijection for any count.
+__device__ __forceinline__ int xcd_tile(int b, int count) {
+    const int per = count >> 3, rest = count & 7, x = b & 7;
+    return x * per + min(x, rest) + (b >> 3);
+}
+
 // ---- device parameters and launchers (checked by the C entry points before) ------------------------
 
 struct GroupWeights {

@@ -1,94 +1,8 @@
 // The 4-bit group quantizer, the weights it stands for, 8-bit activation checkpoints and the sums of
 // split products: passes over memory.
-#include "kq_group.h"
+#include "kq_values.h"
 
 namespace kq {
-
-// ---- element access by type --------------------------------------------------------------------------
-
-// N consecutive values at any alignment of their type, as fp32
-template <int TYPE, int N>
-__device__ __forceinline__ void load_values(const void* base, int64_t at, float (&v)[N]) {
-    if constexpr (TYPE == KQ_T_F32) {
-        __builtin_memcpy(v, (const float*)base + at, 4 * N);
-    } else {
-        unsigned h[N / 2];
-        __builtin_memcpy(h, (const uint16_t*)base + at, 2 * N);
-#pragma unroll
-        for (int t = 0; t < N / 2; ++t) {
-            v[2 * t] = Act<TYPE == KQ_T_BF16>::lo(h[t]);
-            v[2 * t + 1] = Act<TYPE == KQ_T_BF16>::hi(h[t]);
-        }
-    }
-}
-template <int TYPE>
-__device__ __forceinline__ float load_value_as(const void* base, int64_t at) {
-    if constexpr (TYPE == KQ_T_F32) return ((const float*)base)[at];
-    else return Act<TYPE == KQ_T_BF16>::lo(((const uint16_t*)base)[at]);
-}
-// 4-byte aligned pieces of a stream that is written once and not read soon: past the caches' normal ways
-// (fp32 weights of 4096 x 25088 rebuilt: 75 us, 131 us with ordinary stores).
-__device__ __forceinline__ void stream_store(void* at, const unsigned* v, int words) {
-    if (words == 4) {
-        using u32x4_a4 = __attribute__((ext_vector_type(4), aligned(4))) unsigned;
-        __builtin_nontemporal_store((u32x4_a4){v[0], v[1], v[2], v[3]}, (u32x4_a4*)at);
-    } else {
-        using u32x2_a4 = __attribute__((ext_vector_type(2), aligned(4))) unsigned;
-        __builtin_nontemporal_store((u32x2_a4){v[0], v[1]}, (u32x2_a4*)at);
-    }
-}
-
-template <int TYPE, int N>
-__device__ __forceinline__ void store_values(void* base, int64_t at, const float (&v)[N], int count) {
-    if constexpr (TYPE == KQ_T_F32) {
-        float* o = (float*)base + at;
-        if (count >= N) {
-            unsigned h[N];
-            __builtin_memcpy(h, v, 4 * N);
-#pragma unroll
-            for (int t = 0; t < N; t += 4) stream_store(o + t, h + t, 4);
-        } else {
-#pragma unroll
-            for (int t = 0; t < N; ++t)
-                if (t < count) o[t] = v[t];
-        }
-    } else {
-        uint16_t* o = (uint16_t*)base + at;
-        if (count >= N) {
-            unsigned h[N / 2];
-#pragma unroll
-            for (int t = 0; t < N / 2; ++t) h[t] = Act<TYPE == KQ_T_BF16>::pack(v[2 * t], v[2 * t + 1]);
-            if (((uintptr_t)o & 3) == 0) stream_store(o, h, N / 2);
-            else __builtin_memcpy(o, h, 2 * N);
-        } else {
-#pragma unroll
-            for (int t = 0; t < N; ++t)
-                if (t < count) o[t] = Act<TYPE == KQ_T_BF16>::one(v[t]);
-        }
-    }
-}
-
-// 8 columns at c0 of a row, zeros past the row's `limit`
-template <int TYPE>
-__device__ __forceinline__ void load_columns(const void* base, int64_t row_at, int c0, int limit, float (&v)[8]) {
-    if (c0 + 8 <= limit) {
-        load_values<TYPE, 8>(base, row_at + c0, v);
-    } else {
-#pragma unroll
-        for (int t = 0; t < 8; ++t) v[t] = c0 + t < limit ? load_value_as<TYPE>(base, row_at + c0 + t) : 0.0f;
-    }
-}
-
-// max |v| as fp32 bits without the sign: an infinity or NaN is larger than every finite value
-__device__ __forceinline__ unsigned max_bits(const float (&v)[8]) {
-    unsigned a = 0;
-#pragma unroll
-    for (int t = 0; t < 8; ++t) {
-        const unsigned b = __builtin_bit_cast(unsigned, v[t]) & 0x7fffffffu;
-        a = b > a ? b : a;
-    }
-    return a;
-}
 
 // ---- quantizer -----------------------------------------------------------------------------------------
 // A workgroup a 16 x 128 tile, sixteen lanes a row, 8 neighbouring columns and one dword of codes a lane, four rows a

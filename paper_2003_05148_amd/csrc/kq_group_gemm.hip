@@ -235,8 +235,6 @@ struct StageA {
 
 // A step of B from memory to LDS: a wave's instruction takes 64 chunks of 16 bytes, eight rows; lane l writes
 // chunk l of them, so it reads the chunk that belongs there.
-using lds_ptr = __attribute__((address_space(3))) void*;
-using global_ptr = const __attribute__((address_space(1))) void*;
 template <int BJ, int WAVES>
 struct DirectB {
     static constexpr int N = BJ / 8 / WAVES;
@@ -263,13 +261,6 @@ struct DirectB {
         }
     }
 };
-
-// Workgroups are dealt to the eight XCDs in turn; tile numbers are dealt so that an XCD's workgroups take
-// neighbouring tiles (their operands meet in its L2).  A bijection for any count.
-__device__ __forceinline__ int xcd_tile(int b, int count) {
-    const int per = count >> 3, rest = count & 7, x = b & 7;
-    return x * per + min(x, rest) + (b >> 3);
-}
 
 template <bool BF, bool LUT, int MODE, int BI, int BJ, int WI, int WJ>
 __global__ __launch_bounds__(64 * WI * WJ) void group_gemm_kernel(const GemmParams p) {
