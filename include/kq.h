@@ -748,17 +748,18 @@ kq_status kq_block_linear_grad_weight(const void* dY, int32_t type, int64_t ldy,
  *   A NaN or +infinity in a row makes its loss and gradient NaN; -infinity in Z is a class that is masked out (gradient
  *   0, or the teacher's share: its loss is infinite then).
  *   1 <= v <= KQ_DISTILL_MAX_CLASSES, 1 <= top <= KQ_DISTILL_MAX_TOP, 0 <= m <= KQ_GROUP_MAX_ROWS,
- *   2^-10 <= temperature <= 2^20 (else KQ_ERR_UNSUPPORTED), 0 <= alpha <= 1; alpha > 0 needs labels.
+ *   m v <= KQ_DISTILL_MAX_LOGITS, 2^-10 <= temperature <= 2^20 (else KQ_ERR_UNSUPPORTED), 0 <= alpha <= 1; alpha > 0 needs labels.
  *
  * kq_distill -- loss device [m] fp32 and dZ [m][v] (Z's type, pitch lddz; dZ may be Z).
  * kq_distill_loss -- loss, and stats device [m][3] fp32 for the gradient: the row's largest logit, the sum of
  *   exp((z - largest) / T) and that of exp(z - largest) (0 where it is not needed).
  * kq_distill_grad -- dZ (may be Z) from the same inputs, stats and dloss (device [m] fp32, or NULL for `scale`).
- *   Sums in fp32, in an order that the sizes alone decide.
- *   workspace: kq_distill_workspace_bytes(m, v, top) (may be 0).
+ *   Sums in fp32, in an order that the sizes and the alignment of Z's rows decide.
+ *   workspace: kq_distill_workspace_bytes(type, m, v, top) (may be 0).
  */
 #define KQ_DISTILL_MAX_CLASSES (1 << 24)
 #define KQ_DISTILL_MAX_TOP 256
+#define KQ_DISTILL_MAX_LOGITS ((int64_t)1 << 38)
 typedef struct kq_distill_args {
     const void* Z;
     int32_t type;
@@ -772,7 +773,7 @@ typedef struct kq_distill_args {
     int32_t label_bytes;
     float temperature, alpha;
 } kq_distill_args;
-size_t kq_distill_workspace_bytes(int64_t m, int64_t v, int32_t top);
+size_t kq_distill_workspace_bytes(int32_t type, int64_t m, int64_t v, int32_t top);
 kq_status kq_distill(const kq_distill_args* args /* host */, const float* dloss, float scale, float* loss, void* dZ,
                      int64_t lddz, void* ws, size_t ws_bytes, void* stream);
 kq_status kq_distill_loss(const kq_distill_args* args /* host */, float* loss, float* stats, void* ws, size_t ws_bytes,

@@ -140,7 +140,7 @@ def _load():
         "kq_block_linear_grad_input": ([_P, _I32, _I64, _I64, _I64, _I64, _P, _P, _P, _I64, _P, _SZ, _P], _I32),
         "kq_block_linear_grad_weight_workspace_bytes": ([_I32, _I64, _I64, _I64], _SZ),
         "kq_block_linear_grad_weight": ([_P, _I32, _I64, _I64, _I64, _I64, _P, _P, _P, _I32, _I64, _P, _P, _SZ, _P], _I32),
-        "kq_distill_workspace_bytes": ([_I64, _I64, _I32], _SZ),
+        "kq_distill_workspace_bytes": ([_I32, _I64, _I64, _I32], _SZ),
         "kq_distill": ([_P, _P, ctypes.c_float, _P, _P, _I64, _P, _SZ, _P], _I32),
         "kq_distill_loss": ([_P, _P, _P, _P, _SZ, _P], _I32),
         "kq_distill_grad": ([_P, _P, _P, ctypes.c_float, _P, _I64, _P], _I32),
@@ -1521,7 +1521,7 @@ def kq_distill(Z, top_values, top_idx, temperature: float = 1.0, labels=None, al
         _row_floats(dloss, dev, m, "dloss")
     loss = _row_floats(loss, dev, m, "loss")
     dZ, dz, lddz = _out_rows(dZ, Z, Z.shape[:-1], z.shape[1], _TYPES, "dZ")
-    wp, wn = _scratch_for(dev, lib.kq_distill_workspace_bytes(m, z.shape[1], a.top), workspace)
+    wp, wn = _scratch_for(dev, lib.kq_distill_workspace_bytes(a.type, m, z.shape[1], a.top), workspace)
     _check(lib.kq_distill(ctypes.byref(a), _ptr(dloss), scale, loss.data_ptr(), dz.data_ptr(), lddz, wp, wn, _stream(dev)),
            "kq_distill")
     return loss, dZ
@@ -1537,7 +1537,7 @@ def kq_distill_loss(Z, top_values, top_idx, temperature: float = 1.0, labels=Non
         stats = torch.empty(m, 3, dtype=torch.float32, device=dev)
     _dev(stats, torch.float32, "stats", (m, 3))
     _same_device(dev, stats=stats)
-    wp, wn = _scratch_for(dev, lib.kq_distill_workspace_bytes(m, z.shape[1], a.top), workspace)
+    wp, wn = _scratch_for(dev, lib.kq_distill_workspace_bytes(a.type, m, z.shape[1], a.top), workspace)
     _check(lib.kq_distill_loss(ctypes.byref(a), loss.data_ptr(), stats.data_ptr(), wp, wn, _stream(dev)), "kq_distill_loss")
     return loss, stats
 

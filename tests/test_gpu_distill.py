@@ -228,11 +228,14 @@ def test_in_place_strides_and_leading_sizes(m, v, dtype):
     big = torch.full((m, v + 13), 5.0, dtype=dtype, device=DEV)
     view = big[:, 6:6 + v]
     view.copy_(z)
+    one = torch.ones(m).double()
+    l1, d1 = kq.kq_distill(view, tv, ti, **how)      # (rows that begin elsewhere: another order of the sums)
+    check(l1, d1, Z, values, idx, labels, 2.0, 0.3, one)
     l2, d2 = kq.kq_distill(view, tv, ti, dZ=view, **how)
-    assert torch.equal(l2, loss) and torch.equal(view, dz) and d2 is view
+    assert torch.equal(l2, l1) and torch.equal(view, d1) and d2 is view
     view.copy_(z)
     kq.kq_distill_grad(view, tv, ti, stats, dZ=view, **how)
-    assert torch.equal(view, g)
+    assert torch.equal(view, g)     # (no sums in it)
     assert torch.all(big[:, :6] == 5) and torch.all(big[:, 6 + v:] == 5)
     if m % 2 == 0:
         l3, d3 = kq.kq_distill(z.view(2, m // 2, v), tv.view(2, m // 2, -1), ti.view(2, m // 2, -1), temperature=2.0,
