@@ -12,84 +12,152 @@
 
 namespace kq {
 
-// 16 columns at c0 of a row, zeros past k
+// A lane's 32 columns of a block of a row of X: 16 from 16 q and 16 from 64 + 16 q, as they lie in memory.
 template <int TYPE>
-__device__ __forceinline__ void load16(const void* X, int64_t row_at, int c0, int k, float* v) {
-    float a[8], b[8];
-    load_columns<TYPE>(X, row_at, c0, k, a);
-    load_columns<TYPE>(X, row_at, c0 + 8, k, b);
+struct XBlock {
+    static constexpr int kRegs = TYPE == KQ_T_E4M3 ? 2 : TYPE == KQ_T_F32 ? 8 : 4;  // of 16 bytes
+    static constexpr int kBytes = TYPE == KQ_T_E4M3 ? 1 : TYPE == KQ_T_F32 ? 4 : 2;
+    u32x4 r[kRegs];
+    unsigned e;   // KQ_T_E4M3: the exponent
+    __device__ __forceinline__ void load(const char* row, int b, int q, int64_t k) {
+        const int64_t c0 = (int64_t)b * kBlock + 16 * q;
+        if (TYPE == KQ_T_E4M3 || c0 + 80 <= k) {
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-        v[t] = a[t];
-        v[8 + t] = b[t];
+            for (int i = 0; i < kRegs; ++i)
+                __builtin_memcpy(&r[i], row + (c0 + i / (kRegs / 2) * 64) * kBytes + i % (kRegs / 2) * 16, 16);
+        } else {  // the row ends here
+#pragma unroll
+            for (int i = 0; i < kRegs; ++i) {
+                constexpr int kIn = 16 / kBytes;   // values of a register
+                const int64_t c = c0 + i / (kRegs / 2) * 64 + i % (kRegs / 2) * kIn;
+                if (c + kIn <= k) {
+                    __builtin_memcpy(&r[i], row + c * kBytes, 16);
+                    continue;
+                }
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    unsigned v = 0;
+                    if constexpr (TYPE == KQ_T_F32) {
+                        if (c + t < k) v = ((const unsigned*)row)[c + t];
+                    } else if constexpr (TYPE != KQ_T_E4M3) {
+                        if (c + 2 * t < k) v = ((const uint16_t*)row)[c + 2 * t];
+                        if (c + 2 * t + 1 < k) v |= (unsigned)((const uint16_t*)row)[c + 2 * t + 1] << 16;
+                    }
+                    r[i][t] = v;
+                }
+            }
+        }
     }
-}
+    // its bytes (x[0] the first 16 columns) and the block's exponent: the largest magnitude of four lanes
+    __device__ __forceinline__ unsigned quantize(u32x4 (&x)[2]) const {
+        if constexpr (TYPE == KQ_T_E4M3) {
+            x[0] = r[0];
+            x[1] = r[1];
+            return e;
+        } else {
+            unsigned a = 0;
+            if constexpr (TYPE == KQ_T_F32) {
+#pragma unroll
+                for (int i = 0; i < kRegs; ++i)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) a = max(a, r[i][t] & 0x7fffffffu);
+            } else {  // the magnitudes of 16-bit floats order like integers, two at a time
+                using u16x2 = __attribute__((ext_vector_type(2))) unsigned short;
+                u16x2 m = {0, 0};
+#pragma unroll
+                for (int i = 0; i < kRegs; ++i)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const unsigned v = r[i][t] & 0x7fff7fffu;
+                        m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, v));
+                    }
+                const unsigned h = m.x > m.y ? m.x : m.y;
+                a = __builtin_bit_cast(unsigned, TYPE == KQ_T_BF16 ? Act<true>::lo(h) : Act<false>::lo(h));
+            }
+            a = max(a, (unsigned)__shfl_xor(a, 16));
+            a = max(a, (unsigned)__shfl_xor(a, 32));
+            const unsigned ex = block_exponent(a);
+            const float scale = __builtin_bit_cast(float, (ex == 255u ? 127u : ex) << 23);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {  // four bytes; the conversion divides by the power of two
+                    using s16x2 = __attribute__((ext_vector_type(2))) short;
+                    s16x2 w = {0, 0};
+                    if constexpr (TYPE == KQ_T_F32) {
+                        const unsigned v0 = r[4 * h + t][0], v1 = r[4 * h + t][1], v2 = r[4 * h + t][2], v3 = r[4 * h + t][3];
+                        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, __builtin_bit_cast(float, v0), __builtin_bit_cast(float, v1), scale, false);
+                        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, __builtin_bit_cast(float, v2), __builtin_bit_cast(float, v3), scale, true);
+                    } else {
+                        const unsigned v0 = r[2 * h + t / 2][2 * (t & 1)], v1 = r[2 * h + t / 2][2 * (t & 1) + 1];
+                        if constexpr (TYPE == KQ_T_BF16) {
+                            w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, v0), scale, false);
+                            w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, v1), scale, true);
+                        } else {
+                            w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, __builtin_bit_cast(f16x2, v0), scale, false);
+                            w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, __builtin_bit_cast(f16x2, v1), scale, true);
+                        }
+                    }
+                    x[h][t] = __builtin_bit_cast(unsigned, w);
+                }
+            return ex;
+        }
+    }
+};
 
+// RT: 16-row tiles of W a workgroup takes; they share what a wave does to X.
 template <int TYPE, int WAVES, int RT>
 __global__ __launch_bounds__(64 * WAVES) void block_matvec_kernel(const BlockMatvecParams p) {
     __shared__ f32x4 s_sum[RT * WAVES * 64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r16 = lane & 15, q = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * RT * 16;
+    const int64_t n0 = (int64_t)blockIdx.x * (16 * RT);
     const int blocks = (int)(p.kp >> 7);
     const int b_begin = blockIdx.y * p.blocks_per_split, b_end = min(b_begin + p.blocks_per_split, blocks);
+    static_assert(kBlock % (16 * RT) == 0, "a workgroup's rows of W lie in one block");
     // rows past the last repeat it: what they give is not stored
     const uint8_t* w_row[RT];
-    const uint8_t* w_exp[RT];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        w_row[t] = p.values + min(n0 + 16 * t + r16, p.n - 1) * p.kp;
-        w_exp[t] = p.exps + (min(n0 + 16 * t, p.n - 1) >> 7) * blocks;  // (16 rows lie in one block)
-    }
+    for (int t = 0; t < RT; ++t) w_row[t] = p.values + min(n0 + 16 * t + r16, p.n - 1) * p.kp + 16 * q;
+    const uint8_t* const w_exp = p.exps + (n0 >> 7) * blocks;
     const int64_t xr = min(r16, p.m - 1);
+    const char* const x_row = (const char*)p.X + xr * p.ldx * XBlock<TYPE>::kBytes;
+    const uint8_t* const x_exp = TYPE == KQ_T_E4M3 ? p.x_exps + xr * blocks : nullptr;
     f32x4 y[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) y[t] = f32x4{0, 0, 0, 0};
 
-    for (int b = b_begin + wave; b < b_end; b += WAVES) {
+    struct Block {
         u32x4 w[RT][2];
-        unsigned ew[RT];
+        unsigned ew;
+        XBlock<TYPE> x;
+    };
+    auto fetch = [&](Block& f, int b) {
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-            w[t][0] = *(const u32x4*)(w_row[t] + (int64_t)b * kBlock + 16 * q);
-            w[t][1] = *(const u32x4*)(w_row[t] + (int64_t)b * kBlock + 64 + 16 * q);
-            ew[t] = w_exp[t][b];
+            f.w[t][0] = *(const u32x4*)(w_row[t] + (int64_t)b * kBlock);
+            f.w[t][1] = *(const u32x4*)(w_row[t] + (int64_t)b * kBlock + 64);
         }
-        u32x4 x[2];
-        unsigned ex;
-        if constexpr (TYPE == KQ_T_E4M3) {
-            const uint8_t* row = (const uint8_t*)p.X + xr * p.kp + (int64_t)b * kBlock;
-            x[0] = *(const u32x4*)(row + 16 * q);
-            x[1] = *(const u32x4*)(row + 64 + 16 * q);
-            ex = p.x_exps[xr * blocks + b];
-        } else {
-            float v[2][16];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) load16<TYPE>(p.X, xr * p.ldx, b * kBlock + 64 * h + 16 * q, (int)p.k, v[h]);
-            unsigned a = 0;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int t = 0; t < 16; ++t) a = max(a, __builtin_bit_cast(unsigned, v[h][t]) & 0x7fffffffu);
-            a = max(a, (unsigned)__shfl_xor(a, 16));
-            a = max(a, (unsigned)__shfl_xor(a, 32));
-            ex = block_exponent(a);
-            const float inv = ex == 255u ? 0.0f : block_inverse(ex);
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int t = 0; t < 4; ++t) x[h][t] = encode4(v[h][4 * t], v[h][4 * t + 1], v[h][4 * t + 2], v[h][4 * t + 3], inv);
-        }
-        u32x4 xd[4];
+        f.ew = w_exp[b];
+        f.x.load(x_row, b, q, p.k);
+        if constexpr (TYPE == KQ_T_E4M3) f.x.e = x_exp[b];
+    };
+    Block next;
+    if (b_begin + wave < b_end) fetch(next, b_begin + wave);
+    for (int b = b_begin + wave; b < b_end; b += WAVES) {  // the next block's loads are on their way
+        const Block now = next;
+        if (b + WAVES < b_end) fetch(next, b + WAVES);
+        u32x4 x[2], xd[4];
+        const unsigned ex = now.x.quantize(x);
 #pragma unroll
         for (int i = 0; i < 4; ++i) xd[i] = decode8(x[i >> 1][2 * (i & 1)], x[i >> 1][2 * (i & 1) + 1], 1.0f);
+        const int shift = (int)(now.ew + ex) - 254;
+        const float one = now.ew == 255u || ex == 255u ? __builtin_bit_cast(float, 0x7fc00000u) : 1.0f;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
             f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc = Act<true>::mfma(decode8(w[t][i >> 1][2 * (i & 1)], w[t][i >> 1][2 * (i & 1) + 1], 1.0f), xd[i], acc);
-            const int shift = (int)(ew[t] + ex) - 254;
-            const float one = ew[t] == 255u || ex == 255u ? __builtin_bit_cast(float, 0x7fc00000u) : 1.0f;
+            for (int i = 0; i < 4; ++i) acc = Act<true>::mfma(decode8(now.w[t][i >> 1][2 * (i & 1)], now.w[t][i >> 1][2 * (i & 1) + 1], 1.0f), xd[i], acc);
 #pragma unroll
             for (int r = 0; r < 4; ++r) y[t][r] = __builtin_fmaf(__builtin_ldexpf(acc[r], shift), one, y[t][r]);
         }
@@ -99,51 +167,71 @@ __global__ __launch_bounds__(64 * WAVES) void block_matvec_kernel(const BlockMat
 #pragma unroll
     for (int t = 0; t < RT; ++t) s_sum[(t * WAVES + wave) * 64 + lane] = y[t];
     __syncthreads();
-    if (wave < RT) {
+    if (wave < RT && r16 < p.m) {
         f32x4 v = s_sum[wave * WAVES * 64 + lane];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) v += s_sum[(wave * WAVES + w) * 64 + lane];
-        if (r16 < p.m) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int64_t n = n0 + 16 * wave + 4 * q + r;
-                if (n >= p.n) break;
-                if (p.part) {
-                    p.part[((int64_t)blockIdx.y * p.m + r16) * p.n + n] = v[r];
-                    continue;
-                }
-                const float o = v[r] + (p.bias ? p.bias[n] : 0.0f);
-                const int64_t at = (int64_t)r16 * p.ldy + n;
-                if (p.y_type == KQ_T_F32) ((float*)p.Y)[at] = o;
-                else ((uint16_t*)p.Y)[at] = p.y_type == KQ_T_BF16 ? Act<true>::one(o) : Act<false>::one(o);
+        for (int r = 0; r < 4; ++r) {
+            const int64_t n = n0 + 16 * wave + 4 * q + r;
+            if (n >= p.n) break;
+            if (p.part) {
+                p.part[((int64_t)blockIdx.y * p.m + r16) * p.n + n] = v[r];
+                continue;
             }
+            const float o = v[r] + (p.bias ? p.bias[n] : 0.0f);
+            const int64_t at = (int64_t)r16 * p.ldy + n;
+            if (p.y_type == KQ_T_F32) ((float*)p.Y)[at] = o;
+            else ((uint16_t*)p.Y)[at] = p.y_type == KQ_T_BF16 ? Act<true>::one(o) : Act<false>::one(o);
         }
     }
 }
 
+// Row tiles a workgroup takes, splits of the columns and waves.  A wave's work on X (quantizing it, reading it from L2) is
+// shared by its row tiles, so there are several where W is long or has more row tiles than the chip has room for; the
+// columns are split where the workgroups would not fill the chip and are long enough for the joining launch (2 to 3 us).
+// Measured (us, rows of bf16 X / n x k; row tiles x splits w waves):
+//    1 / 4096 x 25088: 1x1w16 29.9, 2x2w8 23.1, 2x4w4 23.0, 4x4w4 23.6     16 / 4096 x 25088: 1x1w16 38.8, 2x2w8 29.3, 4x4w4 25.2
+//    1 / 4096 x 4096:  1x1w8 6.7, 2x2w8 8.0, 4x4w4 8.5                     16 / 4096 x 4096:  4x4w8 9.0, 1x1w8 9.0
+//    1 / 1000 x 25088: 2x8w8 9.5, 1x4w8 9.9, 4x8w4 above 11.7             16 / 1000 x 25088: 2x8w8 11.8, 1x4w8 13.7
+//   16 / 8192 x 8192:  1x1 above 22, 2x1w8 19.3, 4x4w4 19.4                1 / 1000 x 512:   1x1w4 3.3, 2x1w4 3.6
 BlockMatvecPlan block_matvec_plan(int m, int64_t n, int64_t k) {
     BlockMatvecPlan v = {};
     const int64_t blocks = block_pitch(k) / kBlock, tiles = ceil_div64(n, 16);
-    v.row_tiles = 1;
-    v.waves = 4;
-    const int64_t room = tiles < 256 ? 256 / tiles : 1, long_enough = blocks >= 64 ? blocks / 16 : 1;
+    v.row_tiles = blocks >= 96 ? (m > 4 && tiles > 128 ? 4 : 2) : tiles >= 512 ? 2 : 1;
+    const int64_t groups = ceil_div64(tiles, v.row_tiles), room = groups < 256 ? 256 / groups : 1;
+    const int64_t long_enough = blocks >= 16 ? blocks / 8 : 1;
     const int64_t splits = room < long_enough ? room : long_enough;
     v.blocks_per_split = (int)ceil_div64(blocks, splits);
     v.splits = (int)ceil_div64(blocks, v.blocks_per_split);
+    v.waves = v.row_tiles == 4 || v.blocks_per_split <= 12 ? 4 : v.row_tiles == 2 || v.blocks_per_split <= 64 ? 8 : 16;
     v.ws_bytes = v.splits > 1 ? (size_t)v.splits * (size_t)m * (size_t)n * sizeof(float) : 0;
     return v;
+}
+
+template <int TYPE>
+static void launch_matvec_type(const BlockMatvecPlan& v, const BlockMatvecParams& p, hipStream_t s) {
+    const dim3 grid((unsigned)ceil_div64(p.n, 16 * v.row_tiles), (unsigned)p.splits), block(64 * v.waves);
+    if (v.row_tiles == 4) {
+        block_matvec_kernel<TYPE, 4, 4><<<grid, block, 0, s>>>(p);
+    } else if (v.row_tiles == 2) {
+        if (v.waves == 8) block_matvec_kernel<TYPE, 8, 2><<<grid, block, 0, s>>>(p);
+        else block_matvec_kernel<TYPE, 4, 2><<<grid, block, 0, s>>>(p);
+    } else {
+        if (v.waves == 16) block_matvec_kernel<TYPE, 16, 1><<<grid, block, 0, s>>>(p);
+        else if (v.waves == 8) block_matvec_kernel<TYPE, 8, 1><<<grid, block, 0, s>>>(p);
+        else block_matvec_kernel<TYPE, 4, 1><<<grid, block, 0, s>>>(p);
+    }
 }
 
 hipError_t launch_block_matvec(const BlockMatvecPlan& plan, BlockMatvecParams p, hipStream_t s) {
     p.splits = plan.splits;
     p.blocks_per_split = plan.blocks_per_split;
     if (p.splits == 1) p.part = nullptr;
-    const dim3 grid((unsigned)ceil_div64(ceil_div64(p.n, 16), plan.row_tiles), (unsigned)p.splits), block(64 * plan.waves);
-    if (plan.row_tiles != 1 || plan.waves != 4) return hipErrorInvalidValue;
-    if (p.x_type == KQ_T_E4M3) block_matvec_kernel<KQ_T_E4M3, 4, 1><<<grid, block, 0, s>>>(p);
-    else if (p.x_type == KQ_T_F32) block_matvec_kernel<KQ_T_F32, 4, 1><<<grid, block, 0, s>>>(p);
-    else if (p.x_type == KQ_T_BF16) block_matvec_kernel<KQ_T_BF16, 4, 1><<<grid, block, 0, s>>>(p);
-    else block_matvec_kernel<KQ_T_F16, 4, 1><<<grid, block, 0, s>>>(p);
+    if (p.x_type == KQ_T_E4M3) launch_matvec_type<KQ_T_E4M3>(plan, p, s);
+    else if (p.x_type == KQ_T_F32) launch_matvec_type<KQ_T_F32>(plan, p, s);
+    else if (p.x_type == KQ_T_BF16) launch_matvec_type<KQ_T_BF16>(plan, p, s);
+    else launch_matvec_type<KQ_T_F16>(plan, p, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     const JoinParams j = {p.part, p.splits, p.m, p.n, p.bias, p.Y, p.ldy, p.y_type};
