@@ -936,7 +936,10 @@ if _kqhost is not None and _raw_stream is not None:
         "kq_quantize_groups", "kq_reconstruct_groups", "kq_group_linear_workspace_bytes", "kq_group_linear",
         "kq_group_linear_grad_input_workspace_bytes", "kq_group_linear_grad_input", "kq_checkpoint_pack",
         "kq_checkpoint_restore", "kq_checkpoint_grad_workspace_bytes", "kq_checkpoint_grad_scales",
-        "kq_checkpoint_grad_weight")), _raw_stream, lambda device, nbytes: _ws(device, nbytes))
+        "kq_checkpoint_grad_weight", "kq_quantize_blocks", "kq_reconstruct_blocks", "kq_block_linear_workspace_bytes",
+        "kq_block_linear", "kq_block_linear_grad_input_workspace_bytes", "kq_block_linear_grad_input",
+        "kq_block_linear_grad_weight_workspace_bytes", "kq_block_linear_grad_weight", "kq_distill_workspace_bytes",
+        "kq_distill", "kq_distill_loss", "kq_distill_grad")), _raw_stream, lambda device, nbytes: _ws(device, nbytes))
     _fast = _kqhost
 else:
     _fast = None
@@ -1317,6 +1320,10 @@ def kq_quantize_blocks(X, rows: int = 1, values=None, exps=None):
     """A matrix [..., k] (fp32, bf16 or fp16; a matrix may have strided rows) in 8-bit floats with a power of two for each
     block of `rows` rows (1: activations, 128: weights) by 128 columns.  Returns (values float8_e4m3fn [m, k rounded up to
     128], exps uint8 [ceil(m / rows), ceil(k / 128)]); include/kq.h has the formulas."""
+    if _fast is not None and values is None and exps is None:
+        r = _fast.quantize_blocks(X, rows)
+        if r is not None:
+            return r
     x, ty, ld = _rows(X, _TYPES, "X")
     m, k = x.shape
     dev = x.device
@@ -1331,6 +1338,10 @@ def kq_quantize_blocks(X, rows: int = 1, values=None, exps=None):
 
 def kq_reconstruct_blocks(values, exps, in_features: int, rows: int = 1, dtype=torch.float32, X_hat=None):
     """What values and exponents stand for, [m, in_features] of `dtype` (or X_hat's)."""
+    if _fast is not None and X_hat is None:
+        r = _fast.reconstruct_blocks(values, exps, in_features, rows, _TYPES.get(dtype, -1))
+        if r is not None:
+            return r
     m, k = _blocks(values, exps, in_features, rows, "values")
     dev = values.device
     if X_hat is None:
@@ -1361,6 +1372,10 @@ def kq_block_linear(X, values, exps, bias=None, x_exps=None, dtype=None, Y=None,
     """Y = X_hat W_hat^T + bias for a weight [n, k] as kq_quantize_blocks(W, rows=128) leaves it.  X [..., k] is fp32, bf16 or
     fp16 and quantized on the way, or it is the values of kq_quantize_blocks(X) with x_exps its exponents.  bias fp32 [n] or
     None; Y [..., n] of `dtype` (X's type, or bf16 for 8-bit values).  From one row (a token) to any number of them."""
+    if _fast is not None and workspace is None and (dtype is None or dtype in _TYPES):
+        r = _fast.block_linear(X, values, exps, bias, x_exps, -1 if dtype is None else _TYPES[dtype], Y)
+        if r is not None:
+            return r
     if x_exps is None:
         x, xt, ldx = _rows(X, _TYPES, "X")
         m, k = x.shape
@@ -1389,6 +1404,10 @@ def kq_block_linear(X, values, exps, bias=None, x_exps=None, dtype=None, Y=None,
 def kq_block_linear_grad_input(dY, values, exps, in_features: int, dX=None, workspace=None):
     """dX = dY_hat W_hat: dY [..., n] fp32, bf16 or fp16, quantized on the way in blocks of 128 of its columns; dX
     [..., in_features] in its type."""
+    if _fast is not None and workspace is None:
+        r = _fast.block_grad_input(dY, values, exps, in_features, dX)
+        if r is not None:
+            return r
     dy, ty, ldy = _rows(dY, _TYPES, "dY")
     m = dy.shape[0]
     n, k = _blocks(values, exps, in_features, KQ_BLOCK, "values")
@@ -1408,6 +1427,10 @@ def kq_block_linear_grad_weight(dY, x_values, x_exps, in_features: int, bias: bo
     """Gradient of the weight, dY^T X (`dtype` [n, in_features]), from dY [..., n] (fp32, bf16 or fp16) and the values that
     kq_quantize_blocks(X) gives: both are quantized along the rows, in blocks of 128 rows by 1 column.  bias: also the
     column sums of dY (fp32, not quantized).  Returns (dW, dbias or None)."""
+    if _fast is not None and dW is None and dbias is None and workspace is None:
+        r = _fast.block_grad_weight(dY, x_values, x_exps, in_features, bias, _TYPES.get(dtype, -1))
+        if r is not None:
+            return r
     m, k = _blocks(x_values, x_exps, in_features, 1, "x_values")
     dy, ty, ldy = _rows(dY, _TYPES, "dY")
     n, dev = dy.shape[1], dy.device
@@ -1515,6 +1538,10 @@ def kq_distill(Z, top_values, top_idx, temperature: float = 1.0, labels=None, al
     type at top_idx, int32 or int64) and, with weight alpha, its labels, and the gradient of sum_row d[row] loss[row]: d is
     dloss (fp32, one a row) or `scale` for all rows (1 / rows for the mean).  Entries and labels outside [0, v) are absent.
     Returns (loss fp32 [rows], dZ like Z; dZ may be Z).  include/kq.h has the formulas."""
+    if _fast is not None and loss is None and workspace is None:
+        r = _fast.distill(Z, top_values, top_idx, temperature, labels, alpha, scale, dloss, dZ)
+        if r is not None:
+            return r
     a, z = _distill_args(Z, top_values, top_idx, temperature, labels, alpha)
     dev, m = z.device, z.shape[0]
     if dloss is not None:
@@ -1530,6 +1557,10 @@ def kq_distill(Z, top_values, top_idx, temperature: float = 1.0, labels=None, al
 def kq_distill_loss(Z, top_values, top_idx, temperature: float = 1.0, labels=None, alpha: float = 0.0, loss=None, stats=None,
                     workspace=None):
     """The loss alone: (loss fp32 [rows], stats fp32 [rows, 3] for kq_distill_grad)."""
+    if _fast is not None and loss is None and stats is None and workspace is None:
+        r = _fast.distill_loss(Z, top_values, top_idx, temperature, labels, alpha)
+        if r is not None:
+            return r
     a, z = _distill_args(Z, top_values, top_idx, temperature, labels, alpha)
     dev, m = z.device, z.shape[0]
     loss = _row_floats(loss, dev, m, "loss")
@@ -1546,6 +1577,10 @@ def kq_distill_grad(Z, top_values, top_idx, stats, dloss=None, temperature: floa
                     scale: float = 1.0, dZ=None):
     """The gradient of the logits from what kq_distill_loss kept: dloss fp32 [rows], or None for `scale` in all of them.
     dZ may be Z."""
+    if _fast is not None:
+        r = _fast.distill_grad(Z, top_values, top_idx, temperature, labels, alpha, scale, stats, dloss, dZ)
+        if r is not None:
+            return r
     a, z = _distill_args(Z, top_values, top_idx, temperature, labels, alpha)
     dev, m = z.device, z.shape[0]
     _dev(stats, torch.float32, "stats", (m, 3))

@@ -8,8 +8,8 @@
 // case (plain contiguous tensors of the right types and shapes on one GPU, the outputs given): the
 // caller then goes through its own checks, which convert, allocate or raise.
 //
-// The calls of the 4-bit fully-connected layer and of the 8-bit checkpoints (group_linear and the others
-// below) do the whole call here in the plain case: checks, outputs, scratch and the library call.  A call
+// The calls of the 4-bit and 8-bit fully-connected layers, of the 8-bit checkpoints and of distillation (group_linear and
+// the others below) do the whole call here in the plain case: checks, outputs, scratch and the library call.  A call
 // on one token runs a few microseconds on the GPU; in Python its checks and its sixteen arguments took
 // 10 us (here 4.3, of which the launch is about 3).  They return the outputs, or None where anything is not plain or the library refuses: the
 // caller then goes through its own checks, which convert or raise.  bind(addresses, stream, scratch) gives
@@ -119,17 +119,30 @@ struct Library {
     decltype(&kq_checkpoint_grad_workspace_bytes) grad_ws = nullptr;
     decltype(&kq_checkpoint_grad_scales) grad_scales = nullptr;
     decltype(&kq_checkpoint_grad_weight) grad_weight = nullptr;
+    decltype(&kq_quantize_blocks) quantize_blocks = nullptr;
+    decltype(&kq_reconstruct_blocks) reconstruct_blocks = nullptr;
+    decltype(&kq_block_linear_workspace_bytes) block_linear_ws = nullptr;
+    decltype(&kq_block_linear) block_linear = nullptr;
+    decltype(&kq_block_linear_grad_input_workspace_bytes) block_grad_input_ws = nullptr;
+    decltype(&kq_block_linear_grad_input) block_grad_input = nullptr;
+    decltype(&kq_block_linear_grad_weight_workspace_bytes) block_grad_weight_ws = nullptr;
+    decltype(&kq_block_linear_grad_weight) block_grad_weight = nullptr;
+    decltype(&kq_distill_workspace_bytes) distill_ws = nullptr;
+    decltype(&kq_distill) distill = nullptr;
+    decltype(&kq_distill_loss) distill_loss = nullptr;
+    decltype(&kq_distill_grad) distill_grad = nullptr;
     PyObject* stream = nullptr;   // device index -> stream handle
     PyObject* scratch = nullptr;  // (torch.device, bytes) -> uint8 tensor
 } g_lib;
 
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t count) {
-    if (count != 3 || !PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != 11) {
-        PyErr_SetString(PyExc_TypeError, "bind(eleven addresses, stream, scratch)");
+    constexpr int kFunctions = 23;
+    if (count != 3 || !PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != kFunctions) {
+        PyErr_SetString(PyExc_TypeError, "bind(23 addresses, stream, scratch)");
         return nullptr;
     }
-    void* f[11];
-    for (int i = 0; i < 11; ++i) {
+    void* f[kFunctions];
+    for (int i = 0; i < kFunctions; ++i) {
         f[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(a[0], i));
         if (PyErr_Occurred()) return nullptr;
     }
@@ -145,6 +158,18 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t count) {
     l.grad_ws = (decltype(l.grad_ws))f[8];
     l.grad_scales = (decltype(l.grad_scales))f[9];
     l.grad_weight = (decltype(l.grad_weight))f[10];
+    l.quantize_blocks = (decltype(l.quantize_blocks))f[11];
+    l.reconstruct_blocks = (decltype(l.reconstruct_blocks))f[12];
+    l.block_linear_ws = (decltype(l.block_linear_ws))f[13];
+    l.block_linear = (decltype(l.block_linear))f[14];
+    l.block_grad_input_ws = (decltype(l.block_grad_input_ws))f[15];
+    l.block_grad_input = (decltype(l.block_grad_input))f[16];
+    l.block_grad_weight_ws = (decltype(l.block_grad_weight_ws))f[17];
+    l.block_grad_weight = (decltype(l.block_grad_weight))f[18];
+    l.distill_ws = (decltype(l.distill_ws))f[19];
+    l.distill = (decltype(l.distill))f[20];
+    l.distill_loss = (decltype(l.distill_loss))f[21];
+    l.distill_grad = (decltype(l.distill_grad))f[22];
     l.stream = Py_NewRef(a[1]);
     l.scratch = Py_NewRef(a[2]);
     g_lib = l;  // (bound once, when the binding is imported)
@@ -490,6 +515,295 @@ PyObject* grad_weight(PyObject*, PyObject* const* a, Py_ssize_t count) {
     });
 }
 
+// ---- the 8-bit fully-connected layer --------------------------------------------------------------------
+
+constexpr int64_t kBlock = KQ_BLOCK;
+at::ScalarType scalar_of(int64_t type) { return type == KQ_T_F32 ? at::kFloat : type == KQ_T_BF16 ? at::kBFloat16 : at::kHalf; }
+
+// dtype's type number, -1 for None; anything else is not plain
+int64_t type_number(Call& c, PyObject* o) {
+    if (!PyLong_CheckExact(o)) {
+        c.ok = false;
+        return -1;
+    }
+    const long v = PyLong_AsLong(o);
+    c.ok = c.ok && v >= -1 && v <= 2;
+    return v;
+}
+
+// values and exponents of an 8-bit matrix of k columns (0: as many as there are)
+struct Blocks {
+    int64_t m = 0, k = 0;
+    const uint8_t* values = nullptr;
+    const uint8_t* exps = nullptr;
+    Blocks(Call& c, PyObject* values_o, PyObject* exps_o, int64_t k_, int64_t rows) {
+        at::Tensor t = c.tensor(values_o);
+        c.ok = c.ok && t.dim() == 2 && t.scalar_type() == at::kFloat8_e4m3fn && t.is_contiguous();
+        if (!c.ok) return;
+        m = t.size(0);
+        k = k_ > 0 ? k_ : t.size(1);
+        const int64_t kb = (k + kBlock - 1) / kBlock;
+        const at::Tensor e = c.dense(exps_o, at::kByte, {(m + rows - 1) / rows, kb});
+        c.ok = c.ok && m > 0 && kb > 0 && t.size(1) == kb * kBlock;
+        if (!c.ok) return;
+        values = (const uint8_t*)t.data_ptr();
+        exps = (const uint8_t*)e.data_ptr();
+    }
+};
+
+// (X, rows)
+PyObject* quantize_blocks(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded(count, 2, [&]() -> PyObject* {
+        Call c;
+        int64_t ld = 0;
+        const at::Tensor X = c.rows(a[0], ld);
+        const int64_t rows = c.integer(a[1]);
+        if (!c.ok || (rows != 1 && rows != kBlock)) return nullptr;
+        void* const s = c.stream();
+        if (!c.ok) return nullptr;
+        const int64_t m = X.size(0), k = X.size(1), kb = (k + kBlock - 1) / kBlock;
+        const at::Tensor v = c.make({m, kb * kBlock}, at::kFloat8_e4m3fn), e = c.make({(m + rows - 1) / rows, kb}, at::kByte);
+        if (g_lib.quantize_blocks(X.data_ptr(), Call::type_of(X), ld, m, k, (int32_t)rows, (uint8_t*)v.data_ptr(), (uint8_t*)e.data_ptr(), s) != KQ_OK)
+            return nullptr;
+        return pair(v, e);
+    });
+}
+
+// (values, exps, k, rows, dtype's type number)
+PyObject* reconstruct_blocks(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded(count, 5, [&]() -> PyObject* {
+        Call c;
+        const int64_t k = c.integer(a[2]), rows = c.integer(a[3]), type = type_number(c, a[4]);
+        if (!c.ok || (rows != 1 && rows != kBlock) || type < 0) return nullptr;
+        const Blocks w(c, a[0], a[1], k, rows);
+        if (!c.ok) return nullptr;
+        void* const s = c.stream();
+        if (!c.ok) return nullptr;
+        const at::Tensor X = c.make({w.m, k}, scalar_of(type));
+        if (g_lib.reconstruct_blocks(w.values, w.exps, w.m, k, (int32_t)rows, (int32_t)type, X.data_ptr(), k, s) != KQ_OK) return nullptr;
+        return THPVariable_Wrap(X);
+    });
+}
+
+// (X, values, exps, bias, x_exps, dtype's type number or -1, Y)
+PyObject* block_linear(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded(count, 7, [&]() -> PyObject* {
+        Call c;
+        int64_t m, k, ldx = 0, type = type_number(c, a[5]);
+        int32_t xt;
+        const void* x;
+        const uint8_t* xe = nullptr;
+        if (a[4] == Py_None) {
+            const at::Tensor X = c.rows(a[0], ldx);
+            if (!c.ok) return nullptr;
+            m = X.size(0), k = X.size(1), xt = Call::type_of(X), x = X.data_ptr();
+        } else {
+            const Blocks q(c, a[0], a[4], 0, 1);
+            if (!c.ok) return nullptr;
+            m = q.m, k = ldx = q.k, xt = KQ_T_E4M3, x = q.values, xe = q.exps;
+        }
+        const Blocks w(c, a[1], a[2], k, kBlock);
+        const float* bias = nullptr;
+        if (a[3] != Py_None) {
+            const at::Tensor b = c.dense(a[3], at::kFloat, {w.m});
+            if (c.ok) bias = (const float*)b.data_ptr();
+        }
+        at::Tensor Y;
+        int64_t ldy = w.m;
+        if (a[6] != Py_None) {
+            Y = c.rows(a[6], ldy);
+            if (!c.ok || Y.size(0) != m || Y.size(1) != w.m || (type >= 0 && Call::type_of(Y) != type)) return nullptr;
+            type = Call::type_of(Y);
+        }
+        if (type < 0) type = xt == KQ_T_E4M3 ? KQ_T_BF16 : xt;
+        if (!c.ok) return nullptr;
+        void* const s = c.stream();
+        const at::Tensor ws = c.scratch(g_lib.block_linear_ws(xt, (int32_t)type, m, w.m, k));
+        if (!c.ok) return nullptr;
+        if (!Y.defined()) Y = c.make({m, w.m}, scalar_of(type));
+        if (g_lib.block_linear(x, xt, ldx, xe, m, w.m, k, w.values, w.exps, bias, Y.data_ptr(), (int32_t)type, ldy, address(ws), bytes_of(ws), s) != KQ_OK)
+            return nullptr;
+        return a[6] != Py_None ? Py_NewRef(a[6]) : THPVariable_Wrap(Y);
+    });
+}
+
+// (dY, values, exps, k, dX)
+PyObject* block_grad_input(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded(count, 5, [&]() -> PyObject* {
+        Call c;
+        int64_t ldy = 0, ldx = 0;
+        const at::Tensor dY = c.rows(a[0], ldy);
+        const int64_t k = c.integer(a[3]);
+        if (!c.ok) return nullptr;
+        const Blocks w(c, a[1], a[2], k, kBlock);
+        const int64_t m = dY.size(0), n = dY.size(1);
+        const int32_t type = Call::type_of(dY);
+        if (!c.ok || w.m != n) return nullptr;
+        at::Tensor dX;
+        if (a[4] != Py_None) {
+            dX = c.rows(a[4], ldx);
+            if (!c.ok || dX.scalar_type() != dY.scalar_type() || dX.size(0) != m || dX.size(1) != k) return nullptr;
+        }
+        void* const s = c.stream();
+        const at::Tensor ws = c.scratch(g_lib.block_grad_input_ws(type, m, n, k));
+        if (!c.ok) return nullptr;
+        if (!dX.defined()) {
+            dX = c.make({m, k}, dY.scalar_type());
+            ldx = k;
+        }
+        if (g_lib.block_grad_input(dY.data_ptr(), type, ldy, m, n, k, w.values, w.exps, dX.data_ptr(), ldx, address(ws), bytes_of(ws), s) != KQ_OK)
+            return nullptr;
+        return a[4] != Py_None ? Py_NewRef(a[4]) : THPVariable_Wrap(dX);
+    });
+}
+
+// (dY, x_values, x_exps, k, bias, dtype's type number)
+PyObject* block_grad_weight(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded(count, 6, [&]() -> PyObject* {
+        Call c;
+        int64_t ldy = 0;
+        const at::Tensor dY = c.rows(a[0], ldy);
+        const int64_t k = c.integer(a[3]), type = type_number(c, a[5]);
+        if (!c.ok || type < 0 || (a[4] != Py_True && a[4] != Py_False)) return nullptr;
+        const Blocks x(c, a[1], a[2], k, 1);
+        const int64_t m = dY.size(0), n = dY.size(1);
+        if (!c.ok || x.m != m) return nullptr;
+        void* const s = c.stream();
+        const at::Tensor ws = c.scratch(g_lib.block_grad_weight_ws((int32_t)type, m, n, k));
+        if (!c.ok) return nullptr;
+        const at::Tensor dW = c.make({n, k}, scalar_of(type));
+        at::Tensor db;
+        if (a[4] == Py_True) db = c.make({n}, at::kFloat);
+        if (g_lib.block_grad_weight(dY.data_ptr(), Call::type_of(dY), ldy, m, n, k, x.values, x.exps, dW.data_ptr(), (int32_t)type, k,
+                                    (float*)address(db), address(ws), bytes_of(ws), s) != KQ_OK)
+            return nullptr;
+        return pair(dW, db);
+    });
+}
+
+// ---- distillation -----------------------------------------------------------------------------------------
+
+float number(Call& c, PyObject* o) {
+    if (!PyFloat_CheckExact(o)) {
+        c.ok = false;
+        return 0.0f;
+    }
+    return (float)PyFloat_AS_DOUBLE(o);
+}
+int32_t index_bytes(Call& c, const at::Tensor& t) {
+    const int32_t b = t.scalar_type() == at::kLong ? 8 : t.scalar_type() == at::kInt ? 4 : 0;
+    c.ok = c.ok && b != 0;
+    return b;
+}
+
+// (Z, top_values, top_idx, temperature, labels, alpha): the first six arguments of each call
+struct Distill {
+    kq_distill_args args = {};
+    at::Tensor Z;
+    Distill(Call& c, PyObject* const* a) {
+        Z = c.rows(a[0], args.ldz);
+        const at::Tensor tv = c.tensor(a[1]), ti = c.tensor(a[2]);
+        args.temperature = number(c, a[3]);
+        args.alpha = number(c, a[5]);
+        if (!c.ok || Z.size(0) < 1 || tv.dim() != 2 || !tv.is_contiguous() || !ti.is_contiguous() || ti.sizes() != tv.sizes() || tv.size(0) != Z.size(0) ||
+            Call::type_of(tv) < 0) {
+            c.ok = false;
+            return;
+        }
+        args.Z = Z.data_ptr();
+        args.type = Call::type_of(Z);
+        args.m = Z.size(0);
+        args.v = Z.size(1);
+        args.top_values = tv.data_ptr();
+        args.top_type = Call::type_of(tv);
+        args.top_idx = ti.data_ptr();
+        args.idx_bytes = index_bytes(c, ti);
+        c.ok = c.ok && tv.size(1) >= 1 && tv.size(1) <= KQ_DISTILL_MAX_TOP;
+        args.top = (int32_t)tv.size(1);
+        if (a[4] != Py_None) {
+            const at::Tensor y = c.tensor(a[4]);
+            if (!c.ok || y.dim() != 1 || y.size(0) != args.m || !y.is_contiguous()) {
+                c.ok = false;
+                return;
+            }
+            args.labels = y.data_ptr();
+            args.label_bytes = index_bytes(c, y);
+        }
+    }
+};
+const float* row_floats(Call& c, PyObject* o, int64_t m) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor t = c.dense(o, at::kFloat, {m});
+    return c.ok ? (const float*)t.data_ptr() : nullptr;
+}
+// dZ, given or made like Z
+at::Tensor gradient(Call& c, PyObject* o, const at::Tensor& Z, int64_t& ld) {
+    if (o == Py_None) {
+        if (!c.ok) return {};
+        ld = Z.size(1);
+        return c.make(Z.sizes(), Z.scalar_type());
+    }
+    at::Tensor t = c.rows(o, ld);
+    c.ok = c.ok && t.scalar_type() == Z.scalar_type() && t.sizes() == Z.sizes();
+    return t;
+}
+
+// (.., scale, dloss, dZ)
+PyObject* distill(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded(count, 9, [&]() -> PyObject* {
+        Call c;
+        const Distill d(c, a);
+        const float scale = number(c, a[6]);
+        if (!c.ok) return nullptr;
+        const float* const dloss = row_floats(c, a[7], d.args.m);
+        int64_t ld = 0;
+        void* const s = c.stream();
+        const at::Tensor ws = c.scratch(g_lib.distill_ws(d.args.type, d.args.m, d.args.v, d.args.top));
+        const at::Tensor dZ = gradient(c, a[8], d.Z, ld);
+        if (!c.ok) return nullptr;
+        const at::Tensor loss = c.make({d.args.m}, at::kFloat);
+        if (g_lib.distill(&d.args, dloss, scale, (float*)loss.data_ptr(), dZ.data_ptr(), ld, address(ws), bytes_of(ws), s) != KQ_OK) return nullptr;
+        PyObject* const r = pair(loss, dZ);
+        if (r && a[8] != Py_None && PyTuple_SetItem(r, 1, Py_NewRef(a[8])) != 0) {
+            Py_DECREF(r);
+            return nullptr;
+        }
+        return r;
+    });
+}
+
+PyObject* distill_loss(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded(count, 6, [&]() -> PyObject* {
+        Call c;
+        const Distill d(c, a);
+        if (!c.ok) return nullptr;
+        void* const s = c.stream();
+        const at::Tensor ws = c.scratch(g_lib.distill_ws(d.args.type, d.args.m, d.args.v, d.args.top));
+        if (!c.ok) return nullptr;
+        const at::Tensor loss = c.make({d.args.m}, at::kFloat), stats = c.make({d.args.m, 3}, at::kFloat);
+        if (g_lib.distill_loss(&d.args, (float*)loss.data_ptr(), (float*)stats.data_ptr(), address(ws), bytes_of(ws), s) != KQ_OK) return nullptr;
+        return pair(loss, stats);
+    });
+}
+
+// (.., scale, stats, dloss, dZ)
+PyObject* distill_grad(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded(count, 10, [&]() -> PyObject* {
+        Call c;
+        const Distill d(c, a);
+        const float scale = number(c, a[6]);
+        if (!c.ok) return nullptr;
+        const at::Tensor stats = c.dense(a[7], at::kFloat, {d.args.m, 3});
+        const float* const dloss = row_floats(c, a[8], d.args.m);
+        int64_t ld = 0;
+        void* const s = c.stream();
+        const at::Tensor dZ = gradient(c, a[9], d.Z, ld);
+        if (!c.ok) return nullptr;
+        if (g_lib.distill_grad(&d.args, (const float*)stats.data_ptr(), dloss, scale, dZ.data_ptr(), ld, s) != KQ_OK) return nullptr;
+        return a[9] != Py_None ? Py_NewRef(a[9]) : THPVariable_Wrap(dZ);
+    });
+}
+
 #define KQ_FAST(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, "the plain case of a call, or None"}
 PyMethodDef methods[] = {{"recon_args", recon_args, METH_O, "descriptor array of kq_reconstruct_stack, or None"},
                          {"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, "the library's functions, stream, scratch"},
@@ -501,6 +815,14 @@ PyMethodDef methods[] = {{"recon_args", recon_args, METH_O, "descriptor array of
                          KQ_FAST(checkpoint_restore),
                          KQ_FAST(grad_scales),
                          KQ_FAST(grad_weight),
+                         KQ_FAST(quantize_blocks),
+                         KQ_FAST(reconstruct_blocks),
+                         KQ_FAST(block_linear),
+                         KQ_FAST(block_grad_input),
+                         KQ_FAST(block_grad_weight),
+                         KQ_FAST(distill),
+                         KQ_FAST(distill_loss),
+                         KQ_FAST(distill_grad),
                          {nullptr, nullptr, 0, nullptr}};
 #undef KQ_FAST
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kqhost", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
