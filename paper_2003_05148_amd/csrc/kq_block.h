@@ -102,6 +102,8 @@ struct BlockGemmPlan {
     int bi, bj;              // output tile
     int splits, steps_per_split;
     size_t part_bytes;
+    int64_t rest_from;       // columns i from here on have a tile of their own, or 0
+    int rest_bi, rest_bj;
 };
 // exact: products on the 16-bit matrix instructions
 BlockGemmPlan block_gemm_plan(bool exact, int64_t I, int64_t J, int64_t C);

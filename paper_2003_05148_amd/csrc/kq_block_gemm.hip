@@ -342,42 +342,108 @@ __global__ __launch_bounds__(64 * WI * WJ, 1) void block_gemm_kernel(const Block
     }
 }
 
-BlockGemmPlan block_gemm_plan(bool exact, int64_t I, int64_t J, int64_t C) {
-    (void)exact;
+// The tile and the splits with the shortest modelled time.  A workgroup's block of the contraction takes `few` us where few
+// CUs have one, `full` where all 256 have (the clock and the caches give way), and a CU with n of them n times `shared`; a
+// split contraction pays the joining launch and its partial sums, written and read at about 6 MB a us.  Where the tiles of
+// 256 x 256 are a little over a number of full rounds, the columns of the last one are a product of their own (98 x 16 tiles
+// of 4096 deep: six rounds and 128 small tiles instead of seven).  Fitted to sweeps, us for one output size with 4096 deep,
+// 8-bit / exact:
+//   4096 x 256:  128x64 14.8 / 20.8, 128x128 18.1 / 21.5 (four splits), 256x256 28 / 33
+//   4096 x 1024: 128x64 25.5 / 38.3, 128x128 27.9 / 39.3, 256x256 40 / 51
+//   4096 x 2048: 128x64 50.6 / 71.0, 128x128 35.4 / 61.6, 256x256 52.7 / 75.8
+//   4096 x 4096: 128x64 95, 128x128 78 / 132, 256x256 59.8 / 110
+struct BlockTileTime {
+    int bi, bj;
+    float fixed;
+    float few[2], full[2], shared[2];  // 8-bit, exact
+};
+constexpr BlockTileTime kTiles[] = {
+    {128, 64, 4.0f, {0.30f, 0.33f}, {0.56f, 0.76f}, {0.365f, 0.53f}},
+    {128, 128, 5.0f, {0.33f, 0.50f}, {0.72f, 1.10f}, {0.53f, 0.90f}},
+    {256, 256, 9.0f, {0.55f, 1.00f}, {1.59f, 3.15f}, {1.59f, 3.10f}},
+};
+
+static float block_time(const BlockTileTime& t, bool exact, int64_t workgroups) {
+    if (workgroups <= 256) return t.few[exact] + (t.full[exact] - t.few[exact]) * (float)workgroups / 256.0f;
+    const float shared = (float)ceil_div64(workgroups, 256) * t.shared[exact];
+    return shared > t.full[exact] ? shared : t.full[exact];
+}
+
+static BlockGemmPlan one_plan(bool exact, int64_t I, int64_t J, int64_t steps, bool may_split, float& best) {
     BlockGemmPlan g = {};
-    const int64_t steps = block_pitch(C) / kBlock;
-    g.bi = 128;
-    g.bj = J <= 32 ? 32 : 128;
-    const int64_t tiles = ceil_div64(I, g.bi) * ceil_div64(J, g.bj);
+    const float value_us = (float)I * (float)J * 8.0f / 6e6f;
+    best = 0.0f;
     int64_t splits = 1;
-    while (tiles * splits < 256 && splits * 8 <= steps) splits *= 2;
-    g.steps_per_split = (int)(steps ? ceil_div64(steps, splits) : 1);
+    for (const BlockTileTime& t : kTiles) {
+        const int64_t tiles = ceil_div64(I, t.bi) * ceil_div64(J, t.bj);
+        for (int s = 1; s <= 32 && (s == 1 || (may_split && s * 4 <= steps && s * tiles <= 1024)); s = s < 4 ? s + 1 : s * 3 / 2) {
+            const float us = t.fixed + (float)ceil_div64(steps, s) * block_time(t, exact, tiles * s) + (s > 1 ? 2.5f + (float)s * value_us : 0.0f);
+            if (g.bi == 0 || us < best) {
+                best = us;
+                g.bi = t.bi;
+                g.bj = t.bj;
+                splits = s;
+            }
+        }
+    }
+    // (an even number of blocks a split: the kernel takes two at a time)
+    const int64_t per = splits > 1 ? ceil_div64(ceil_div64(steps, splits), 2) * 2 : steps;
+    g.steps_per_split = (int)(per ? per : 1);
     g.splits = steps ? (int)ceil_div64(steps, g.steps_per_split) : 1;
+    return g;
+}
+
+BlockGemmPlan block_gemm_plan(bool exact, int64_t I, int64_t J, int64_t C) {
+    const int64_t steps = block_pitch(C) / kBlock;
+    float best;
+    BlockGemmPlan g = one_plan(exact, I, J, steps, true, best);
     g.part_bytes = g.splits > 1 ? ((size_t)g.splits * (size_t)(I * J) * sizeof(float) + 255) & ~size_t(255) : 0;
+    const int64_t jtiles = ceil_div64(J, 256), rounds = ceil_div64(I, 256) * jtiles / 256;
+    const int64_t itiles = rounds * 256 / jtiles, rest = I - itiles * 256;
+    if (rounds > 0 && rest > 0) {
+        float rest_us;
+        const BlockGemmPlan r = one_plan(exact, rest, J, steps, false, rest_us);
+        const float us = 9.0f + (float)rounds * kTiles[2].shared[exact] * (float)steps + rest_us;
+        if (us < best) {
+            g = {256, 256, 1, (int)(steps ? steps : 1), 0, itiles * 256, r.bi, r.bj};
+        }
+    }
     return g;
 }
 
 template <bool EXACT, bool AROWS>
-static hipError_t launch_tile(const BlockGemmPlan& g, const BlockGemmParams& p, hipStream_t s) {
+static hipError_t launch_tile(int bi, int bj, BlockGemmParams p, hipStream_t s) {
+    p.itiles = (int)ceil_div64(p.I, bi);
+    p.jtiles = (int)ceil_div64(p.J, bj);
     const dim3 grid((unsigned)((int64_t)p.itiles * p.jtiles), (unsigned)p.splits);
-    const int tile = g.bi * 1000 + g.bj;
+    const int tile = bi * 1000 + bj;
     if (tile == 256256) block_gemm_kernel<EXACT, AROWS, 256, 256, 2, 2><<<grid, dim3(256), 0, s>>>(p);
     else if (tile == 128128) block_gemm_kernel<EXACT, AROWS, 128, 128, 2, 2><<<grid, dim3(256), 0, s>>>(p);
     else if (tile == 128064) block_gemm_kernel<EXACT, AROWS, 128, 64, 2, 2><<<grid, dim3(256), 0, s>>>(p);
-    else if (tile == 128032) block_gemm_kernel<EXACT, AROWS, 128, 32, 2, 1><<<grid, dim3(128), 0, s>>>(p);
     else return hipErrorInvalidValue;
     return hipGetLastError();
 }
+static hipError_t launch_form(bool exact, bool a_rows, int bi, int bj, const BlockGemmParams& p, hipStream_t s) {
+    if (exact) return a_rows ? launch_tile<true, true>(bi, bj, p, s) : launch_tile<true, false>(bi, bj, p, s);
+    return a_rows ? launch_tile<false, true>(bi, bj, p, s) : launch_tile<false, false>(bi, bj, p, s);
+}
 
 hipError_t launch_block_gemm(bool exact, bool a_rows, const BlockGemmPlan& plan, BlockGemmParams p, void* part, hipStream_t s) {
-    p.itiles = (int)ceil_div64(p.I, plan.bi);
-    p.jtiles = (int)ceil_div64(p.J, plan.bj);
     p.splits = plan.splits;
     p.steps_per_split = plan.steps_per_split;
     p.part = plan.splits > 1 ? (float*)part : nullptr;
-    hipError_t e;
-    if (exact) e = a_rows ? launch_tile<true, true>(plan, p, s) : launch_tile<true, false>(plan, p, s);
-    else e = a_rows ? launch_tile<false, true>(plan, p, s) : launch_tile<false, false>(plan, p, s);
+    if (plan.rest_from > 0) {  // (a multiple of 256: whole blocks of A's exponents)
+        BlockGemmParams r = p;
+        r.I = p.I - plan.rest_from;
+        r.A.v += plan.rest_from * p.A.pitch;
+        r.A.e += (a_rows ? plan.rest_from : plan.rest_from >> 7) * p.A.e_row;
+        r.out = (char*)p.out + plan.rest_from * (p.type == KQ_T_F32 ? 4 : 2);
+        if (p.bias) r.bias = p.bias + plan.rest_from;
+        p.I = plan.rest_from;
+        const hipError_t e = launch_form(exact, a_rows, plan.bi, plan.bj, p, s);
+        return e != hipSuccess ? e : launch_form(exact, a_rows, plan.rest_bi, plan.rest_bj, r, s);
+    }
+    const hipError_t e = launch_form(exact, a_rows, plan.bi, plan.bj, p, s);
     if (e != hipSuccess || plan.splits == 1) return e;
     const JoinParams j = {p.part, p.splits, p.J, p.I, p.bias, p.out, p.ldo, p.type};
     return launch_join(j, s);
