@@ -66,8 +66,8 @@ struct BlockReconstructParams {
 };
 hipError_t launch_reconstruct_blocks(const BlockReconstructParams& p, hipStream_t s);
 
-// out[c][r], r along the 128-row blocks of X, pitch rp (a multiple of 128, zeros past m).  Quantized along r again, or
-// (exps NULL: a weight) the same bytes.
+// out[c][r], r along the 128-row blocks of X, pitch rp (a multiple of 128, zeros past m): quantized along r (again, where X is
+// bytes), or the same bytes.
 struct BlockTransposeParams {
     const void* X;        // [m][cols], or bytes of pitch ldx with in_exps [m][ldx / 128]
     int64_t ldx;
@@ -75,10 +75,13 @@ struct BlockTransposeParams {
     const uint8_t* in_exps;
     int64_t m, cols, rp;
     uint8_t* values;      // [cols][rp]
-    uint8_t* exps;        // [cols][rp / 128], or NULL
+    uint8_t* exps;        // [cols][rp / 128]; not of the same bytes
     float* sums;          // [rp / 128][cols]: sums over each 128 rows, or NULL
 };
-hipError_t launch_transpose_blocks(const BlockTransposeParams& p, hipStream_t s);
+// dY quantized in blocks of one row, W's bytes transposed
+hipError_t launch_grad_input_operands(const BlockQuantizeParams& q, const BlockTransposeParams& t, hipStream_t s);
+// X's values and dY, transposed and quantized along the rows
+hipError_t launch_grad_weight_operands(const BlockTransposeParams& x, const BlockTransposeParams& dy, hipStream_t s);
 
 struct BlockOperand {
     const uint8_t* v;
@@ -97,6 +100,9 @@ struct BlockGemmParams {
     float* part;             // partial sums of a split contraction, or NULL
     int splits, steps_per_split;
     int itiles, jtiles;
+    float* dbias;            // [J] or NULL: the sum of bias_parts rows of bias_part [bias_parts][J]
+    const float* bias_part;
+    int bias_parts;
 };
 struct BlockGemmPlan {
     int bi, bj;              // output tile

@@ -8,9 +8,9 @@ namespace kq {
 // ---- blocks of one row -------------------------------------------------------------------------------------
 // Sixteen lanes a block, 8 columns a lane.  a 2^-e is exact, so the conversion's rounding is the only one.
 template <int TYPE>
-__global__ __launch_bounds__(256) void quantize_rows_kernel(const BlockQuantizeParams p) {
+__device__ __forceinline__ void quantize_rows(const BlockQuantizeParams& p, unsigned workgroup) {
     const unsigned per_row = (unsigned)(p.kp >> 3);       // 8-column pieces
-    const unsigned id = blockIdx.x * 256u + threadIdx.x;  // (at most 2^34 values and their padding: fewer than 2^32 threads)
+    const unsigned id = workgroup * 256u + threadIdx.x;  // (at most 2^34 values and their padding: fewer than 2^32 threads)
     const int64_t row = id / per_row;
     const bool live = row < p.m;                          // (blocks are whole: the lanes of one agree)
     const int c0 = live ? (int)(id - (unsigned)row * per_row) * 8 : 0;
@@ -37,6 +37,11 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const BlockQuantizeP
     *(u32x2*)(p.values + row * p.kp + c0) = w;
     if ((threadIdx.x & 15) == 0) p.exps[row * (p.kp >> 7) + (c0 >> 7)] = (uint8_t)e;
 }
+template <int TYPE>
+__global__ __launch_bounds__(256) void quantize_rows_kernel(const BlockQuantizeParams p) {
+    quantize_rows<TYPE>(p, blockIdx.x);
+}
+static unsigned quantize_rows_workgroups(const BlockQuantizeParams& p) { return (unsigned)ceil_div64(p.m * (p.kp >> 3), 256); }
 
 // ---- blocks of 128 rows ------------------------------------------------------------------------------------
 // A workgroup a block, 16 lanes a row of it, eight rows a thread.
@@ -85,7 +90,7 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(const BlockQuantize
 hipError_t launch_quantize_blocks(const BlockQuantizeParams& p, int rows, hipStream_t s) {
     const dim3 block(256);
     if (rows == 1) {
-        const dim3 grid((unsigned)ceil_div64(p.m * (p.kp >> 3), 256));
+        const dim3 grid(quantize_rows_workgroups(p));
         if (p.type == KQ_T_F32) quantize_rows_kernel<KQ_T_F32><<<grid, block, 0, s>>>(p);
         else if (p.type == KQ_T_BF16) quantize_rows_kernel<KQ_T_BF16><<<grid, block, 0, s>>>(p);
         else quantize_rows_kernel<KQ_T_F16><<<grid, block, 0, s>>>(p);
@@ -130,26 +135,19 @@ hipError_t launch_reconstruct_blocks(const BlockReconstructParams& p, hipStream_
 // ---- transposed, and quantized along the other direction ---------------------------------------------------
 // A workgroup takes 128 rows by 128 columns; a thread 8 neighbouring rows of 8 neighbouring columns, so that what it
 // writes to LDS transposed are 8-byte pieces.  Piece q of column c lies at q ^ (c / 8): the sixteen column groups of a
-// wave's store fall on sixteen different pieces.
-template <int TYPE>
-__device__ __forceinline__ void load_bytes_or_columns(const BlockTransposeParams& p, int64_t row, int64_t c0, float (&v)[8]) {
-    if (row >= p.m || c0 >= p.cols) {
-#pragma unroll
-        for (int t = 0; t < 8; ++t) v[t] = 0.0f;
-    } else if constexpr (TYPE == KQ_T_E4M3) {
-        const u32x2 w = *(const u32x2*)((const uint8_t*)p.X + row * p.ldx + c0);
-        const float step = checkpoint_step(p.in_exps[row * (p.ldx >> 7) + (c0 >> 7)]);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            v[4 * h] = __builtin_amdgcn_cvt_f32_fp8((int)w[h], 0) * step;
-            v[4 * h + 1] = __builtin_amdgcn_cvt_f32_fp8((int)w[h], 1) * step;
-            v[4 * h + 2] = __builtin_amdgcn_cvt_f32_fp8((int)w[h], 2) * step;
-            v[4 * h + 3] = __builtin_amdgcn_cvt_f32_fp8((int)w[h], 3) * step;
-        }
-    } else {
-        load_columns<TYPE>(p.X, row * p.ldx, (int)c0, (int)p.cols, v);
-    }
+// wave's store fall on sixteen different pieces.  All of a thread's loads are on their way before the first is used.
+struct TransposeShared {
+    u32x2 t[128 * 16];
+    unsigned max[4][128];
+    float sum[4][128];
+};
+__device__ __forceinline__ unsigned tile_of(const BlockTransposeParams& p, unsigned workgroup, int64_t& r0, int64_t& c0) {
+    const unsigned ctiles = (unsigned)((p.cols + 127) >> 7), rt = workgroup / ctiles;
+    c0 = (int64_t)(workgroup - rt * ctiles) * 128;
+    r0 = (int64_t)rt * 128;
+    return rt;
 }
+static unsigned transpose_workgroups(const BlockTransposeParams& p) { return (unsigned)(ceil_div64(p.cols, 128) * (p.rp >> 7)); }
 
 // 128 columns of 128 bytes, from LDS to memory
 __device__ __forceinline__ void store_transposed(const BlockTransposeParams& p, const u32x2* s_t, int64_t r0, int64_t c0) {
@@ -161,77 +159,147 @@ __device__ __forceinline__ void store_transposed(const BlockTransposeParams& p, 
     }
 }
 
+// A thread's 8 x 8 values as they lie in memory: zeros past the matrix.
 template <int TYPE>
-__global__ __launch_bounds__(256) void transpose_quantize_kernel(const BlockTransposeParams p) {
-    __shared__ u32x2 s_t[128 * 16];
-    __shared__ unsigned s_max[4][128];
-    __shared__ float s_sum[4][128];
+struct RawTile {
+    static constexpr int kWords = TYPE == KQ_T_F32 ? 8 : TYPE == KQ_T_E4M3 ? 2 : 4;
+    unsigned w[8][kWords];
+    unsigned e[8];
+    __device__ __forceinline__ void load(const BlockTransposeParams& p, int64_t r0, int64_t c0, bool whole) {
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            const int64_t row = min(r0 + t, p.m - 1);
+            if constexpr (TYPE == KQ_T_E4M3) {  // (whole padded rows)
+                __builtin_memcpy(w[t], (const uint8_t*)p.X + row * p.ldx + c0, 8);
+                e[t] = p.in_exps[row * (p.ldx >> 7) + (c0 >> 7)];
+            } else {
+                const char* at = (const char*)p.X + (row * p.ldx + c0) * (TYPE == KQ_T_F32 ? 4 : 2);
+                if (whole) {
+                    __builtin_memcpy(w[t], at, 4 * kWords);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kWords; ++j) {
+                        if constexpr (TYPE == KQ_T_F32) {
+                            w[t][j] = c0 + j < p.cols ? ((const unsigned*)at)[j] : 0u;
+                        } else {
+                            const unsigned lo = c0 + 2 * j < p.cols ? ((const uint16_t*)at)[2 * j] : 0u;
+                            const unsigned hi = c0 + 2 * j + 1 < p.cols ? ((const uint16_t*)at)[2 * j + 1] : 0u;
+                            w[t][j] = lo | hi << 16;
+                        }
+                    }
+                }
+            }
+        }
+        if (r0 + 8 > p.m) {
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+                if (r0 + t >= p.m) {
+                    e[t] = 0;
+#pragma unroll
+                    for (int j = 0; j < kWords; ++j) w[t][j] = 0;
+                }
+        }
+    }
+    // columns 2 j and 2 j + 1 of row t
+    __device__ __forceinline__ void pair(int t, int j, float& a, float& b) const {
+        if constexpr (TYPE == KQ_T_F32) {
+            a = __builtin_bit_cast(float, w[t][2 * j]);
+            b = __builtin_bit_cast(float, w[t][2 * j + 1]);
+        } else if constexpr (TYPE == KQ_T_E4M3) {
+            const f32x2 v = j & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)w[t][j >> 1], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)w[t][j >> 1], false);
+            const float step = checkpoint_step(e[t]);
+            a = v.x * step;
+            b = v.y * step;
+        } else {
+            a = Act<TYPE == KQ_T_BF16>::lo(w[t][j]);
+            b = Act<TYPE == KQ_T_BF16>::hi(w[t][j]);
+        }
+    }
+};
+
+template <int TYPE>
+__device__ __forceinline__ void transpose_quantize(const BlockTransposeParams& p, unsigned workgroup, TransposeShared& s) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = tid & 15, rg = tid >> 4;
-    const unsigned ctiles = (unsigned)((p.cols + 127) >> 7), rt = blockIdx.x / ctiles;
-    const int64_t c0 = (int64_t)(blockIdx.x - rt * ctiles) * 128, r0 = (int64_t)rt * 128;
-    float v[8][8];
+    int64_t r0, c0;
+    const unsigned rt = tile_of(p, workgroup, r0, c0);
+    RawTile<TYPE> raw;
+    raw.load(p, r0 + 8 * rg, c0 + 8 * l16, c0 + 128 <= p.cols);
 #pragma unroll
-    for (int t = 0; t < 8; ++t) load_bytes_or_columns<TYPE>(p, r0 + 8 * rg + t, c0 + 8 * l16, v[t]);
+    for (int j = 0; j < 4; ++j) {
+        float a = 0.0f, b = 0.0f, sa = 0.0f, sb = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        unsigned a = 0;
-#pragma unroll
-        for (int t = 0; t < 8; ++t) a = max(a, __builtin_bit_cast(unsigned, v[t][j]) & 0x7fffffffu);
-        a = max(a, (unsigned)__shfl_xor(a, 16));
-        a = max(a, (unsigned)__shfl_xor(a, 32));
-        if (lane < 16) s_max[wave][8 * l16 + j] = a;
-    }
-    if (p.sums) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float s = 0.0f;
-#pragma unroll
-            for (int t = 0; t < 8; ++t) s += v[t][j];
-            s += __shfl_xor(s, 16);
-            s += __shfl_xor(s, 32);
-            if (lane < 16) s_sum[wave][8 * l16 + j] = s;
+        for (int t = 0; t < 8; ++t) {
+            float x, y;
+            raw.pair(t, j, x, y);
+            a = __builtin_elementwise_maximum(a, __builtin_fabsf(x));  // (a NaN stays)
+            b = __builtin_elementwise_maximum(b, __builtin_fabsf(y));
+            sa += x;
+            sb += y;
+        }
+        unsigned ma = __builtin_bit_cast(unsigned, a) & 0x7fffffffu, mb = __builtin_bit_cast(unsigned, b) & 0x7fffffffu;
+        ma = max(ma, (unsigned)__shfl_xor(ma, 16));
+        mb = max(mb, (unsigned)__shfl_xor(mb, 16));
+        ma = max(ma, (unsigned)__shfl_xor(ma, 32));
+        mb = max(mb, (unsigned)__shfl_xor(mb, 32));
+        if (lane < 16) {
+            s.max[wave][8 * l16 + 2 * j] = ma;
+            s.max[wave][8 * l16 + 2 * j + 1] = mb;
+        }
+        if (p.sums) {
+            sa += __shfl_xor(sa, 16);
+            sb += __shfl_xor(sb, 16);
+            sa += __shfl_xor(sa, 32);
+            sb += __shfl_xor(sb, 32);
+            if (lane < 16) {
+                s.sum[wave][8 * l16 + 2 * j] = sa;
+                s.sum[wave][8 * l16 + 2 * j + 1] = sb;
+            }
         }
     }
     __syncthreads();
+    auto exponent = [&](int c) { return block_exponent(max(max(s.max[0][c], s.max[1][c]), max(s.max[2][c], s.max[3][c]))); };
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int c = 8 * l16 + j;
-        const unsigned e = block_exponent(max(max(s_max[0][c], s_max[1][c]), max(s_max[2][c], s_max[3][c])));
-        u32x2 w = {kNaN4, kNaN4};
-        if (e != 255u) {
-            const float inv = block_inverse(e);
-            w = u32x2{encode4(v[0][j], v[1][j], v[2][j], v[3][j], inv), encode4(v[4][j], v[5][j], v[6][j], v[7][j], inv)};
-        }
-        s_t[c * 16 + (rg ^ l16)] = w;
+    for (int j = 0; j < 4; ++j) {
+        const int c = 8 * l16 + 2 * j;
+        const unsigned ea = exponent(c), eb = exponent(c + 1);
+        float x[8], y[8];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) raw.pair(t, j, x[t], y[t]);
+        const float ia = block_inverse(ea == 255u ? 127u : ea), ib = block_inverse(eb == 255u ? 127u : eb);
+        u32x2 a = {encode4(x[0], x[1], x[2], x[3], ia), encode4(x[4], x[5], x[6], x[7], ia)};
+        u32x2 b = {encode4(y[0], y[1], y[2], y[3], ib), encode4(y[4], y[5], y[6], y[7], ib)};
+        if (ea == 255u) a = u32x2{kNaN4, kNaN4};
+        if (eb == 255u) b = u32x2{kNaN4, kNaN4};
+        s.t[c * 16 + (rg ^ l16)] = a;
+        s.t[(c + 1) * 16 + (rg ^ l16)] = b;
     }
     __syncthreads();
-    store_transposed(p, s_t, r0, c0);
+    store_transposed(p, s.t, r0, c0);
     if (tid < 128 && c0 + tid < p.cols) {
-        p.exps[(c0 + tid) * (p.rp >> 7) + rt] =
-            (uint8_t)block_exponent(max(max(s_max[0][tid], s_max[1][tid]), max(s_max[2][tid], s_max[3][tid])));
-        if (p.sums) p.sums[(int64_t)rt * p.cols + c0 + tid] = ((s_sum[0][tid] + s_sum[1][tid]) + s_sum[2][tid]) + s_sum[3][tid];
+        p.exps[(c0 + tid) * (p.rp >> 7) + rt] = (uint8_t)exponent(tid);
+        if (p.sums) p.sums[(int64_t)rt * p.cols + c0 + tid] = ((s.sum[0][tid] + s.sum[1][tid]) + s.sum[2][tid]) + s.sum[3][tid];
     }
 }
 
 // The same bytes transposed.
-__global__ __launch_bounds__(256) void transpose_bytes_kernel(const BlockTransposeParams p) {
-    __shared__ u32x2 s_t[128 * 16];
+__device__ __forceinline__ void transpose_bytes(const BlockTransposeParams& p, unsigned workgroup, u32x2* s_t) {
     const int tid = threadIdx.x, l16 = tid & 15, rg = tid >> 4;
-    const unsigned ctiles = (unsigned)((p.cols + 127) >> 7), rt = blockIdx.x / ctiles;
-    const int64_t c0 = (int64_t)(blockIdx.x - rt * ctiles) * 128, r0 = (int64_t)rt * 128;
-    u32x2 v[8];
+    int64_t r0, c0;
+    tile_of(p, workgroup, r0, c0);
+    RawTile<KQ_T_E4M3> raw;
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {  // (a column piece past the matrix is inside the padded row)
-        const int64_t row = r0 + 8 * rg + t;
-        v[t] = row < p.m ? *(const u32x2*)((const uint8_t*)p.X + row * p.ldx + c0 + 8 * l16) : u32x2{0, 0};
-    }
+    for (int t = 0; t < 8; ++t)
+        __builtin_memcpy(raw.w[t], (const uint8_t*)p.X + min(r0 + 8 * rg + t, p.m - 1) * p.ldx + c0 + 8 * l16, 8);
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+        if (r0 + 8 * rg + t >= p.m) raw.w[t][0] = raw.w[t][1] = 0;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         // 4 x 4 bytes: rows 4 g .. 4 g + 3 of columns 4 h .. 4 h + 3
         unsigned o[4][2];
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-            const unsigned a = v[4 * g][h], b = v[4 * g + 1][h], c = v[4 * g + 2][h], d = v[4 * g + 3][h];
+            const unsigned a = raw.w[4 * g][h], b = raw.w[4 * g + 1][h], c = raw.w[4 * g + 2][h], d = raw.w[4 * g + 3][h];
             const unsigned ab0 = __builtin_amdgcn_perm(b, a, 0x05010400u), ab1 = __builtin_amdgcn_perm(b, a, 0x07030602u);
             const unsigned cd0 = __builtin_amdgcn_perm(d, c, 0x05010400u), cd1 = __builtin_amdgcn_perm(d, c, 0x07030602u);
             o[0][g] = __builtin_amdgcn_perm(cd0, ab0, 0x05040100u);
@@ -246,13 +314,35 @@ __global__ __launch_bounds__(256) void transpose_bytes_kernel(const BlockTranspo
     store_transposed(p, s_t, r0, c0);
 }
 
-hipError_t launch_transpose_blocks(const BlockTransposeParams& p, hipStream_t s) {
-    const dim3 grid((unsigned)(ceil_div64(p.cols, 128) * (p.rp >> 7))), block(256);
-    if (p.exps == nullptr) transpose_bytes_kernel<<<grid, block, 0, s>>>(p);
-    else if (p.type == KQ_T_E4M3) transpose_quantize_kernel<KQ_T_E4M3><<<grid, block, 0, s>>>(p);
-    else if (p.type == KQ_T_F32) transpose_quantize_kernel<KQ_T_F32><<<grid, block, 0, s>>>(p);
-    else if (p.type == KQ_T_BF16) transpose_quantize_kernel<KQ_T_BF16><<<grid, block, 0, s>>>(p);
-    else transpose_quantize_kernel<KQ_T_F16><<<grid, block, 0, s>>>(p);
+// Both operands of a gradient in one launch, the first `first` workgroups the first of them: two short passes after each
+// other leave half the chip idle at their ends, and each launch costs 2 to 3 us.
+template <int TYPE>
+__global__ __launch_bounds__(256) void grad_input_operands_kernel(const BlockQuantizeParams q, const BlockTransposeParams t, unsigned first) {
+    __shared__ u32x2 s_t[128 * 16];
+    if (blockIdx.x < first) transpose_bytes(t, blockIdx.x, s_t);
+    else quantize_rows<TYPE>(q, blockIdx.x - first);
+}
+template <int TYPE>
+__global__ __launch_bounds__(256) void grad_weight_operands_kernel(const BlockTransposeParams x, const BlockTransposeParams dy, unsigned first) {
+    __shared__ TransposeShared s;
+    if (blockIdx.x < first) transpose_quantize<KQ_T_E4M3>(x, blockIdx.x, s);
+    else transpose_quantize<TYPE>(dy, blockIdx.x - first, s);
+}
+
+hipError_t launch_grad_input_operands(const BlockQuantizeParams& q, const BlockTransposeParams& t, hipStream_t s) {
+    const unsigned first = transpose_workgroups(t);
+    const dim3 grid(first + quantize_rows_workgroups(q)), block(256);
+    if (q.type == KQ_T_F32) grad_input_operands_kernel<KQ_T_F32><<<grid, block, 0, s>>>(q, t, first);
+    else if (q.type == KQ_T_BF16) grad_input_operands_kernel<KQ_T_BF16><<<grid, block, 0, s>>>(q, t, first);
+    else grad_input_operands_kernel<KQ_T_F16><<<grid, block, 0, s>>>(q, t, first);
+    return hipGetLastError();
+}
+hipError_t launch_grad_weight_operands(const BlockTransposeParams& x, const BlockTransposeParams& dy, hipStream_t s) {
+    const unsigned first = transpose_workgroups(x);
+    const dim3 grid(first + transpose_workgroups(dy)), block(256);
+    if (dy.type == KQ_T_F32) grad_weight_operands_kernel<KQ_T_F32><<<grid, block, 0, s>>>(x, dy, first);
+    else if (dy.type == KQ_T_BF16) grad_weight_operands_kernel<KQ_T_BF16><<<grid, block, 0, s>>>(x, dy, first);
+    else grad_weight_operands_kernel<KQ_T_F16><<<grid, block, 0, s>>>(x, dy, first);
     return hipGetLastError();
 }
 

@@ -176,10 +176,9 @@ kq_status kq_block_linear_grad_input(const void* dY, int32_t type, int64_t ldy, 
     float* const part = r.take<float>(z.plan.part_bytes);
     const int64_t np = block_pitch(n), kp = block_pitch(k);
     const BlockQuantizeParams q = {dY, ldy, type, m, n, np, r.take(z.dy), r.take(z.dy_exps)};
-    hipError_t e = launch_quantize_blocks(q, 1, s);
-    if (e != hipSuccess) return hip_status(e);
     const BlockTransposeParams t = {values, kp, KQ_T_E4M3, nullptr, n, k, np, r.take(z.wt), nullptr, nullptr};
-    if ((e = launch_transpose_blocks(t, s)) != hipSuccess) return hip_status(e);
+    const hipError_t e = launch_grad_input_operands(q, t, s);
+    if (e != hipSuccess) return hip_status(e);
     BlockGemmParams p = {};
     p.A = {t.values, np, exps, 1, kp / kBlock};  // row block of W^T = column block of W
     p.B = {q.values, np, q.exps, np / kBlock, 1};
@@ -217,23 +216,21 @@ kq_status kq_block_linear_grad_weight(const void* dY, int32_t type, int64_t ldy,
     p.out = dW;
     p.type = dw_type;
     p.ldo = lddw;
-    float *part = nullptr, *sums = nullptr;
-    hipError_t e;
+    float* part = nullptr;
     if (m > 0) {
         Regions r = {(char*)ws};
         part = r.take<float>(z.plan.part_bytes);
         const BlockTransposeParams g = {dY, ldy, type, nullptr, m, n, mp, r.take(z.dyt), r.take(z.dyt_exps),
-                                        dbias ? sums = r.take<float>(z.sums) : nullptr};
-        if ((e = launch_transpose_blocks(g, s)) != hipSuccess) return hip_status(e);
+                                        dbias ? r.take<float>(z.sums) : nullptr};
         const BlockTransposeParams x = {x_values, kp, KQ_T_E4M3, x_exps, m, k, mp, r.take(z.xt), r.take(z.xt_exps), nullptr};
-        if ((e = launch_transpose_blocks(x, s)) != hipSuccess) return hip_status(e);
+        const hipError_t e = launch_grad_weight_operands(x, g, s);
+        if (e != hipSuccess) return hip_status(e);
         p.A = {x.values, mp, x.exps, mp / kBlock, 1};
         p.B = {g.values, mp, g.exps, mp / kBlock, 1};
+        p.bias_part = g.sums;
+        p.bias_parts = (int)(mp / kBlock);
     }
-    if (dbias) {
-        const JoinParams j = {sums, (int)(mp / kBlock), 1, n, nullptr, dbias, n, KQ_T_F32};
-        if ((e = launch_join(j, s)) != hipSuccess) return hip_status(e);
-    }
+    p.dbias = dbias;
     return hip_status(launch_block_gemm(dw_type == KQ_T_F32, true, z.plan, p, part, s));
 }
 

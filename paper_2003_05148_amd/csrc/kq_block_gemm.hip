@@ -315,6 +315,16 @@ __global__ __launch_bounds__(64 * WI * WJ, 1) void block_gemm_kernel(const Block
         __builtin_amdgcn_s_waitcnt(waitcnt(0, 0));  // (no load may arrive in LDS after the workgroup's end)
     }
 
+    if constexpr (AROWS) {  // the bias' gradient from its partial sums, once
+        if (p.dbias && i0 == 0 && blockIdx.y == 0) {
+            for (int64_t j = j0 + tid; j < min(j0 + BJ, p.J); j += 64 * WAVES) {
+                float v = 0.0f;
+                for (int t = 0; t < p.bias_parts; ++t) v += p.bias_part[(int64_t)t * p.J + j];
+                p.dbias[j] = v;
+            }
+        }
+    }
+
     // Lane holds out[j][i .. i + 3] for j = its column, i = 8 g + 4 half of a 32 x 32 tile: neighbours by fours, rows apart.
     // They go through LDS, 32 rows of the wave at a time in a part of its own, and leave as whole rows (of 4096 x 4096
     // bf16, stored by fours: 11 us).
@@ -439,6 +449,7 @@ hipError_t launch_block_gemm(bool exact, bool a_rows, const BlockGemmPlan& plan,
         r.A.e += (a_rows ? plan.rest_from : plan.rest_from >> 7) * p.A.e_row;
         r.out = (char*)p.out + plan.rest_from * (p.type == KQ_T_F32 ? 4 : 2);
         if (p.bias) r.bias = p.bias + plan.rest_from;
+        r.dbias = nullptr;
         p.I = plan.rest_from;
         const hipError_t e = launch_form(exact, a_rows, plan.bi, plan.bj, p, s);
         return e != hipSuccess ? e : launch_form(exact, a_rows, plan.rest_bi, plan.rest_bj, r, s);
