@@ -138,7 +138,7 @@ hipError_t launch_reconstruct_blocks(const BlockReconstructParams& p, hipStream_
 // wave's store fall on sixteen different pieces.  All of a thread's loads are on their way before the first is used.
 struct TransposeShared {
     u32x2 t[128 * 16];
-    unsigned max[4][128];
+    unsigned exps[4][64];   // of two neighbouring columns
     float sum[4][128];
 };
 __device__ __forceinline__ unsigned tile_of(const BlockTransposeParams& p, unsigned workgroup, int64_t& r0, int64_t& c0) {
@@ -163,38 +163,55 @@ __device__ __forceinline__ void store_transposed(const BlockTransposeParams& p, 
 template <int TYPE>
 struct RawTile {
     static constexpr int kWords = TYPE == KQ_T_F32 ? 8 : TYPE == KQ_T_E4M3 ? 2 : 4;
+    static constexpr int kBytes = TYPE == KQ_T_F32 ? 4 : TYPE == KQ_T_E4M3 ? 1 : 2;
     unsigned w[8][kWords];
-    unsigned e[8];
-    __device__ __forceinline__ void load(const BlockTransposeParams& p, int64_t r0, int64_t c0, bool whole) {
+    float step[8];   // KQ_T_E4M3: the row's power of two
+    __device__ __forceinline__ void load(const BlockTransposeParams& p, int64_t r0, int64_t c0, bool with_exps = true) {
+        const int64_t first = min(r0, p.m - 1);
+        const int last = (int)min(p.m - 1 - first, (int64_t)7);  // (rows past it: again, and cleared below)
+        const char* at = (const char*)p.X + first * p.ldx * kBytes;
+        if (TYPE == KQ_T_E4M3 || c0 + 8 <= p.cols) {  // (bytes: whole padded rows)
+            at += c0 * kBytes;
 #pragma unroll
-        for (int t = 0; t < 8; ++t) {
-            const int64_t row = min(r0 + t, p.m - 1);
-            if constexpr (TYPE == KQ_T_E4M3) {  // (whole padded rows)
-                __builtin_memcpy(w[t], (const uint8_t*)p.X + row * p.ldx + c0, 8);
-                e[t] = p.in_exps[row * (p.ldx >> 7) + (c0 >> 7)];
-            } else {
-                const char* at = (const char*)p.X + (row * p.ldx + c0) * (TYPE == KQ_T_F32 ? 4 : 2);
-                if (whole) {
-                    __builtin_memcpy(w[t], at, 4 * kWords);
-                } else {
+            for (int t = 0; t < 8; ++t) {
+                __builtin_memcpy(w[t], at, 4 * kWords);
+                at += t < last ? p.ldx * kBytes : 0;
+            }
+        } else {  // a row's end: loads at clamped places, all at once
 #pragma unroll
-                    for (int j = 0; j < kWords; ++j) {
-                        if constexpr (TYPE == KQ_T_F32) {
-                            w[t][j] = c0 + j < p.cols ? ((const unsigned*)at)[j] : 0u;
-                        } else {
-                            const unsigned lo = c0 + 2 * j < p.cols ? ((const uint16_t*)at)[2 * j] : 0u;
-                            const unsigned hi = c0 + 2 * j + 1 < p.cols ? ((const uint16_t*)at)[2 * j + 1] : 0u;
-                            w[t][j] = lo | hi << 16;
-                        }
+            for (int t = 0; t < 8; ++t) {
+#pragma unroll
+                for (int j = 0; j < kWords; ++j) {
+                    if constexpr (TYPE == KQ_T_F32) {
+                        const unsigned v = ((const unsigned*)at)[min(c0 + j, p.cols - 1)];
+                        w[t][j] = c0 + j < p.cols ? v : 0u;
+                    } else {
+                        const unsigned lo = ((const uint16_t*)at)[min(c0 + 2 * j, p.cols - 1)], hi = ((const uint16_t*)at)[min(c0 + 2 * j + 1, p.cols - 1)];
+                        w[t][j] = (c0 + 2 * j < p.cols ? lo : 0u) | (c0 + 2 * j + 1 < p.cols ? hi << 16 : 0u);
                     }
                 }
+                at += t < last ? p.ldx * kBytes : 0;
+            }
+        }
+        if constexpr (TYPE == KQ_T_E4M3) {
+            if (with_exps) {
+                const int64_t pitch = p.ldx >> 7;
+                const uint8_t* e = p.in_exps + first * pitch + (c0 >> 7);
+                unsigned x[8];
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {
+                    x[t] = *e;
+                    e += t < last ? pitch : 0;
+                }
+#pragma unroll
+                for (int t = 0; t < 8; ++t) step[t] = checkpoint_step(x[t]);
             }
         }
         if (r0 + 8 > p.m) {
 #pragma unroll
             for (int t = 0; t < 8; ++t)
                 if (r0 + t >= p.m) {
-                    e[t] = 0;
+                    step[t] = 0.0f;
 #pragma unroll
                     for (int j = 0; j < kWords; ++j) w[t][j] = 0;
                 }
@@ -207,9 +224,8 @@ struct RawTile {
             b = __builtin_bit_cast(float, w[t][2 * j + 1]);
         } else if constexpr (TYPE == KQ_T_E4M3) {
             const f32x2 v = j & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)w[t][j >> 1], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)w[t][j >> 1], false);
-            const float step = checkpoint_step(e[t]);
-            a = v.x * step;
-            b = v.y * step;
+            a = v.x * step[t];
+            b = v.y * step[t];
         } else {
             a = Act<TYPE == KQ_T_BF16>::lo(w[t][j]);
             b = Act<TYPE == KQ_T_BF16>::hi(w[t][j]);
@@ -217,13 +233,20 @@ struct RawTile {
     }
 };
 
-template <int TYPE>
+__device__ __forceinline__ unsigned max_u16x2(unsigned a, unsigned b) {
+    using u16x2 = __attribute__((ext_vector_type(2))) unsigned short;
+    return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
+template <int TYPE, bool SUMS>
 __device__ __forceinline__ void transpose_quantize(const BlockTransposeParams& p, unsigned workgroup, TransposeShared& s) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = tid & 15, rg = tid >> 4;
     int64_t r0, c0;
     const unsigned rt = tile_of(p, workgroup, r0, c0);
     RawTile<TYPE> raw;
-    raw.load(p, r0 + 8 * rg, c0 + 8 * l16, c0 + 128 <= p.cols);
+    raw.load(p, r0 + 8 * rg, c0 + 8 * l16);
+    // A block's exponent is the largest of its rows' (it never falls as the magnitude grows), so exponents are exchanged, two
+    // columns a register.
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         float a = 0.0f, b = 0.0f, sa = 0.0f, sb = 0.0f;
@@ -233,19 +256,16 @@ __device__ __forceinline__ void transpose_quantize(const BlockTransposeParams& p
             raw.pair(t, j, x, y);
             a = __builtin_elementwise_maximum(a, __builtin_fabsf(x));  // (a NaN stays)
             b = __builtin_elementwise_maximum(b, __builtin_fabsf(y));
-            sa += x;
-            sb += y;
+            if constexpr (SUMS) {
+                sa += x;
+                sb += y;
+            }
         }
-        unsigned ma = __builtin_bit_cast(unsigned, a) & 0x7fffffffu, mb = __builtin_bit_cast(unsigned, b) & 0x7fffffffu;
-        ma = max(ma, (unsigned)__shfl_xor(ma, 16));
-        mb = max(mb, (unsigned)__shfl_xor(mb, 16));
-        ma = max(ma, (unsigned)__shfl_xor(ma, 32));
-        mb = max(mb, (unsigned)__shfl_xor(mb, 32));
-        if (lane < 16) {
-            s.max[wave][8 * l16 + 2 * j] = ma;
-            s.max[wave][8 * l16 + 2 * j + 1] = mb;
-        }
-        if (p.sums) {
+        unsigned e = block_exponent(__builtin_bit_cast(unsigned, a) & 0x7fffffffu) | block_exponent(__builtin_bit_cast(unsigned, b) & 0x7fffffffu) << 16;
+        e = max_u16x2(e, (unsigned)__shfl_xor(e, 16));
+        e = max_u16x2(e, (unsigned)__shfl_xor(e, 32));
+        if (lane < 16) s.exps[wave][4 * l16 + j] = e;
+        if constexpr (SUMS) {
             sa += __shfl_xor(sa, 16);
             sb += __shfl_xor(sb, 16);
             sa += __shfl_xor(sa, 32);
@@ -257,11 +277,11 @@ __device__ __forceinline__ void transpose_quantize(const BlockTransposeParams& p
         }
     }
     __syncthreads();
-    auto exponent = [&](int c) { return block_exponent(max(max(s.max[0][c], s.max[1][c]), max(s.max[2][c], s.max[3][c]))); };
+    auto exponents = [&](int pair) { return max_u16x2(max_u16x2(s.exps[0][pair], s.exps[1][pair]), max_u16x2(s.exps[2][pair], s.exps[3][pair])); };
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int c = 8 * l16 + 2 * j;
-        const unsigned ea = exponent(c), eb = exponent(c + 1);
+        const unsigned e = exponents(4 * l16 + j), ea = e & 0xffffu, eb = e >> 16;
         float x[8], y[8];
 #pragma unroll
         for (int t = 0; t < 8; ++t) raw.pair(t, j, x[t], y[t]);
@@ -276,8 +296,8 @@ __device__ __forceinline__ void transpose_quantize(const BlockTransposeParams& p
     __syncthreads();
     store_transposed(p, s.t, r0, c0);
     if (tid < 128 && c0 + tid < p.cols) {
-        p.exps[(c0 + tid) * (p.rp >> 7) + rt] = (uint8_t)exponent(tid);
-        if (p.sums) p.sums[(int64_t)rt * p.cols + c0 + tid] = ((s.sum[0][tid] + s.sum[1][tid]) + s.sum[2][tid]) + s.sum[3][tid];
+        p.exps[(c0 + tid) * (p.rp >> 7) + rt] = (uint8_t)(exponents(tid >> 1) >> (16 * (tid & 1)));
+        if constexpr (SUMS) p.sums[(int64_t)rt * p.cols + c0 + tid] = ((s.sum[0][tid] + s.sum[1][tid]) + s.sum[2][tid]) + s.sum[3][tid];
     }
 }
 
@@ -287,12 +307,7 @@ __device__ __forceinline__ void transpose_bytes(const BlockTransposeParams& p, u
     int64_t r0, c0;
     tile_of(p, workgroup, r0, c0);
     RawTile<KQ_T_E4M3> raw;
-#pragma unroll
-    for (int t = 0; t < 8; ++t)
-        __builtin_memcpy(raw.w[t], (const uint8_t*)p.X + min(r0 + 8 * rg + t, p.m - 1) * p.ldx + c0 + 8 * l16, 8);
-#pragma unroll
-    for (int t = 0; t < 8; ++t)
-        if (r0 + 8 * rg + t >= p.m) raw.w[t][0] = raw.w[t][1] = 0;
+    raw.load(p, r0 + 8 * rg, c0 + 8 * l16, false);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         // 4 x 4 bytes: rows 4 g .. 4 g + 3 of columns 4 h .. 4 h + 3
@@ -325,8 +340,9 @@ __global__ __launch_bounds__(256) void grad_input_operands_kernel(const BlockQua
 template <int TYPE>
 __global__ __launch_bounds__(256) void grad_weight_operands_kernel(const BlockTransposeParams x, const BlockTransposeParams dy, unsigned first) {
     __shared__ TransposeShared s;
-    if (blockIdx.x < first) transpose_quantize<KQ_T_E4M3>(x, blockIdx.x, s);
-    else transpose_quantize<TYPE>(dy, blockIdx.x - first, s);
+    if (blockIdx.x < first) transpose_quantize<KQ_T_E4M3, false>(x, blockIdx.x, s);
+    else if (dy.sums) transpose_quantize<TYPE, true>(dy, blockIdx.x - first, s);
+    else transpose_quantize<TYPE, false>(dy, blockIdx.x - first, s);
 }
 
 hipError_t launch_grad_input_operands(const BlockQuantizeParams& q, const BlockTransposeParams& t, hipStream_t s) {

@@ -34,16 +34,16 @@ struct XBlock {
                     __builtin_memcpy(&r[i], row + c * kBytes, 16);
                     continue;
                 }
+                // (loads at clamped places, all at once: a branch for each would wait for the one before)
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
-                    unsigned v = 0;
                     if constexpr (TYPE == KQ_T_F32) {
-                        if (c + t < k) v = ((const unsigned*)row)[c + t];
+                        const unsigned v = ((const unsigned*)row)[min(c + t, k - 1)];
+                        r[i][t] = c + t < k ? v : 0u;
                     } else if constexpr (TYPE != KQ_T_E4M3) {
-                        if (c + 2 * t < k) v = ((const uint16_t*)row)[c + 2 * t];
-                        if (c + 2 * t + 1 < k) v |= (unsigned)((const uint16_t*)row)[c + 2 * t + 1] << 16;
+                        const unsigned lo = ((const uint16_t*)row)[min(c + 2 * t, k - 1)], hi = ((const uint16_t*)row)[min(c + 2 * t + 1, k - 1)];
+                        r[i][t] = (c + 2 * t < k ? lo : 0u) | (c + 2 * t + 1 < k ? hi << 16 : 0u);
                     }
-                    r[i][t] = v;
                 }
             }
         }

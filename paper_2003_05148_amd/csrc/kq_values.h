@@ -67,14 +67,20 @@ __device__ __forceinline__ void store_values(void* base, int64_t at, const float
     }
 }
 
-// 8 columns at c0 of a row, zeros past the row's `limit`
+// 8 columns at c0 of a row, zeros past the row's `limit`.  (A row's last few are loaded at clamped places, all at once: with a
+// branch for each the next load waited for the one before.)
 template <int TYPE>
 __device__ __forceinline__ void load_columns(const void* base, int64_t row_at, int c0, int limit, float (&v)[8]) {
     if (c0 + 8 <= limit) {
         load_values<TYPE, 8>(base, row_at + c0, v);
+    } else if (c0 < limit) {
+#pragma unroll
+        for (int t = 0; t < 8; ++t) v[t] = load_value_as<TYPE>(base, row_at + min(c0 + t, limit - 1));
+#pragma unroll
+        for (int t = 0; t < 8; ++t) v[t] = c0 + t < limit ? v[t] : 0.0f;
     } else {
 #pragma unroll
-        for (int t = 0; t < 8; ++t) v[t] = c0 + t < limit ? load_value_as<TYPE>(base, row_at + c0 + t) : 0.0f;
+        for (int t = 0; t < 8; ++t) v[t] = 0.0f;
     }
 }
 
