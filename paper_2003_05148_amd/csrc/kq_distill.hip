@@ -576,6 +576,12 @@ __global__ __launch_bounds__(256) void distill_segment_kernel(const DistillParam
     const float x1 = single >= 0 ? r.at(single) : -__builtin_inff();
     const bool ce = p.alpha > 0.0f, two = ce && p.T != 1.0f;
     const Exponential eT = {p.eT_hi, p.eT_lo}, e1 = {p.e1_hi, p.e1_lo};
+    u32x4 w[4];  // (on their way while the first wave looks at the teacher's entries)
+    auto load_chunks = [&](int c) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) w[u] = r.load(c + 256 * u < c_end ? c + 256 * u : r.chunks);
+    };
+    if (p.dZ) load_chunks(c_begin + threadIdx.x);
     Teacher te;
     if (wave == 0) {
         te.init<TYPE>(p, r, entries, row, lane, eT);
@@ -624,11 +630,10 @@ __global__ __launch_bounds__(256) void distill_segment_kernel(const DistillParam
     d.init(p, row, s_row[0], __builtin_bit_cast(int, s_row[1]), s, eT, e1);
     char* const out = (char*)p.dZ + row * p.lddz * Row<TYPE>::kBytes;
     char* const first = out + r.head * Row<TYPE>::kBytes;
-    for (int c0 = c_begin + threadIdx.x; c0 < c_end; c0 += 4 * 256) {
-        u32x4 w[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) w[u] = r.load(c0 + 256 * u < c_end ? c0 + 256 * u : r.chunks);
-        d.chunks<TYPE>(first, c0, 256, c_end, w);
+    for (int c = c_begin + threadIdx.x; c < c_end;) {
+        d.chunks<TYPE>(first, c, 256, c_end, w);
+        c += 4 * 256;
+        if (c < c_end) load_chunks(c);
     }
     if (single >= 0) store_one<TYPE>(out, single, d.of(x1));
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the dense stores have ended
