@@ -1286,6 +1286,16 @@ class GroupLinear:
 _E4M3 = torch.float8_e4m3fn
 
 
+def _run(dev, name, *args):
+    """A library call with its tensors' device current; the stream (of that device) comes last."""
+    f = getattr(lib, name)
+    if dev.index is None or dev.index == torch.cuda.current_device():
+        _check(f(*args, _stream(dev)), name)
+    else:
+        with torch.cuda.device(dev):
+            _check(f(*args, _stream(dev)), name)
+
+
 def block_shapes(m: int, k: int, rows: int = 1):
     """Shapes of the values and exponents of an [m, k] matrix in blocks of `rows` (1 or 128) by 128."""
     if rows not in (1, KQ_BLOCK):
@@ -1331,8 +1341,7 @@ def kq_quantize_blocks(X, rows: int = 1, values=None, exps=None):
     values = torch.empty(vs, dtype=_E4M3, device=dev) if values is None else _dev(values, _E4M3, "values", vs)
     exps = torch.empty(es, dtype=torch.uint8, device=dev) if exps is None else _dev(exps, torch.uint8, "exps", es)
     _same_device(dev, values=values, exps=exps)
-    _check(lib.kq_quantize_blocks(x.data_ptr(), ty, ld, m, k, rows, values.data_ptr(), exps.data_ptr(), _stream(dev)),
-           "kq_quantize_blocks")
+    _run(dev, "kq_quantize_blocks", x.data_ptr(), ty, ld, m, k, rows, values.data_ptr(), exps.data_ptr())
     return values, exps
 
 
@@ -1351,8 +1360,7 @@ def kq_reconstruct_blocks(values, exps, in_features: int, rows: int = 1, dtype=t
     if out.shape[0] != m:
         raise ValueError(f"X_hat must have {m} rows")
     _same_device(dev, X_hat=X_hat)
-    _check(lib.kq_reconstruct_blocks(values.data_ptr(), exps.data_ptr(), m, k, rows, ty, out.data_ptr(), ld, _stream(dev)),
-           "kq_reconstruct_blocks")
+    _run(dev, "kq_reconstruct_blocks", values.data_ptr(), exps.data_ptr(), m, k, rows, ty, out.data_ptr(), ld)
     return X_hat
 
 
@@ -1396,8 +1404,8 @@ def kq_block_linear(X, values, exps, bias=None, x_exps=None, dtype=None, Y=None,
         raise TypeError(f"Y must be {dtype}, got {Y.dtype}")
     Y, y, yt, ldy = _typed_rows(Y, dtype, dev, lead, n, "Y")
     wp, wn = _scratch_for(dev, lib.kq_block_linear_workspace_bytes(xt, yt, m, n, k), workspace)
-    _check(lib.kq_block_linear(x.data_ptr(), xt, ldx, _ptr(x_exps), m, n, k, values.data_ptr(), exps.data_ptr(), _ptr(bias),
-                               y.data_ptr(), yt, ldy, wp, wn, _stream(dev)), "kq_block_linear")
+    _run(dev, "kq_block_linear", x.data_ptr(), xt, ldx, _ptr(x_exps), m, n, k, values.data_ptr(), exps.data_ptr(),
+         _ptr(bias), y.data_ptr(), yt, ldy, wp, wn)
     return Y
 
 
@@ -1417,8 +1425,8 @@ def kq_block_linear_grad_input(dY, values, exps, in_features: int, dX=None, work
     _same_device(dev, values=values)
     dX, dx, ldx = _out_rows(dX, dY, dY.shape[:-1], k, _TYPES, "dX")
     wp, wn = _scratch_for(dev, lib.kq_block_linear_grad_input_workspace_bytes(ty, m, n, k), workspace)
-    _check(lib.kq_block_linear_grad_input(dy.data_ptr(), ty, ldy, m, n, k, values.data_ptr(), exps.data_ptr(), dx.data_ptr(),
-                                          ldx, wp, wn, _stream(dev)), "kq_block_linear_grad_input")
+    _run(dev, "kq_block_linear_grad_input", dy.data_ptr(), ty, ldy, m, n, k, values.data_ptr(), exps.data_ptr(),
+         dx.data_ptr(), ldx, wp, wn)
     return dX
 
 
@@ -1442,9 +1450,8 @@ def kq_block_linear_grad_weight(dY, x_values, x_exps, in_features: int, bias: bo
     dW, dw, wt, ldw = _typed_rows(dW, dtype, dev, (n,), k, "dW")
     dbias = _bias_out(dev, n, bias, dbias)
     wp, wn = _scratch_for(dev, lib.kq_block_linear_grad_weight_workspace_bytes(wt, m, n, k), workspace)
-    _check(lib.kq_block_linear_grad_weight(dy.data_ptr(), ty, ldy, m, n, k, x_values.data_ptr(), x_exps.data_ptr(),
-                                           dw.data_ptr(), wt, ldw, _ptr(dbias), wp, wn, _stream(dev)),
-           "kq_block_linear_grad_weight")
+    _run(dev, "kq_block_linear_grad_weight", dy.data_ptr(), ty, ldy, m, n, k, x_values.data_ptr(), x_exps.data_ptr(),
+         dw.data_ptr(), wt, ldw, _ptr(dbias), wp, wn)
     return dW, dbias
 
 
@@ -1549,8 +1556,7 @@ def kq_distill(Z, top_values, top_idx, temperature: float = 1.0, labels=None, al
     loss = _row_floats(loss, dev, m, "loss")
     dZ, dz, lddz = _out_rows(dZ, Z, Z.shape[:-1], z.shape[1], _TYPES, "dZ")
     wp, wn = _scratch_for(dev, lib.kq_distill_workspace_bytes(a.type, m, z.shape[1], a.top), workspace)
-    _check(lib.kq_distill(ctypes.byref(a), _ptr(dloss), scale, loss.data_ptr(), dz.data_ptr(), lddz, wp, wn, _stream(dev)),
-           "kq_distill")
+    _run(dev, "kq_distill", ctypes.byref(a), _ptr(dloss), scale, loss.data_ptr(), dz.data_ptr(), lddz, wp, wn)
     return loss, dZ
 
 
@@ -1569,7 +1575,7 @@ def kq_distill_loss(Z, top_values, top_idx, temperature: float = 1.0, labels=Non
     _dev(stats, torch.float32, "stats", (m, 3))
     _same_device(dev, stats=stats)
     wp, wn = _scratch_for(dev, lib.kq_distill_workspace_bytes(a.type, m, z.shape[1], a.top), workspace)
-    _check(lib.kq_distill_loss(ctypes.byref(a), loss.data_ptr(), stats.data_ptr(), wp, wn, _stream(dev)), "kq_distill_loss")
+    _run(dev, "kq_distill_loss", ctypes.byref(a), loss.data_ptr(), stats.data_ptr(), wp, wn)
     return loss, stats
 
 
@@ -1588,6 +1594,5 @@ def kq_distill_grad(Z, top_values, top_idx, stats, dloss=None, temperature: floa
     if dloss is not None:
         _row_floats(dloss, dev, m, "dloss")
     dZ, dz, lddz = _out_rows(dZ, Z, Z.shape[:-1], z.shape[1], _TYPES, "dZ")
-    _check(lib.kq_distill_grad(ctypes.byref(a), stats.data_ptr(), _ptr(dloss), scale, dz.data_ptr(), lddz, _stream(dev)),
-           "kq_distill_grad")
+    _run(dev, "kq_distill_grad", ctypes.byref(a), stats.data_ptr(), _ptr(dloss), scale, dz.data_ptr(), lddz)
     return dZ

@@ -16,6 +16,7 @@
 // them the library's functions, the current stream's handle by device index, and the scratch buffers.
 #define PY_SSIZE_T_CLEAN
 #include <ATen/ops/empty.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/Device.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -248,6 +249,11 @@ struct Call {
             ok = false;
         }
         return s;
+    }
+    // the same for a device that is the current one (the general path makes it current)
+    void* current_stream() {
+        if (ok && c10::impl::VirtualGuardImpl(dev.type()).getDevice() != dev) ok = false;
+        return ok ? stream() : nullptr;
     }
     // scratch of the current stream, as the general path takes it
     at::Tensor scratch(size_t bytes) {
@@ -559,7 +565,7 @@ PyObject* quantize_blocks(PyObject*, PyObject* const* a, Py_ssize_t count) {
         const at::Tensor X = c.rows(a[0], ld);
         const int64_t rows = c.integer(a[1]);
         if (!c.ok || (rows != 1 && rows != kBlock)) return nullptr;
-        void* const s = c.stream();
+        void* const s = c.current_stream();
         if (!c.ok) return nullptr;
         const int64_t m = X.size(0), k = X.size(1), kb = (k + kBlock - 1) / kBlock;
         const at::Tensor v = c.make({m, kb * kBlock}, at::kFloat8_e4m3fn), e = c.make({(m + rows - 1) / rows, kb}, at::kByte);
@@ -577,7 +583,7 @@ PyObject* reconstruct_blocks(PyObject*, PyObject* const* a, Py_ssize_t count) {
         if (!c.ok || (rows != 1 && rows != kBlock) || type < 0) return nullptr;
         const Blocks w(c, a[0], a[1], k, rows);
         if (!c.ok) return nullptr;
-        void* const s = c.stream();
+        void* const s = c.current_stream();
         if (!c.ok) return nullptr;
         const at::Tensor X = c.make({w.m, k}, scalar_of(type));
         if (g_lib.reconstruct_blocks(w.values, w.exps, w.m, k, (int32_t)rows, (int32_t)type, X.data_ptr(), k, s) != KQ_OK) return nullptr;
@@ -617,7 +623,7 @@ PyObject* block_linear(PyObject*, PyObject* const* a, Py_ssize_t count) {
         }
         if (type < 0) type = xt == KQ_T_E4M3 ? KQ_T_BF16 : xt;
         if (!c.ok) return nullptr;
-        void* const s = c.stream();
+        void* const s = c.current_stream();
         const at::Tensor ws = c.scratch(g_lib.block_linear_ws(xt, (int32_t)type, m, w.m, k));
         if (!c.ok) return nullptr;
         if (!Y.defined()) Y = c.make({m, w.m}, scalar_of(type));
@@ -644,7 +650,7 @@ PyObject* block_grad_input(PyObject*, PyObject* const* a, Py_ssize_t count) {
             dX = c.rows(a[4], ldx);
             if (!c.ok || dX.scalar_type() != dY.scalar_type() || dX.size(0) != m || dX.size(1) != k) return nullptr;
         }
-        void* const s = c.stream();
+        void* const s = c.current_stream();
         const at::Tensor ws = c.scratch(g_lib.block_grad_input_ws(type, m, n, k));
         if (!c.ok) return nullptr;
         if (!dX.defined()) {
@@ -668,7 +674,7 @@ PyObject* block_grad_weight(PyObject*, PyObject* const* a, Py_ssize_t count) {
         const Blocks x(c, a[1], a[2], k, 1);
         const int64_t m = dY.size(0), n = dY.size(1);
         if (!c.ok || x.m != m) return nullptr;
-        void* const s = c.stream();
+        void* const s = c.current_stream();
         const at::Tensor ws = c.scratch(g_lib.block_grad_weight_ws((int32_t)type, m, n, k));
         if (!c.ok) return nullptr;
         const at::Tensor dW = c.make({n, k}, scalar_of(type));
@@ -757,7 +763,7 @@ PyObject* distill(PyObject*, PyObject* const* a, Py_ssize_t count) {
         if (!c.ok) return nullptr;
         const float* const dloss = row_floats(c, a[7], d.args.m);
         int64_t ld = 0;
-        void* const s = c.stream();
+        void* const s = c.current_stream();
         const at::Tensor ws = c.scratch(g_lib.distill_ws(d.args.type, d.args.m, d.args.v, d.args.top));
         const at::Tensor dZ = gradient(c, a[8], d.Z, ld);
         if (!c.ok) return nullptr;
@@ -777,7 +783,7 @@ PyObject* distill_loss(PyObject*, PyObject* const* a, Py_ssize_t count) {
         Call c;
         const Distill d(c, a);
         if (!c.ok) return nullptr;
-        void* const s = c.stream();
+        void* const s = c.current_stream();
         const at::Tensor ws = c.scratch(g_lib.distill_ws(d.args.type, d.args.m, d.args.v, d.args.top));
         if (!c.ok) return nullptr;
         const at::Tensor loss = c.make({d.args.m}, at::kFloat), stats = c.make({d.args.m, 3}, at::kFloat);
@@ -796,7 +802,7 @@ PyObject* distill_grad(PyObject*, PyObject* const* a, Py_ssize_t count) {
         const at::Tensor stats = c.dense(a[7], at::kFloat, {d.args.m, 3});
         const float* const dloss = row_floats(c, a[8], d.args.m);
         int64_t ld = 0;
-        void* const s = c.stream();
+        void* const s = c.current_stream();
         const at::Tensor dZ = gradient(c, a[9], d.Z, ld);
         if (!c.ok) return nullptr;
         if (g_lib.distill_grad(&d.args, (const float*)stats.data_ptr(), dloss, scale, dZ.data_ptr(), ld, s) != KQ_OK) return nullptr;

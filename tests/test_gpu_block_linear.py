@@ -19,6 +19,8 @@ import torch
 
 pytestmark = pytest.mark.gpu
 
+from test_block_plan import SIZES
+
 kq = pytest.importorskip("paper_2003_05148_amd")
 DEV = torch.device("cuda:0")
 BF, HF, F32, E4 = torch.bfloat16, torch.float16, torch.float32, torch.float8_e4m3fn
@@ -356,6 +358,43 @@ def test_gradients_strides_and_outputs():
         assert torch.all(out[:, :11] == 3) and torch.all(out[:, 11 + k:] == 3) and torch.all(out[n] == 3)
 
 
+def again(x):
+    """x (GPU) as it is after quantization in blocks of one row, in 64 bits (the quantizer itself is tested above)."""
+    return kq.kq_reconstruct_blocks(*kq.kq_quantize_blocks(x.contiguous()), x.shape[1]).double()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("i,j,c", SIZES)
+def test_every_tile(i, j, c, dtype):
+    """Sizes of every tile and kind of plan, odd at every edge: the product and both gradients against 64 bits on the GPU."""
+    g = torch.Generator(device=DEV).manual_seed(i + j + c)
+
+    def randn(a, b, spread=0.5):
+        return torch.randn(a, b, device=DEV, generator=g) * torch.exp(spread * torch.randn(a, 1, device=DEV, generator=g))
+
+    def check_gpu(y, a, b):
+        y64, S = a @ b.t(), a.abs() @ b.abs().t()
+        u, exact = U[y.dtype], y.dtype == F32
+        tol = u * y64.abs() + (c + 16) * 2.0 ** -24 * S + TINY[y.dtype] + (0 if exact else 7 * 2.0 ** -13) * S
+        err = (y.double() - y64).abs()
+        assert torch.all(err <= tol), float((err - tol).max())
+        rel = float(err.norm() / y64.norm())
+        assert rel <= u + 2.0 ** -18 + (0 if exact else 2.0 ** -14), rel
+
+    W, X = randn(i, c) / math.sqrt(c), randn(j, c).to(dtype)
+    values, exps = kq.kq_quantize_blocks(W, rows=128)
+    check_gpu(kq.kq_block_linear(X, values, exps), again(X), kq.kq_reconstruct_blocks(values, exps, c, rows=128).double())
+    W, dY = randn(c, i) / math.sqrt(c), (0.01 * randn(j, c)).to(dtype)
+    values, exps = kq.kq_quantize_blocks(W, rows=128)
+    check_gpu(kq.kq_block_linear_grad_input(dY, values, exps, i), again(dY),
+              kq.kq_reconstruct_blocks(values, exps, i, rows=128).double().t())
+    x, dY = kq.kq_quantize_blocks(randn(c, i).to(BF)), (0.01 * randn(c, j)).to(BF)
+    dW, db = kq.kq_block_linear_grad_weight(dY, *x, i, bias=True, dtype=dtype)
+    check_gpu(dW, again(dY.t()), again(kq.kq_reconstruct_blocks(*x, i).t()))
+    d = dY.double()
+    assert torch.all((db.double() - d.sum(0)).abs() <= (c + 1) * 2.0 ** -24 * d.abs().sum(0))
+
+
 # ---- how the calls run ---------------------------------------------------------------------------------
 
 def test_same_bits_every_time_and_on_another_stream():
@@ -408,6 +447,23 @@ def test_captured_and_replayed():
             torch.cuda.synchronize()
             for a, b in zip(out, want):
                 assert torch.equal(a, b)
+
+
+def test_without_the_host_helper(monkeypatch):
+    """The binding's own checks and calls give what the C++ helper's plain case gives."""
+    (values, exps), _ = layer(300, 600, 1)
+    X, dY = acts(40, 600, BF, 1).to(DEV), (0.01 * acts(40, 300, BF, 2)).to(DEV)
+    bias = torch.randn(300, device=DEV)
+
+    def calls():
+        x = kq.kq_quantize_blocks(X)
+        return [x[0].view(torch.uint8), x[1], kq.kq_reconstruct_blocks(*x, 600, dtype=HF), kq.kq_block_linear(X, values, exps, bias=bias),
+                kq.kq_block_linear(X[:3], values, exps, dtype=F32), kq.kq_block_linear(x[0], values, exps, x_exps=x[1], dtype=HF),
+                kq.kq_block_linear_grad_input(dY, values, exps, 600), *kq.kq_block_linear_grad_weight(dY, *x, 600, bias=True, dtype=BF)]
+    want = calls()
+    monkeypatch.setattr(kq, "_fast", None)
+    for a, b in zip(want, calls()):
+        assert a.dtype == b.dtype and torch.equal(a, b)
 
 
 def test_given_workspace():

@@ -276,6 +276,21 @@ def test_streams_and_graphs(m, v):
             assert torch.equal(a, b)
 
 
+def test_without_the_host_helper(monkeypatch):
+    """The binding's own checks and calls give what the C++ helper's plain case gives."""
+    z, tv, ti, y = on(*logits(9, 700, 6, BF, 1))
+    d = torch.rand(9, device=DEV)
+
+    def calls():
+        l2, stats = kq.kq_distill_loss(z, tv, ti, 2.0, y, 0.3)
+        return [*kq.kq_distill(z, tv, ti, temperature=2.0, labels=y, alpha=0.3, dloss=d), *kq.kq_distill(z, tv, ti, scale=0.5), l2, stats,
+                kq.kq_distill_grad(z, tv, ti, stats, d, 2.0, y, 0.3)]
+    want = calls()
+    monkeypatch.setattr(kq, "_fast", None)
+    for a, b in zip(want, calls()):
+        assert a.dtype == b.dtype and torch.equal(a, b)
+
+
 def test_offsets_past_32_bits():
     """Rows more than 2^32 bytes apart, and a large number of classes."""
     v = 200000
