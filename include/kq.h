@@ -695,7 +695,7 @@ kq_status kq_checkpoint_grad_weight(const void* dY, int32_t type, int64_t ldy, i
  *   Types are KQ_T_*; KQ_T_E4M3 stands for such a pair where an input may be one.  Matrices are row-major with a row
  *   pitch in elements, aligned to their type; a KQ_T_E4M3 matrix has the pitch kp.  Sizes are limited as for the
  *   4-bit layers; m = 0 writes nothing (gradients of parameters are zero then).
- *   Products whose magnitude is below 2^-126 may be taken as zero.
+ *   In products, values and products whose magnitude is below 2^-126 may be taken as zero.
  *
  * kq_quantize_blocks, kq_reconstruct_blocks -- X [m][k] of any KQ_T_* type but KQ_T_E4M3; rows 1 or 128 (else
  *   KQ_ERR_UNSUPPORTED).
@@ -743,10 +743,11 @@ kq_status kq_block_linear_grad_weight(const void* dY, int32_t type, int64_t ldy,
  *   teacher logits / T, q the softmax of z / T and s the softmax of z,
  *     loss = (1 - alpha) T^2 sum_j p_j (log p_j - log q_idx[j])  +  alpha (-log s_label),
  *     dz_c = d [ (1 - alpha) T (q_c - sum of p_j with idx[j] = c)  +  alpha (s_c - [c = label]) ];
- *   a row without a present entry (or label) has no first (second) term in either.  d is dloss[row], or `scale` for
- *   all rows where dloss is NULL.  A term with a weight of zero (alpha 0 or 1) is not computed.
- *   A NaN or +infinity in a row makes its loss and gradient NaN; -infinity in Z is a class that is masked out (gradient
- *   0, or the teacher's share: its loss is infinite then).
+ *   a row without a present entry (or label) has no first (second) term in either; one without both has loss and
+ *   gradient 0, whatever it holds.  d is dloss[row], or `scale` for all rows where dloss is NULL.  A term with a weight
+ *   of zero (alpha 0 or 1) is not computed.
+ *   A NaN or +infinity in any other row makes its loss and gradient NaN; -infinity in Z is a class that is masked out
+ *   (gradient 0, or the teacher's share: its loss is infinite then).
  *   1 <= v <= KQ_DISTILL_MAX_CLASSES, 1 <= top <= KQ_DISTILL_MAX_TOP, 0 <= m <= KQ_GROUP_MAX_ROWS,
  *   m v <= KQ_DISTILL_MAX_LOGITS, 2^-10 <= temperature <= 2^20 (else KQ_ERR_UNSUPPORTED), 0 <= alpha <= 1; alpha > 0 needs labels.
  *
@@ -759,7 +760,7 @@ kq_status kq_block_linear_grad_weight(const void* dY, int32_t type, int64_t ldy,
  */
 #define KQ_DISTILL_MAX_CLASSES (1 << 24)
 #define KQ_DISTILL_MAX_TOP 256
-#define KQ_DISTILL_MAX_LOGITS ((int64_t)1 << 38)
+#define KQ_DISTILL_MAX_LOGITS ((int64_t)1 << 35)
 typedef struct kq_distill_args {
     const void* Z;
     int32_t type;

@@ -288,17 +288,19 @@ struct Factors {
 struct Dense {
     Factors f;
     float M;
-    bool one;
+    bool one, none;   // none: a row without either term, whatever its logits are
     Exponential eT, e1;
     __device__ __forceinline__ void init(const DistillParams& p, int64_t row, float St, int label, const Sums& s, const Exponential& aT, const Exponential& a1) {
         f.init(p, row, St, label, s);
         M = s.M;
         one = p.T == 1.0f || f.f1 == 0.0f;
+        none = f.fT == 0.0f && f.f1 == 0.0f;
         eT = aT;
         e1 = a1;
     }
     __device__ __forceinline__ float of(float z) const {
         const float d = z - M;
+        if (none) return 0.0f;
         return one ? (f.fT + f.f1) * eT(d) : f.fT * eT(d) + f.f1 * e1(d);
     }
     template <int TYPE, bool ONE>
@@ -334,7 +336,12 @@ struct Dense {
     }
     template <int TYPE, int CH>
     __device__ __forceinline__ void chunks(char* first, int c, int step, int end, u32x4 (&w)[CH]) const {
-        if (one) store<TYPE, true>(first, c, step, end, w);
+        if (none) {
+            const u32x4 g = {0, 0, 0, 0};
+#pragma unroll
+            for (int t = 0; t < CH; ++t)
+                if (c + t * step < end) __builtin_memcpy(first + (unsigned)(c + t * step) * 16u, &g, 16);
+        } else if (one) store<TYPE, true>(first, c, step, end, w);
         else store<TYPE, false>(first, c, step, end, w);
     }
 };
@@ -444,6 +451,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, WAVES == 16 ? 8 : 1)
     const float x1 = single >= 0 ? r.at(single) : -__builtin_inff();
     Teacher te;
     if (leader) te.init<TYPE>(p, r, entries, row, lane, eT);
+    if (WAVES > 1 && wave == 0) __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): what was read of Z is here before it may be written
     if (WAVES > 1 && threadIdx.x == 0) {
         s_row[0] = te.St;
         s_row[1] = __builtin_bit_cast(float, te.label);

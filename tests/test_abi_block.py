@@ -106,7 +106,7 @@ def test_distill():
                    dict(top_values=FAKE + 2), dict(top_idx=None), dict(top_idx=FAKE + 4), dict(labels=None), dict(labels=FAKE + 4),
                    dict(alpha=-0.1), dict(alpha=1.1), dict(alpha=math.nan)):
             assert f(ctypes.byref(args(**kw))) == ARG, kw
-        for kw in (dict(m=MAXM + 1), dict(v=MAXF + 1), dict(top=257), dict(type=3), dict(top_type=3), dict(idx_bytes=2),
+        for kw in (dict(m=MAXM + 1), dict(v=MAXF + 1), dict(m=1 << 20, v=(1 << 15) + 1, ldz=1 << 16), dict(top=257), dict(type=3), dict(top_type=3), dict(idx_bytes=2),
                    dict(label_bytes=2), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=math.nan),
                    dict(temperature=math.inf), dict(temperature=2.0 ** -11), dict(temperature=2.0 ** 21)):
             assert f(ctypes.byref(args(**kw))) == UNS, kw

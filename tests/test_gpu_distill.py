@@ -170,6 +170,22 @@ def test_rows_with_nothing(v):
 
 
 @pytest.mark.parametrize("v", [10, 1500, 9000, 70001])
+def test_rows_without_a_term_are_zero_whatever_they_hold(v):
+    m = 5
+    for dtype in (F32, BF):
+        Z, values, idx, labels = logits(m, v, 4, dtype, v, absent=0.0)
+        idx[:4], labels[:4] = -1, -1
+        Z[0], Z[1, v - 1], Z[2, 0] = -math.inf, math.nan, math.inf
+        z, tv, ti, y = on(Z, values, idx, labels)
+        for T, alpha in ((2.0, 0.5), (1.0, 0.25), (1.0, 0.0)):
+            loss, dz = kq.kq_distill(z, tv, ti, temperature=T, labels=y, alpha=alpha)
+            l2, stats = kq.kq_distill_loss(z, tv, ti, T, y, alpha)
+            for a, g in ((loss, dz), (l2, kq.kq_distill_grad(z, tv, ti, stats, None, T, y, alpha))):
+                assert torch.all(a[:4] == 0) and torch.all(g[:4] == 0)
+                check(a[4:], g[4:], Z[4:], values[4:], idx[4:], labels[4:], T, alpha, torch.ones(1).double())
+
+
+@pytest.mark.parametrize("v", [10, 1500, 9000, 70001])
 def test_masked_classes_and_bad_rows(v):
     m = 6
     Z, values, idx, labels = logits(m, v, 5, F32, v, absent=0.0)
