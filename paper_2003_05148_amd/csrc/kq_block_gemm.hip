@@ -323,6 +323,7 @@ __global__ __launch_bounds__(64 * WI * WJ, 1) void block_gemm_kernel(const Block
         if (p.dbias && i0 == 0 && blockIdx.y == 0) {
             for (int64_t j = j0 + tid; j < min(j0 + BJ, p.J); j += 64 * WAVES) {
                 float v = 0.0f;
+#pragma unroll 16
                 for (int t = 0; t < p.bias_parts; ++t) v += p.bias_part[(int64_t)t * p.J + j];
                 p.dbias[j] = v;
             }

@@ -250,6 +250,32 @@ def test_linear_extreme_scales():
             check(Y, hat((X * b).to(dtype), 1), hat(W * a, 128), 256, dtype == F32 or m <= 16)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_values_below_the_smallest_normal_number(dtype):
+    """Blocks whose values are around and below 2^-126 meet large ones.  Values below it may count as zero: no more than
+    their terms are missing."""
+    n, k = 130, 256
+
+    def near(y, a, b, terms, exact):
+        small = lambda x: torch.where(x.abs() < 2.0 ** -126, x.abs(), 0.0)
+        lost = small(a) @ b.abs().t() + a.abs() @ small(b).t()
+        S, y64, y = a.abs() @ b.abs().t(), a @ b.t(), y.double().cpu()
+        tol = U[dtype] * (y64.abs() + lost) + ((terms + 16) * 2.0 ** -24 + (0 if exact else 7 * 2.0 ** -13)) * S + TINY[dtype]
+        assert torch.all((y - y64).abs() <= tol + lost)
+
+    for m in (5, 40):
+        for a, b in ((2.0 ** 100, 2.0 ** -130), (2.0 ** -132, 2.0 ** 110)):
+            W, X = torch.randn(n, k, generator=gen(1)) * a, (torch.randn(m, k, generator=gen(2)) * b).to(dtype)
+            q = kq.kq_quantize_blocks(W.to(DEV), rows=128)
+            Wh, Xh = hat(W, 128), hat(X, 1)
+            for x, xe in ((X.to(DEV), None), kq.kq_quantize_blocks(X.to(DEV))):
+                near(kq.kq_block_linear(x, *q, x_exps=xe, dtype=dtype), Xh, Wh, k, dtype == F32 or m <= 16)
+            dY = (torch.randn(m, n, generator=gen(3)) * (2.0 ** -30 / b)).to(dtype)   # (1 / b alone is past fp32)
+            x = kq.kq_quantize_blocks(X.to(DEV))
+            dW, _ = kq.kq_block_linear_grad_weight(dY.to(DEV), *x, k, dtype=dtype)
+            near(dW, hat(dY.double().t().contiguous(), 1), hat(Xh.t().contiguous(), 1), m, dtype == F32)
+
+
 def test_linear_strides_leading_sizes_and_outputs():
     (values, exps), W = layer(100, 300, 4)
     big = acts(60, 700, BF, 3).to(DEV)
@@ -279,6 +305,18 @@ def test_grad_input(m, n, k, dtype):
     dX = kq.kq_block_linear_grad_input(dY.to(DEV), values, exps, k)
     assert dX.dtype == dtype
     check(dX, hat(dY, 1), W.t(), n, dtype == F32)
+
+
+@pytest.mark.parametrize("m", [64 * 128, 64 * 128 + 1, 70 * 128, 95 * 128 + 5, 128 * 128])
+def test_bias_gradient_of_many_rows(m):
+    """Sums over 128 rows are added in groups above 64 of them, and the rest of them alone: within the tolerance of m terms."""
+    n, k = 5, 130
+    dY, x = acts(m, n, BF, m), kq.kq_quantize_blocks(acts(m, k, BF, 1).to(DEV))
+    _, db = kq.kq_block_linear_grad_weight(dY.to(DEV), *x, k, True)
+    d = dY.double()
+    assert torch.all((db.double().cpu() - d.sum(0)).abs() <= (m + 16) * 2.0 ** -24 * d.abs().sum(0))
+    ones = torch.ones(m, n, dtype=BF, device=DEV)
+    assert torch.all(kq.kq_block_linear_grad_weight(ones, *x, k, True)[1] == m)     # (each sum of integers is exact)
 
 
 @pytest.mark.parametrize("out", [F32, BF, HF])
