@@ -707,8 +707,8 @@ kq_status kq_checkpoint_grad_weight(const void* dY, int32_t type, int64_t ldy, i
  * kq_block_linear_grad_weight -- dW[o][c] = sum_m dY^[m][o] X^[m][c] from X's values (rows = 1): both are quantized along m, in
  *   blocks of 128 rows by 1 column (X's values again: a power of two changes them only where they become
  *   subnormal).  dw_type is any but KQ_T_E4M3.  dbias (fp32 [n], or NULL): sum_m dY[m][o], not quantized.
- *   Sums.  Where the output is fp32, and in kq_block_linear of up to 16 rows, products are exact and sums are fp32.
- *   Otherwise the 8-bit matrix instruction adds them: eight products at a time, each cut off 13 bits below the
+ *   Sums.  Where the output is fp32, and in kq_block_linear of up to 16 rows and of small products, products are exact and
+ *   sums are fp32.  Otherwise the 8-bit matrix instruction adds them: eight products at a time, each cut off 13 bits below the
  *   largest of the eight (on random operands 1.5e-5 of the result's norm, where rounding to bf16 is 1.7e-3 and to
  *   fp16 2.1e-4), and the eights in fp32.  The order of a sum goes by the sizes alone.
  *   workspaces: the *_workspace_bytes of the same arguments (may be 0: ws may be NULL then).

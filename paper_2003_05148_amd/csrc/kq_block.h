@@ -110,14 +110,15 @@ struct BlockGemmPlan {
     size_t part_bytes;
     int64_t rest_from;       // columns i from here on have a tile of their own, or 0
     int rest_bi, rest_bj;
+    float us;                // as modelled
 };
 // exact: products on the 16-bit matrix instructions
 BlockGemmPlan block_gemm_plan(bool exact, int64_t I, int64_t J, int64_t C);
 // a_rows: A's blocks are 1 x 128 (else 128 x 128)
 hipError_t launch_block_gemm(bool exact, bool a_rows, const BlockGemmPlan& plan, BlockGemmParams p, void* part, hipStream_t s);
 
-// Y = X W^T for at most kBlockMatvecRows rows of X.
-constexpr int kBlockMatvecRows = 16;
+// Y = X W^T for few rows of X: up to kBlockMatvecRows always, up to kBlockMatvecMost where the plan is the faster one.
+constexpr int kBlockMatvecRows = 16, kBlockMatvecMost = 1024;
 struct BlockMatvecParams {
     const uint8_t* values;   // W
     const uint8_t* exps;
@@ -137,8 +138,10 @@ struct BlockMatvecParams {
 struct BlockMatvecPlan {
     int row_tiles, waves, splits, blocks_per_split;
     size_t ws_bytes;
+    float us;                // as modelled, above kBlockMatvecRows rows
 };
-BlockMatvecPlan block_matvec_plan(int m, int64_t n, int64_t k);
+BlockMatvecPlan block_matvec_plan(int m, int64_t n, int64_t k);              // up to kBlockMatvecRows rows
+BlockMatvecPlan block_matvec_plan(int x_type, int m, int64_t n, int64_t k);  // more of them
 hipError_t launch_block_matvec(const BlockMatvecPlan& plan, BlockMatvecParams p, hipStream_t s);
 
 }  // namespace kq

@@ -2,10 +2,10 @@
 // rows of e4m3 bytes with one power of two for 128 of them.
 //
 // A workgroup holds a BI x BJ tile of the output in registers and walks the contraction block by block (128 deep).
-// The operands' bytes go from memory to LDS directly, rows of 128 bytes in eight 16-byte chunks, chunk ch of row r
-// at ch ^ (r & 7).  i is the contiguous dimension of the output, so that four accumulators of a lane are neighbours
-// in memory.  The contraction is in any order that both operands share: lane l of the 32 x 32 x 64 instruction takes
-// chunks 2 h' and 2 h' + 1 of its row's half, h' = l / 32.
+// The operands' bytes go from memory to LDS directly, rows of 128 bytes in eight 16-byte chunks, chunk ch of row r at an
+// exclusive or of ch and three bits of r (block_swizzle).  i is the contiguous dimension of the output, so that four
+// accumulators of a lane are neighbours in memory.  The contraction is in any order that both operands share: lane l
+// of the 32 x 32 x 64 instruction takes chunks 2 h' and 2 h' + 1 of its row's half, h' = l / 32.
 //
 // Two forms.  The scaled 8-bit instruction takes the bytes and both exponents as they are, at twice the 16-bit rate;
 // it adds eight products at a time and cuts each off 13 bits below the largest of them.  That is 1.5e-5 of the
@@ -87,9 +87,10 @@ struct RowExponents {
             now[t] = u32x2{(unsigned)v, (unsigned)(v >> 32)};
         }
     }
-    __device__ __forceinline__ void shift() {  // two blocks on
+    template <int BLOCKS>
+    __device__ __forceinline__ void shift() {
 #pragma unroll
-        for (int t = 0; t < N; ++t) now[t] = u32x2{__builtin_amdgcn_alignbit(now[t].y, now[t].x, 16), now[t].y >> 16};
+        for (int t = 0; t < N; ++t) now[t] = BLOCKS == 4 ? u32x2{now[t].y, 0u} : u32x2{__builtin_amdgcn_alignbit(now[t].y, now[t].x, 16), now[t].y >> 16};
     }
 };
 
@@ -143,13 +144,15 @@ __device__ __forceinline__ void store_rows(const float* rows, char* out, int64_t
     }
 }
 
-template <bool EXACT, bool AROWS, int BI, int BJ, int WI, int WJ>
+template <bool EXACT, bool AROWS, int BI, int BJ, int WI, int WJ, int RING>
 __global__ __launch_bounds__(64 * WI * WJ, 1) void block_gemm_kernel(const BlockGemmParams p) {
     constexpr int MI = BI / WI / 32, MJ = BJ / WJ / 32, WAVES = WI * WJ;
     static_assert(MI * 32 <= kBlock, "a wave's rows of A lie in one block");
     // (arrays of their own, so that the compiler can tell the direct loads' target from what is read beside them)
     __shared__ u32x4 s_0[(BI + BJ) * 8];
     __shared__ u32x4 s_1[(BI + BJ) * 8];
+    __shared__ u32x4 s_2[RING > 2 ? (BI + BJ) * 8 : 1];
+    __shared__ u32x4 s_3[RING > 2 ? (BI + BJ) * 8 : 1];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave % WI, wj = wave / WI, r32 = lane & 31, half = lane >> 5;
     const int tile = xcd_tile(blockIdx.x, p.itiles * p.jtiles);
@@ -250,7 +253,9 @@ __global__ __launch_bounds__(64 * WI * WJ, 1) void block_gemm_kernel(const Block
     };
     // Half a block is multiplied from registers while the next half's fragments are read from LDS.  Between a block's halves
     // every wave has read the second one's fragments, and the next block has to be there: one barrier a block.  After it the
-    // block's place takes the one after the next, which has until then.
+    // block's place takes the one RING blocks on, which has until then.  Four places instead of two where a CU has one workgroup
+    // all the same and the loads come from memory (4096 x 128 x 25088, 64 workgroups: 79 us, 112 with two; 4096 x 512 x 4096,
+    // 256 workgroups: 18.0 and 23.1; of 64 workgroups with the operands in the L2s 13.7 and 14.5).
     constexpr int PER = DirectRows<BI, WAVES>::N + DirectRows<BJ, WAVES>::N;
     // A matrix instruction, then its share of the reads and loads: they issue while it runs.  The reads go with the first half
     // of the instructions, so that LDS has answered at the end; the loads with all of them, since they hold up the wave
@@ -274,12 +279,12 @@ __global__ __launch_bounds__(64 * WI * WJ, 1) void block_gemm_kernel(const Block
         multiply(f0, xa, byte);
         in_turn(std::false_type{});
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(waitcnt(0, 0));
+        __builtin_amdgcn_s_waitcnt(waitcnt((RING - 2) * PER, 0));
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        load_block(b + 2, now);
+        load_block(b + RING, now);
         read_fragments(next, 0, f0);
         multiply(f1, xa, byte);
         in_turn(std::true_type{});
@@ -291,30 +296,43 @@ __global__ __launch_bounds__(64 * WI * WJ, 1) void block_gemm_kernel(const Block
         if constexpr (!AROWS) block_exp = load_block_exps(b_begin);
         load_block(b_begin, s_0);
         load_block(b_begin + 1, s_1);
-        __builtin_amdgcn_s_waitcnt(waitcnt(PER, 15));
+        if constexpr (RING > 2) {
+            load_block(b_begin + 2, s_2);
+            load_block(b_begin + 3, s_3);
+        }
+        __builtin_amdgcn_s_waitcnt(waitcnt((RING - 1) * PER, 15));
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         read_fragments(s_0, 0, f0);
-        // Two blocks a turn.  Behind an odd last one comes the same block again, with exponents of zero on both sides: its
+        // RING blocks a turn.  Behind an odd last one comes the same block again, with exponents of zero on both sides: its
         // products are below 2^-220, nothing in fp32.  (A branch there made the compiler move the accumulators about.)
-        constexpr std::integral_constant<int, 0> first = {};
-        constexpr std::integral_constant<int, 1> second = {};
-        for (int b = b_begin, t = 0; b < b_end; b += 2, ++t) {
-            if ((t & 3) == 0) {
+        constexpr int kTurns = 8 / RING;
+        auto block_byte = [&](int t, int i) { return AROWS ? 0u : (unsigned)__builtin_amdgcn_readlane(block_exp, (RING * t + i) & 63); };
+        for (int b = b_begin, t = 0; b < b_end; b += RING, ++t) {
+            if (t % kTurns == 0) {
                 if constexpr (AROWS) ea.take(b);
                 eb.take(b);
-                if (!AROWS && (t & 31) == 0 && t > 0) block_exp = load_block_exps(b);
+                if (!AROWS && t % (8 * kTurns) == 0 && t > 0) block_exp = load_block_exps(b);
             }
-            if ((t & 3) == 2) {
+            if (t % kTurns == kTurns / 2) {
                 if constexpr (AROWS) ea.load(b + 4);
                 eb.load(b + 4);
             }
-            const unsigned xa0 = AROWS ? 0 : __builtin_amdgcn_readlane(block_exp, (2 * t) & 63), xa1 = AROWS ? 0 : __builtin_amdgcn_readlane(block_exp, (2 * t + 1) & 63);
-            block(b, xa0, first, s_0, s_1);
-            block(b + 1, xa1, second, s_1, s_0);
-            if constexpr (AROWS) ea.shift();
-            eb.shift();
+            if constexpr (RING == 2) {
+                const unsigned xa0 = block_byte(t, 0), xa1 = block_byte(t, 1);
+                block(b, xa0, std::integral_constant<int, 0>{}, s_0, s_1);
+                block(b + 1, xa1, std::integral_constant<int, 1>{}, s_1, s_0);
+            } else {
+                const unsigned xa0 = block_byte(t, 0), xa1 = block_byte(t, 1), xa2 = block_byte(t, 2), xa3 = block_byte(t, 3);
+                block(b, xa0, std::integral_constant<int, 0>{}, s_0, s_1);
+                block(b + 1, xa1, std::integral_constant<int, 1>{}, s_1, s_2);
+                if (b + 2 >= b_end) break;
+                block(b + 2, xa2, std::integral_constant<int, 2>{}, s_2, s_3);
+                block(b + 3, xa3, std::integral_constant<int, 3>{}, s_3, s_0);
+            }
+            if constexpr (AROWS) ea.template shift<RING>();
+            eb.template shift<RING>();
         }
         __builtin_amdgcn_s_waitcnt(waitcnt(0, 0));  // (no load may arrive in LDS after the workgroup's end)
     }
@@ -366,7 +384,7 @@ __global__ __launch_bounds__(64 * WI * WJ, 1) void block_gemm_kernel(const Block
 // of 4096 deep: six rounds and 128 small tiles instead of seven).  Fitted to sweeps, us for one output size with 4096 deep,
 // 8-bit / exact:
 //   4096 x 256:  128x64 14.8 / 20.8, 128x128 18.1 / 21.5 (four splits), 256x256 28 / 33
-//   4096 x 1024: 128x64 25.5 / 38.3, 128x128 27.9 / 39.3, 256x256 40 / 51
+//   4096 x 1024: 128x64 25.5 / 38.3, 128x128 25.1 / 39.3, 256x256 40 / 51
 //   4096 x 2048: 128x64 50.6 / 71.0, 128x128 35.4 / 61.6, 256x256 52.7 / 75.8
 //   4096 x 4096: 128x64 95, 128x128 78 / 132, 256x256 59.8 / 110
 struct BlockTileTime {
@@ -375,8 +393,8 @@ struct BlockTileTime {
     float few[2], full[2], shared[2];  // 8-bit, exact
 };
 constexpr BlockTileTime kTiles[] = {
-    {128, 64, 4.0f, {0.30f, 0.33f}, {0.56f, 0.76f}, {0.365f, 0.53f}},
-    {128, 128, 5.0f, {0.33f, 0.50f}, {0.72f, 1.10f}, {0.53f, 0.90f}},
+    {128, 64, 4.0f, {0.30f, 0.33f}, {0.44f, 0.74f}, {0.365f, 0.53f}},
+    {128, 128, 5.0f, {0.33f, 0.50f}, {0.63f, 1.10f}, {0.53f, 0.90f}},
     {256, 256, 9.0f, {0.55f, 1.00f}, {1.59f, 3.15f}, {1.59f, 3.10f}},
 };
 
@@ -414,6 +432,7 @@ BlockGemmPlan block_gemm_plan(bool exact, int64_t I, int64_t J, int64_t C) {
     const int64_t steps = block_pitch(C) / kBlock;
     float best;
     BlockGemmPlan g = one_plan(exact, I, J, steps, true, best);
+    g.us = best;
     g.part_bytes = g.splits > 1 ? ((size_t)g.splits * (size_t)(I * J) * sizeof(float) + 255) & ~size_t(255) : 0;
     const int64_t jtiles = ceil_div64(J, 256), rounds = ceil_div64(I, 256) * jtiles / 256;
     const int64_t itiles = rounds * 256 / jtiles, rest = I - itiles * 256;
@@ -422,7 +441,7 @@ BlockGemmPlan block_gemm_plan(bool exact, int64_t I, int64_t J, int64_t C) {
         const BlockGemmPlan r = one_plan(exact, rest, J, steps, false, rest_us);
         const float us = 9.0f + (float)rounds * kTiles[2].shared[exact] * (float)steps + rest_us;
         if (us < best) {
-            g = {256, 256, 1, (int)(steps ? steps : 1), 0, itiles * 256, r.bi, r.bj};
+            g = {256, 256, 1, (int)(steps ? steps : 1), 0, itiles * 256, r.bi, r.bj, us};
         }
     }
     return g;
@@ -434,10 +453,26 @@ static hipError_t launch_tile(int bi, int bj, BlockGemmParams p, hipStream_t s) 
     p.jtiles = (int)ceil_div64(p.J, bj);
     const dim3 grid((unsigned)((int64_t)p.itiles * p.jtiles), (unsigned)p.splits);
     const int tile = bi * 1000 + bj;
-    if (tile == 256256) block_gemm_kernel<EXACT, AROWS, 256, 256, 2, 2><<<grid, dim3(256), 0, s>>>(p);
-    else if (tile == 128128) block_gemm_kernel<EXACT, AROWS, 128, 128, 2, 2><<<grid, dim3(256), 0, s>>>(p);
-    else if (tile == 128064) block_gemm_kernel<EXACT, AROWS, 128, 64, 2, 2><<<grid, dim3(256), 0, s>>>(p);
-    else return hipErrorInvalidValue;
+    // (four places for the decoding form only where that paid: 25088 x 64 x 4096 28.1 us, 33.9 with two, but 4096 x 256 x 4096
+    // 23.9 and 22.2; of 128 x 128 tiles 25.1 and 28.4 with 256 workgroups, 19.4 and 18.5 with 64)
+    const int64_t workgroups = (int64_t)grid.x * grid.y;
+    const bool alone = workgroups <= 256, many = workgroups > 128;
+    if (tile == 256256) {
+        block_gemm_kernel<EXACT, AROWS, 256, 256, 2, 2, 2><<<grid, dim3(256), 0, s>>>(p);
+    } else if (tile == 128128) {
+        if constexpr (!EXACT) {
+            if (alone && many) {
+                block_gemm_kernel<EXACT, AROWS, 128, 128, 2, 2, 4><<<grid, dim3(256), 0, s>>>(p);
+                return hipGetLastError();
+            }
+        }
+        block_gemm_kernel<EXACT, AROWS, 128, 128, 2, 2, 2><<<grid, dim3(256), 0, s>>>(p);
+    } else if (tile == 128064) {
+        if (alone && (!EXACT || many || p.steps_per_split > 128)) block_gemm_kernel<EXACT, AROWS, 128, 64, 2, 2, 4><<<grid, dim3(256), 0, s>>>(p);
+        else block_gemm_kernel<EXACT, AROWS, 128, 64, 2, 2, 2><<<grid, dim3(256), 0, s>>>(p);
+    } else {
+        return hipErrorInvalidValue;
+    }
     return hipGetLastError();
 }
 static hipError_t launch_form(bool exact, bool a_rows, int bi, int bj, const BlockGemmParams& p, hipStream_t s) {

@@ -1,4 +1,4 @@
-// Y = X W^T for few rows of X (one token, a small batch): a stream of the weight's bytes past the matrix cores.
+// Y = X W^T for few rows of X (one token, a small batch, a small layer): a stream of the weight's bytes past the matrix cores.
 //
 // A wave multiplies 16 rows of W by 16 rows of X, a block of 128 columns at a time.  Lane (row r = l % 16, q = l / 16)
 // takes columns 16 q .. 16 q + 15 and 64 more of both, so a wave's two loads of W are 16 rows of 64 neighbouring bytes;
@@ -120,7 +120,8 @@ __global__ __launch_bounds__(64 * WAVES) void block_matvec_kernel(const BlockMat
 #pragma unroll
     for (int t = 0; t < RT; ++t) w_row[t] = p.values + min(n0 + 16 * t + r16, p.n - 1) * p.kp + 16 * q;
     const uint8_t* const w_exp = p.exps + (n0 >> 7) * blocks;
-    const int64_t xr = min(r16, p.m - 1);
+    const int xr0 = (int)blockIdx.z * 16 + r16;
+    const int64_t xr = min(xr0, p.m - 1);
     const char* const x_row = (const char*)p.X + xr * p.ldx * XBlock<TYPE>::kBytes;
     const uint8_t* const x_exp = TYPE == KQ_T_E4M3 ? p.x_exps + xr * blocks : nullptr;
     f32x4 y[RT];
@@ -167,7 +168,7 @@ __global__ __launch_bounds__(64 * WAVES) void block_matvec_kernel(const BlockMat
 #pragma unroll
     for (int t = 0; t < RT; ++t) s_sum[(t * WAVES + wave) * 64 + lane] = y[t];
     __syncthreads();
-    if (wave < RT && r16 < p.m) {
+    if (wave < RT && xr0 < p.m) {
         f32x4 v = s_sum[wave * WAVES * 64 + lane];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) v += s_sum[(wave * WAVES + w) * 64 + lane];
@@ -176,11 +177,11 @@ __global__ __launch_bounds__(64 * WAVES) void block_matvec_kernel(const BlockMat
             const int64_t n = n0 + 16 * wave + 4 * q + r;
             if (n >= p.n) break;
             if (p.part) {
-                p.part[((int64_t)blockIdx.y * p.m + r16) * p.n + n] = v[r];
+                p.part[((int64_t)blockIdx.y * p.m + xr0) * p.n + n] = v[r];
                 continue;
             }
             const float o = v[r] + (p.bias ? p.bias[n] : 0.0f);
-            const int64_t at = (int64_t)r16 * p.ldy + n;
+            const int64_t at = (int64_t)xr0 * p.ldy + n;
             if (p.y_type == KQ_T_F32) ((float*)p.Y)[at] = o;
             else ((uint16_t*)p.Y)[at] = p.y_type == KQ_T_BF16 ? Act<true>::one(o) : Act<false>::one(o);
         }
@@ -209,9 +210,34 @@ BlockMatvecPlan block_matvec_plan(int m, int64_t n, int64_t k) {
     return v;
 }
 
+// More than 16 rows: sixteens of them in the grid's third dimension.  Every workgroup quantizes its rows of X again, so this is
+// for products that are small: nothing is launched before it, and its workgroups are smaller than the product's.  A
+// workgroup's block takes `x` us for X and 0.054 us for each row tile, and workgroups of one CU share it; a split
+// contraction pays the joining launch.  Fitted to (us, rows / n x k; here and quantizer and product): 64 / 1000 x 512
+// bf16 4.4 and 8.5, fp32 4.8 and 9.7, 8-bit X 3.9 and 5.8; 64 / 1000 x 4096 bf16 8.6 (4x4w4) and 12.4; 32 / 4096 x 4096
+// 10.9 (2x1w4) and 12.9, 64 / 4096 x 4096 14.2 and 13.9; 512 / 1000 x 512 6.9 (4x1w4) and 8.7.
+BlockMatvecPlan block_matvec_plan(int x_type, int m, int64_t n, int64_t k) {
+    const int64_t blocks = block_pitch(k) / kBlock;
+    const float x = x_type == KQ_T_E4M3 ? 0.06f : x_type == KQ_T_F32 ? 0.215f : 0.109f;
+    const float value_us = (float)m * (float)n * 8.0f / 6e6f;
+    BlockMatvecPlan v = {};
+    for (int rt = 1; rt <= 4; rt *= 2) {
+        const int64_t groups = ceil_div64(n, 16 * rt) * ceil_div64(m, 16);
+        for (int splits = 1; splits <= 8 && splits <= (blocks + 3) / 4; splits *= 2) {
+            const int64_t per = ceil_div64(blocks, splits), workgroups = groups * ceil_div64(blocks, per);
+            const float share = workgroups > 256 ? (float)workgroups / 256.0f : 1.0f;
+            const float us = 3.8f + share * (float)per * (x + 0.054f * (float)rt) + (splits > 1 ? 2.0f + (float)splits * value_us : 0.0f);
+            if (v.row_tiles && us >= v.us) continue;
+            v = {rt, 4, (int)ceil_div64(blocks, per), (int)per, 0, us};
+        }
+    }
+    v.ws_bytes = v.splits > 1 ? (size_t)v.splits * (size_t)m * (size_t)n * sizeof(float) : 0;
+    return v;
+}
+
 template <int TYPE>
 static void launch_matvec_type(const BlockMatvecPlan& v, const BlockMatvecParams& p, hipStream_t s) {
-    const dim3 grid((unsigned)ceil_div64(p.n, 16 * v.row_tiles), (unsigned)p.splits), block(64 * v.waves);
+    const dim3 grid((unsigned)ceil_div64(p.n, 16 * v.row_tiles), (unsigned)p.splits, (unsigned)ceil_div64(p.m, 16)), block(64 * v.waves);
     if (v.row_tiles == 4) {
         block_matvec_kernel<TYPE, 4, 4><<<grid, block, 0, s>>>(p);
     } else if (v.row_tiles == 2) {

@@ -53,11 +53,11 @@ def test_linear():
     assert f(Y=None) == ARG and f(Y=FAKE + 2, yt=0) == ARG and f(ldy=19) == ARG and f(bias=FAKE + 2) == ARG
     assert f(m=0, X=None, Y=None) == OK
     w = lib.kq_block_linear_workspace_bytes
-    need = w(1, 1, 17, 20, 100)
+    need = w(1, 1, 1100, 20, 100)
     assert need > 0 and need % 256 == 0
-    assert f(m=17) == WS and f(m=17, ws=FAKE, wsb=need - 1) == WS and f(m=17, ws=FAKE + 16, wsb=need) == WS
-    assert w(1, 1, 0, 20, 100) == 0 and w(4, 1, 17, 20, 100) == 0 and w(1, 3, 17, 20, 100) == 0 and w(1, 1, 17, 0, 100) == 0
-    assert w(3, 1, 17, 20, 100) < need
+    assert f(m=1100) == WS and f(m=1100, ws=FAKE, wsb=need - 1) == WS and f(m=1100, ws=FAKE + 16, wsb=need) == WS
+    assert w(1, 1, 0, 20, 100) == 0 and w(4, 1, 1100, 20, 100) == 0 and w(1, 3, 1100, 20, 100) == 0 and w(1, 1, 1100, 0, 100) == 0
+    assert w(3, 1, 1100, 20, 100) < need
 
 
 def test_gradients():

@@ -22,7 +22,7 @@ int main() {
             const BlockGemmPlan g = block_gemm_plan(exact != 0, i, j, c);
             printf("%d %d %d %d %lld %d %d %lld\n", g.bi, g.bj, g.splits, g.steps_per_split, (long long)g.rest_from, g.rest_bi, g.rest_bj, (long long)g.part_bytes);
         } else {
-            const BlockMatvecPlan v = block_matvec_plan((int)j, i, c);
+            const BlockMatvecPlan v = what == 'v' ? block_matvec_plan((int)j, i, c) : block_matvec_plan((int)exact, (int)j, i, c);
             printf("%d %d %d %d %lld 0 0 0\n", v.row_tiles, v.waves, v.splits, v.blocks_per_split, (long long)v.ws_bytes);
         }
     }
@@ -94,6 +94,18 @@ def test_few_rows_over_the_whole_range(plans):
         assert (rt, waves) in ((4, 4), (2, 4), (2, 8), (1, 4), (1, 8), (1, 16))
         assert 1 <= splits <= 65535 and (splits - 1) * per < blocks <= splits * per
         assert ws == (0 if splits == 1 else splits * m * n * 4)
+
+
+def test_more_rows_over_the_whole_range(plans):
+    cases = [("w", t, n, m, k) for t in (0, 1, 2, 3) for n, m, k in accepted() if 16 < m <= 1024] + \
+            [("w", 1, n, m, k) for n in (1, 100, 1000, 4096) for m in (17, 33, 100, 1024) for k in (1, 129, 640, 1025, 25088)]
+    got = plans(cases)
+    for (_, _, n, m, k), (rt, waves, splits, per, ws, *_rest) in zip(cases, got):
+        blocks = pitch(k) // 128
+        assert rt in (1, 2, 4) and waves == 4
+        assert 1 <= splits <= 8 and (splits - 1) * per < blocks <= splits * per
+        assert ws == (0 if splits == 1 else splits * m * n * 4)
+    assert {g[0] for g in got} == {1, 2, 4} and any(g[2] > 1 for g in got)
 
 
 def test_the_multiplied_sizes_take_every_tile(plans):

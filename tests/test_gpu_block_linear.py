@@ -187,6 +187,24 @@ def test_linear(m, n, k, dtype):
     check(Y, hat(X, 1), W, k, dtype == F32 or m <= 16, None if bias is None else bias.double())
 
 
+@pytest.mark.parametrize("m,n,k", [(17, 1000, 512), (64, 1000, 4000), (100, 200, 1000), (130, 1000, 300), (1000, 60, 900), (1024, 1, 1), (300, 17, 5000)])
+def test_small_products_of_many_rows(m, n, k):
+    """Sixteens of rows without a launch for the quantizer: exact products whatever the output's type, with strided rows, a
+    bias and quantized rows too."""
+    (values, exps), W = layer(n, k, m + n)
+    X, bias = acts(m, k, BF, m), torch.randn(n, generator=gen(n))
+    wide = torch.full((m, k + 13), math.nan, dtype=BF, device=DEV)
+    wide[:, 5:5 + k] = X.to(DEV)
+    for dtype in (BF, HF, F32):
+        Y = torch.full((m + 1, n + 3), 7.0, dtype=dtype, device=DEV)
+        kq.kq_block_linear(wide[:, 5:5 + k], values, exps, bias.to(DEV), Y=Y[:m, 2:2 + n])
+        check(Y[:m, 2:2 + n], hat(X, 1), W, k, dtype == F32, bias.double())
+        assert torch.all(Y[:, :2] == 7) and torch.all(Y[:, 2 + n:] == 7) and torch.all(Y[m] == 7)
+    q = kq.kq_quantize_blocks(X.to(DEV))
+    Y = kq.kq_block_linear(q[0], values, exps, bias.to(DEV), q[1])
+    check(Y, hat(X, 1), W, k, False, bias.double())
+
+
 @pytest.mark.parametrize("out", [BF, HF, F32])
 @pytest.mark.parametrize("m,n,k", [(1, 100, 300), (13, 129, 512), (40, 130, 130), (300, 260, 700)])
 def test_linear_of_quantized_rows(m, n, k, out):
@@ -433,6 +451,28 @@ def test_every_tile(i, j, c, dtype):
     assert torch.all((db.double() - d.sum(0)).abs() <= (c + 1) * 2.0 ** -24 * d.abs().sum(0))
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("i,j", [(130, 70), (1500, 1000), (2050, 1030)])
+def test_every_length_of_the_contraction(i, j, dtype):
+    """One to ten blocks, whole and not: where the products' loops begin and end."""
+    g = torch.Generator(device=DEV).manual_seed(i)
+    for c in [128 * s - 5 for s in range(1, 11)] + [256, 512, 1024]:
+        W = torch.randn(c, i, device=DEV, generator=g) / math.sqrt(c)
+        dY = (0.01 * torch.randn(j, c, device=DEV, generator=g)).to(dtype)
+        values, exps = kq.kq_quantize_blocks(W, rows=128)
+        a, b = again(dY), kq.kq_reconstruct_blocks(values, exps, i, rows=128).double().t()
+        dX = kq.kq_block_linear_grad_input(dY, values, exps, i)
+        y64, S = a @ b.t(), a.abs() @ b.abs().t()
+        tol = U[dtype] * y64.abs() + ((c + 16) * 2.0 ** -24 + (0 if dtype == F32 else 7 * 2.0 ** -13)) * S + TINY[dtype]
+        assert torch.all((dX.double() - y64).abs() <= tol), c
+        x = kq.kq_quantize_blocks(torch.randn(c, i, device=DEV, generator=g).to(BF))
+        dW, _ = kq.kq_block_linear_grad_weight(dY.t().contiguous(), *x, i, dtype=dtype)
+        a, b = again(dY), again(kq.kq_reconstruct_blocks(*x, i).t())
+        y64, S = a @ b.t(), a.abs() @ b.abs().t()
+        tol = U[dtype] * y64.abs() + ((c + 16) * 2.0 ** -24 + (0 if dtype == F32 else 7 * 2.0 ** -13)) * S + TINY[dtype]
+        assert torch.all((dW.double() - y64).abs() <= tol), c
+
+
 # ---- how the calls run ---------------------------------------------------------------------------------
 
 def test_same_bits_every_time_and_on_another_stream():
@@ -506,8 +546,8 @@ def test_without_the_host_helper(monkeypatch):
 
 def test_given_workspace():
     (values, exps), _ = layer(300, 600, 1)
-    X = acts(40, 600, BF, 1).to(DEV)
-    nb = kq.lib.kq_block_linear_workspace_bytes(kq.KQ_T_BF16, kq.KQ_T_BF16, 40, 300, 600)
+    X = acts(1100, 600, BF, 1).to(DEV)
+    nb = kq.lib.kq_block_linear_workspace_bytes(kq.KQ_T_BF16, kq.KQ_T_BF16, 1100, 300, 600)
     ws = torch.full((nb + 256,), 255, dtype=torch.uint8, device=DEV)
     assert torch.equal(kq.kq_block_linear(X, values, exps, workspace=ws), kq.kq_block_linear(X, values, exps))
     assert torch.all(ws[nb:] == 255)
