@@ -1,12 +1,12 @@
 // Fully-connected layers in 8-bit floats (e4m3) with a power of two for each block of 128: what the translation
 // units share.
 //
-// Every product is out[j][i] = sum_c A[i][c] B[j][c] of two operands held the same way: rows of e4m3 values along the
+// Every product is out[j][i] = sum_c A[i][c] B[j][c] of two operands held the same way (but for W^T): rows of e4m3 values along the
 // contraction, their pitch a multiple of 128 bytes with zeros past the end, and one exponent byte for 128 of them.  So
 // a kernel has no edges along the contraction, every row is aligned, and a block's exponent is one byte of the scaled
 // matrix instruction (or one factor of a decoded operand).
 //   linear       Y[m][n]   i = n, j = m, c = k   A = W (128 x 128 blocks), B = X
-//   grad input   dX[m][k]  i = k, j = m, c = n   A = W^T (its bytes transposed, the same blocks), B = dY
+//   grad input   dX[m][k]  i = k, j = m, c = n   A = W^T (read as W lies, the same blocks), B = dY
 //   grad weight  dW[n][k]  i = k, j = n, c = m   A = X^T, B = dY^T, both quantized along m
 #pragma once
 
@@ -67,7 +67,7 @@ struct BlockReconstructParams {
 hipError_t launch_reconstruct_blocks(const BlockReconstructParams& p, hipStream_t s);
 
 // out[c][r], r along the 128-row blocks of X, pitch rp (a multiple of 128, zeros past m): quantized along r (again, where X is
-// bytes), or the same bytes.
+// bytes).
 struct BlockTransposeParams {
     const void* X;        // [m][cols], or bytes of pitch ldx with in_exps [m][ldx / 128]
     int64_t ldx;
@@ -75,11 +75,9 @@ struct BlockTransposeParams {
     const uint8_t* in_exps;
     int64_t m, cols, rp;
     uint8_t* values;      // [cols][rp]
-    uint8_t* exps;        // [cols][rp / 128]; not of the same bytes
+    uint8_t* exps;        // [cols][rp / 128]
     float* sums;          // [rp / 128][cols]: sums over each 128 rows, or NULL
 };
-// dY quantized in blocks of one row, W's bytes transposed
-hipError_t launch_grad_input_operands(const BlockQuantizeParams& q, const BlockTransposeParams& t, hipStream_t s);
 // X's values and dY, transposed and quantized along the rows
 hipError_t launch_grad_weight_operands(const BlockTransposeParams& x, const BlockTransposeParams& dy, hipStream_t s);
 
@@ -89,9 +87,12 @@ struct BlockOperand {
     const uint8_t* e;        // exponent of row r, block b: e[r * e_row + b * e_col], r / 128 for r in the 128 x 128 form
     int64_t e_row, e_col;
 };
+// How A lies: rows with an exponent for 128 x 128 of them, rows with their own, or columns A[i][c] at v[c * pitch + i] (128 x 128)
+enum { kFormBlocks, kFormRows, kFormColumns };
 struct BlockGemmParams {
     BlockOperand A, B;
     int64_t I, J;
+    int64_t depth, a_cols;   // kFormColumns: rows c that there are, and columns of each (a multiple of 128)
     int steps;               // blocks of the contraction
     const float* bias;       // [I] or NULL
     void* out;
@@ -114,8 +115,7 @@ struct BlockGemmPlan {
 };
 // exact: products on the 16-bit matrix instructions
 BlockGemmPlan block_gemm_plan(bool exact, int64_t I, int64_t J, int64_t C);
-// a_rows: A's blocks are 1 x 128 (else 128 x 128)
-hipError_t launch_block_gemm(bool exact, bool a_rows, const BlockGemmPlan& plan, BlockGemmParams p, void* part, hipStream_t s);
+hipError_t launch_block_gemm(bool exact, int form, const BlockGemmPlan& plan, BlockGemmParams p, void* part, hipStream_t s);
 
 // Y = X W^T for few rows of X: up to kBlockMatvecRows always, up to kBlockMatvecMost where the plan is the faster one.
 constexpr int kBlockMatvecRows = 16, kBlockMatvecMost = 1024;

@@ -166,7 +166,7 @@ struct RawTile {
     static constexpr int kBytes = TYPE == KQ_T_F32 ? 4 : TYPE == KQ_T_E4M3 ? 1 : 2;
     unsigned w[8][kWords];
     float step[8];   // KQ_T_E4M3: the row's power of two
-    __device__ __forceinline__ void load(const BlockTransposeParams& p, int64_t r0, int64_t c0, bool with_exps = true) {
+    __device__ __forceinline__ void load(const BlockTransposeParams& p, int64_t r0, int64_t c0) {
         const int64_t first = min(r0, p.m - 1);
         const int last = (int)min(p.m - 1 - first, (int64_t)7);  // (rows past it: again, and cleared below)
         const char* at = (const char*)p.X + first * p.ldx * kBytes;
@@ -194,18 +194,16 @@ struct RawTile {
             }
         }
         if constexpr (TYPE == KQ_T_E4M3) {
-            if (with_exps) {
-                const int64_t pitch = p.ldx >> 7;
-                const uint8_t* e = p.in_exps + first * pitch + (c0 >> 7);
-                unsigned x[8];
+            const int64_t pitch = p.ldx >> 7;
+            const uint8_t* e = p.in_exps + first * pitch + (c0 >> 7);
+            unsigned x[8];
 #pragma unroll
-                for (int t = 0; t < 8; ++t) {
-                    x[t] = *e;
-                    e += t < last ? pitch : 0;
-                }
-#pragma unroll
-                for (int t = 0; t < 8; ++t) step[t] = checkpoint_step(x[t]);
+            for (int t = 0; t < 8; ++t) {
+                x[t] = *e;
+                e += t < last ? pitch : 0;
             }
+#pragma unroll
+            for (int t = 0; t < 8; ++t) step[t] = checkpoint_step(x[t]);
         }
         if (r0 + 8 > p.m) {
 #pragma unroll
@@ -301,42 +299,8 @@ __device__ __forceinline__ void transpose_quantize(const BlockTransposeParams& p
     }
 }
 
-// The same bytes transposed.
-__device__ __forceinline__ void transpose_bytes(const BlockTransposeParams& p, unsigned workgroup, u32x2* s_t) {
-    const int tid = threadIdx.x, l16 = tid & 15, rg = tid >> 4;
-    int64_t r0, c0;
-    tile_of(p, workgroup, r0, c0);
-    RawTile<KQ_T_E4M3> raw;
-    raw.load(p, r0 + 8 * rg, c0 + 8 * l16, false);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        // 4 x 4 bytes: rows 4 g .. 4 g + 3 of columns 4 h .. 4 h + 3
-        unsigned o[4][2];
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            const unsigned a = raw.w[4 * g][h], b = raw.w[4 * g + 1][h], c = raw.w[4 * g + 2][h], d = raw.w[4 * g + 3][h];
-            const unsigned ab0 = __builtin_amdgcn_perm(b, a, 0x05010400u), ab1 = __builtin_amdgcn_perm(b, a, 0x07030602u);
-            const unsigned cd0 = __builtin_amdgcn_perm(d, c, 0x05010400u), cd1 = __builtin_amdgcn_perm(d, c, 0x07030602u);
-            o[0][g] = __builtin_amdgcn_perm(cd0, ab0, 0x05040100u);
-            o[1][g] = __builtin_amdgcn_perm(cd0, ab0, 0x07060302u);
-            o[2][g] = __builtin_amdgcn_perm(cd1, ab1, 0x05040100u);
-            o[3][g] = __builtin_amdgcn_perm(cd1, ab1, 0x07060302u);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s_t[(8 * l16 + 4 * h + j) * 16 + (rg ^ l16)] = u32x2{o[j][0], o[j][1]};
-    }
-    __syncthreads();
-    store_transposed(p, s_t, r0, c0);
-}
-
 // Both operands of a gradient in one launch, the first `first` workgroups the first of them: two short passes after each
 // other leave half the chip idle at their ends, and each launch costs 2 to 3 us.
-template <int TYPE>
-__global__ __launch_bounds__(256) void grad_input_operands_kernel(const BlockQuantizeParams q, const BlockTransposeParams t, unsigned first) {
-    __shared__ u32x2 s_t[128 * 16];
-    if (blockIdx.x < first) transpose_bytes(t, blockIdx.x, s_t);
-    else quantize_rows<TYPE>(q, blockIdx.x - first);
-}
 template <int TYPE>
 __global__ __launch_bounds__(256) void grad_weight_operands_kernel(const BlockTransposeParams x, const BlockTransposeParams dy, unsigned first) {
     __shared__ TransposeShared s;
@@ -345,14 +309,6 @@ __global__ __launch_bounds__(256) void grad_weight_operands_kernel(const BlockTr
     else transpose_quantize<TYPE, false>(dy, blockIdx.x - first, s);
 }
 
-hipError_t launch_grad_input_operands(const BlockQuantizeParams& q, const BlockTransposeParams& t, hipStream_t s) {
-    const unsigned first = transpose_workgroups(t);
-    const dim3 grid(first + quantize_rows_workgroups(q)), block(256);
-    if (q.type == KQ_T_F32) grad_input_operands_kernel<KQ_T_F32><<<grid, block, 0, s>>>(q, t, first);
-    else if (q.type == KQ_T_BF16) grad_input_operands_kernel<KQ_T_BF16><<<grid, block, 0, s>>>(q, t, first);
-    else grad_input_operands_kernel<KQ_T_F16><<<grid, block, 0, s>>>(q, t, first);
-    return hipGetLastError();
-}
 hipError_t launch_grad_weight_operands(const BlockTransposeParams& x, const BlockTransposeParams& dy, hipStream_t s) {
     const unsigned first = transpose_workgroups(x);
     const dim3 grid(first + transpose_workgroups(dy)), block(256);

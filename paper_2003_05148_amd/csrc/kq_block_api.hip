@@ -71,13 +71,12 @@ struct LinearSizes {
 };
 struct GradInputSizes {
     BlockGemmPlan plan;
-    size_t dy, dy_exps, wt, total;
+    size_t dy, dy_exps, total;
     GradInputSizes(int32_t type, int64_t m, int64_t n, int64_t k) : plan(block_gemm_plan(type == KQ_T_F32, k, m, n)) {
         const int64_t np = block_pitch(n);
         dy = region(m * np);
         dy_exps = region(m * (np / kBlock));
-        wt = region(k * np);
-        total = plan.part_bytes + dy + dy_exps + wt;
+        total = plan.part_bytes + dy + dy_exps;
     }
 };
 // The bias' gradient: the transposing pass leaves a sum for each 128 rows and the product adds them where it writes its first
@@ -172,7 +171,7 @@ kq_status kq_block_linear(const void* X, int32_t x_type, int64_t ldx, const uint
     p.out = Y;
     p.type = y_type;
     p.ldo = ldy;
-    return hip_status(launch_block_gemm(y_type == KQ_T_F32, false, z.plan, p, part, s));
+    return hip_status(launch_block_gemm(y_type == KQ_T_F32, kFormBlocks, z.plan, p, part, s));
 }
 
 size_t kq_block_linear_grad_input_workspace_bytes(int32_t type, int64_t m, int64_t n, int64_t k) {
@@ -196,11 +195,12 @@ kq_status kq_block_linear_grad_input(const void* dY, int32_t type, int64_t ldy, 
     float* const part = r.take<float>(z.plan.part_bytes);
     const int64_t np = block_pitch(n), kp = block_pitch(k);
     const BlockQuantizeParams q = {dY, ldy, type, m, n, np, r.take(z.dy), r.take(z.dy_exps)};
-    const BlockTransposeParams t = {values, kp, KQ_T_E4M3, nullptr, n, k, np, r.take(z.wt), nullptr, nullptr};
-    const hipError_t e = launch_grad_input_operands(q, t, s);
+    const hipError_t e = launch_quantize_blocks(q, 1, s);
     if (e != hipSuccess) return hip_status(e);
     BlockGemmParams p = {};
-    p.A = {t.values, np, exps, 1, kp / kBlock};  // row block of W^T = column block of W
+    p.A = {values, kp, exps, 1, kp / kBlock};  // row block of W^T = column block of W
+    p.depth = n;
+    p.a_cols = kp;
     p.B = {q.values, np, q.exps, np / kBlock, 1};
     p.I = k;
     p.J = m;
@@ -208,7 +208,7 @@ kq_status kq_block_linear_grad_input(const void* dY, int32_t type, int64_t ldy, 
     p.out = dX;
     p.type = type;
     p.ldo = ldx;
-    return hip_status(launch_block_gemm(type == KQ_T_F32, false, z.plan, p, part, s));
+    return hip_status(launch_block_gemm(type == KQ_T_F32, kFormColumns, z.plan, p, part, s));
 }
 
 size_t kq_block_linear_grad_weight_workspace_bytes(int32_t dw_type, int64_t m, int64_t n, int64_t k) {
@@ -259,7 +259,7 @@ kq_status kq_block_linear_grad_weight(const void* dY, int32_t type, int64_t ldy,
         }
     }
     p.dbias = dbias;
-    return hip_status(launch_block_gemm(dw_type == KQ_T_F32, true, z.plan, p, part, s));
+    return hip_status(launch_block_gemm(dw_type == KQ_T_F32, kFormRows, z.plan, p, part, s));
 }
 
 }  // extern "C"

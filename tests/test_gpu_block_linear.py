@@ -325,6 +325,21 @@ def test_grad_input(m, n, k, dtype):
     check(dX, hat(dY, 1), W.t(), n, dtype == F32)
 
 
+@pytest.mark.parametrize("n,k", [(130, 300), (257, 130), (300, 700), (1, 1)])
+def test_input_gradient_of_weight_blocks_of_nan(n, k):
+    """A block of the last, partial rows of W that is NaN: its columns of dX, and no other."""
+    for m, dtype in ((3, BF), (300, HF), (40, F32)):
+        W = torch.randn(n, k, generator=gen(n)) / math.sqrt(k)
+        W[n - 1, 0] = math.nan
+        values, exps = kq.kq_quantize_blocks(W.to(DEV), rows=128)
+        dY = (0.01 * acts(m, n, F32, k)).to(dtype)
+        dX = kq.kq_block_linear_grad_input(dY.to(DEV), values, exps, k)
+        assert torch.all(torch.isnan(dX[:, :128]))
+        if k > 128:
+            W[n - 1, 0] = 0.0
+            check(dX[:, 128:], hat(dY, 1), hat(W, 128).t().contiguous()[128:], n, dtype == F32)
+
+
 @pytest.mark.parametrize("m", [64 * 128, 64 * 128 + 1, 70 * 128, 95 * 128 + 5, 128 * 128])
 def test_bias_gradient_of_many_rows(m):
     """Sums over 128 rows are added in groups above 64 of them, and the rest of them alone: within the tolerance of m terms."""
