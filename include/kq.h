@@ -755,7 +755,7 @@ kq_status kq_block_linear_grad_weight(const void* dY, int32_t type, int64_t ldy,
  * kq_distill_loss -- loss, and stats device [m][3] fp32 for the gradient: the row's largest logit, the sum of
  *   exp((z - largest) / T) and that of exp(z - largest) (0 where it is not needed).
  * kq_distill_grad -- dZ (may be Z) from the same inputs, stats and dloss (device [m] fp32, or NULL for `scale`).
- *   Sums in fp32, in an order that the sizes and the alignment of Z's rows decide.
+ *   Sums in fp32, in an order that the call, the sizes, the weights of the terms and the alignment of Z's rows decide.
  *   workspace: kq_distill_workspace_bytes(type, m, v, top) (may be 0).
  */
 #define KQ_DISTILL_MAX_CLASSES (1 << 24)

@@ -432,7 +432,7 @@ __device__ __forceinline__ void add_single(Sums& s, float x, bool two, const Exp
 // CH chunks a thread in registers, WAVES waves a row (1: four rows a workgroup).  CH = 0: the row is read again.
 // LOSS, GRAD: what is asked for; the gradient alone takes a row's stats.
 template <int TYPE, int CH, int WAVES, bool LOSS, bool GRAD>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, WAVES == 16 ? 8 : 1) void distill_row_kernel(const DistillParams p) {
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, WAVES == 16 ? (CH > 8 ? 4 : 8) : 1) void distill_row_kernel(const DistillParams p) {
     constexpr int NT = 64 * WAVES;
     constexpr int kHeld = CH ? CH : 1;
     __shared__ float s_red[3][WAVES];
@@ -697,6 +697,11 @@ template <int TYPE, bool LOSS, bool GRAD>
 static void launch_rows(const DistillParams& p, hipStream_t s) {
     const int chunks = p.v / Row<TYPE>::N;
     const dim3 four((unsigned)ceil_div64(p.m, 4)), one((unsigned)p.m);
+    // (16 chunks a thread leave a CU one row, whose loads, sums and stores then come after each other: 1024 x 65536 fp32 103 us
+    // and 126 read twice, 1024 x 50000 85 and 94; 2048 x 128256 bf16 212 and 238, but 100001 200 and 197, and with two
+    // exponentials 253 and 211)
+    const bool two = p.alpha > 0.0f && p.T != 1.0f;
+    const bool hold = GRAD && chunks <= 16384 && (TYPE == KQ_T_F32 || (chunks > 13000 && !two));
     if (chunks <= 128) distill_row_kernel<TYPE, 2, 1, LOSS, GRAD><<<four, 256, 0, s>>>(p);
     else if (chunks <= 512) distill_row_kernel<TYPE, 8, 1, LOSS, GRAD><<<four, 256, 0, s>>>(p);
     if constexpr (LOSS) {
@@ -704,6 +709,7 @@ static void launch_rows(const DistillParams& p, hipStream_t s) {
         if (chunks <= 2048) distill_row_kernel<TYPE, 8, 4, LOSS, GRAD><<<one, 256, 0, s>>>(p);
         else if (chunks <= 4096) distill_row_kernel<TYPE, 4, 16, LOSS, GRAD><<<one, 1024, 0, s>>>(p);
         else if (chunks <= 8192) distill_row_kernel<TYPE, 8, 16, LOSS, GRAD><<<one, 1024, 0, s>>>(p);
+        else if (hold) distill_row_kernel<TYPE, GRAD ? 16 : 0, 16, LOSS, GRAD><<<one, 1024, 0, s>>>(p);
         else distill_row_kernel<TYPE, 0, 16, LOSS, GRAD><<<one, 1024, 0, s>>>(p);
     }
 }

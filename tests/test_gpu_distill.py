@@ -115,6 +115,31 @@ def test_loss_and_gradient(m, v, top, dtype):
     assert torch.equal(a, loss) and torch.equal(b, dz)      # the same bits every time
 
 
+@pytest.mark.parametrize("v,dtype", [(4500, F32), (9001, BF), (12000, F32), (20003, HF), (30001, F32), (50001, BF), (65530, F32), (70001, BF),
+                                     (110001, BF), (130000, HF), (140001, F32)])
+def test_long_rows_of_many(v, dtype):
+    """As many rows as have a workgroup each, with every number of chunks a thread: single rows against the formula, by one call
+    and by two (which may add a row in another order), and all of them again and in place."""
+    m, rows = 193, [0, 1, 2, 96, 191, 192]
+    Z, values, idx, labels = logits(m, v, 20, dtype, v)
+    idx[1], labels[1] = -1, -1                    # a row without a term
+    Z[2, :v // 2] = -math.inf
+    Z[2, idx[2].clamp(min=0)] = 0.0
+    Z[2, labels[2].clamp(min=0)] = 0.0
+    z, tv, ti, y = on(Z, values, idx, labels)
+    for T, alpha in ((1.0, 0.0), (1.0, 0.5), (2.5, 0.3)):
+        loss, dz = kq.kq_distill(z, tv, ti, temperature=T, labels=y, alpha=alpha)
+        pick = lambda x: x[rows]
+        check(loss[rows], dz[rows], pick(Z), pick(values), pick(idx), pick(labels), T, alpha, torch.ones(len(rows)).double())
+        l2, stats = kq.kq_distill_loss(z, tv, ti, T, y, alpha)
+        g = kq.kq_distill_grad(z, tv, ti, stats, None, T, y, alpha)
+        check(l2[rows], g[rows], pick(Z), pick(values), pick(idx), pick(labels), T, alpha, torch.ones(len(rows)).double())
+        l3, same = kq.kq_distill(z.clone(), tv, ti, temperature=T, labels=y, alpha=alpha, dZ=None)
+        inplace = z.clone()
+        l4, out = kq.kq_distill(inplace, tv, ti, temperature=T, labels=y, alpha=alpha, dZ=inplace)
+        assert out is inplace and torch.equal(l3, loss) and torch.equal(l4, loss) and torch.equal(same, dz) and torch.equal(inplace, dz)
+
+
 @pytest.mark.parametrize("T", [1.0, 4.0, 2.0 ** -3])
 @pytest.mark.parametrize("alpha", [0.0, 0.25, 1.0])
 def test_weights_and_types_of_the_inputs(T, alpha):
