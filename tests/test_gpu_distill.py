@@ -398,3 +398,45 @@ def test_a_retraining_step():
     # the product with 0.1 is rounded (2^-24 of it, and 0.1 itself 2^-25) or fused, then the difference (2^-24 of it)
     want = W.double() - 0.1 * dW.double().cpu()
     assert torch.all((fc.master.double().cpu() - want).abs() <= 2.0 ** -24 * want.abs() + 2.0 ** -23 * 0.1 * dW.double().cpu().abs())
+
+
+def example():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "fc8_distill.py")
+    spec = importlib.util.spec_from_file_location("fc8_distill", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    return mod
+
+
+def test_retraining_example_runs():
+    losses, (fc1, fc2) = example().retrain(n_in=300, n_hidden=260, classes=100, batch=70, steps=4)
+    assert len(losses) == 4 and all(math.isfinite(v) for v in losses)
+    assert fc2(torch.relu(fc1(torch.randn(1, 300, device=DEV, dtype=BF)))).shape == (1, 100)
+
+
+def test_retraining_examples_gradients():
+    """Against the formulas in 64 bits on what the 8-bit layers stand for.  The 8-bit steps of the activation, of dZ (twice) and of dA
+    (twice) are at most 2^-4 of a value each, bf16's 2^-8: of a sum's norm (errors of random signs) less than 2^-4 for dZ's
+    products and 2^-3 for those that come after dA."""
+    m, n_in, n_hidden, classes = 70, 300, 260, 100
+    g = gen(8)
+    W1, W2 = torch.randn(n_hidden, n_in, generator=g) / math.sqrt(n_in), 2 * torch.randn(classes, n_hidden, generator=g) / math.sqrt(n_hidden)
+    b1, b2 = 0.1 * torch.randn(n_hidden, generator=g), 0.1 * torch.randn(classes, generator=g)
+    X = torch.randn(m, n_in, generator=g).relu().to(BF)
+    fc1, fc2 = kq.BlockLinear(W1.to(DEV), b1.to(DEV)), kq.BlockLinear(W2.to(DEV), b2.to(DEV))
+    t = torch.relu(X.float() @ W1.t() + b1) @ W2.t() + b2
+    values, idx = t.topk(10, 1)
+    labels = idx[:, 0].contiguous()
+    loss, got = example().gradients(fc1, fc2, X.to(DEV), values.to(DEV), idx.to(DEV), labels.to(DEV))
+    w2 = fc2.weight().double().cpu()
+    H = fc1.forward(X.to(DEV))[0]
+    Z = fc2.forward(torch.relu(H))[0].cpu()
+    want, dz, _, _ = formula(Z, values, idx, labels, 2.0, 0.3, torch.full((m,), 1 / m).double())
+    check(loss, None, Z, values, idx, labels, 2.0, 0.3, torch.full((m,), 1 / m).double())
+    A = torch.relu(H).double().cpu()
+    dH = (dz @ w2) * (A > 0)
+    for a, b, bound in ((got[0], dH.t() @ X.double(), 2.0 ** -3), (got[1], dH.sum(0), 2.0 ** -3), (got[2], dz.t() @ A, 2.0 ** -4),
+                        (got[3], dz.sum(0), 2.0 ** -4)):
+        assert float((a.double().cpu() - b).norm() / b.norm()) < bound
