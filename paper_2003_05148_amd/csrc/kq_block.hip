@@ -6,7 +6,9 @@
 namespace kq {
 
 // ---- blocks of one row -------------------------------------------------------------------------------------
-// Sixteen lanes a block, 8 columns a lane.  a 2^-e is exact, so the conversion's rounding is the only one.
+// Sixteen lanes a block, 8 columns a lane: a block's largest magnitude is four exchanges away.  x 2^-e is exact, so the
+// conversion's rounding is the only one.  Memory bounds it (4096 x 4096 bf16: 10.2 us, 50 MB), a launch where it is small (33 x
+// 1000 fp32: 2.5 us).
 template <int TYPE>
 __device__ __forceinline__ void quantize_rows(const BlockQuantizeParams& p, unsigned workgroup) {
     const unsigned per_row = (unsigned)(p.kp >> 3);       // 8-column pieces
@@ -44,7 +46,8 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const BlockQuantizeP
 static unsigned quantize_rows_workgroups(const BlockQuantizeParams& p) { return (unsigned)ceil_div64(p.m * (p.kp >> 3), 256); }
 
 // ---- blocks of 128 rows ------------------------------------------------------------------------------------
-// A workgroup a block, 16 lanes a row of it, eight rows a thread.
+// A workgroup a block, 16 lanes a row of it, eight rows a thread: the block stays in registers between its largest magnitude
+// and the conversion, so it is read once.  Memory bounds it (4096 x 25088 fp32: 87 us, 5.9 TB/s).
 template <int TYPE>
 __global__ __launch_bounds__(256) void quantize_tiles_kernel(const BlockQuantizeParams p) {
     __shared__ unsigned s_max[4];
@@ -104,7 +107,9 @@ hipError_t launch_quantize_blocks(const BlockQuantizeParams& p, int rows, hipStr
 }
 
 // ---- reconstruction ----------------------------------------------------------------------------------------
-// Sixteen lanes a block, four neighbouring columns at a time: a block's lanes write contiguous memory.
+// Sixteen lanes a block, four neighbouring columns at a time: a block's lanes write contiguous memory.  v 2^e has 4 significant
+// bits, so only 16-bit outputs round (beyond fp16's range, or below a type's smallest normal number).  Memory bounds it
+// (4096 x 25088 to fp32: 76 us, 6.8 TB/s, its stores past the caches' normal ways).
 template <int TYPE>
 __global__ __launch_bounds__(256) void reconstruct_blocks_kernel(const BlockReconstructParams p) {
     const unsigned per_row = (unsigned)(p.kp >> 3), id = blockIdx.x * 256u + threadIdx.x;  // (fewer than 2^32 threads)
@@ -136,6 +141,8 @@ hipError_t launch_reconstruct_blocks(const BlockReconstructParams& p, hipStream_
 // A workgroup takes 128 rows by 128 columns; a thread 8 neighbouring rows of 8 neighbouring columns, so that what it
 // writes to LDS transposed are 8-byte pieces.  Piece q of column c lies at q ^ (c / 8): the sixteen column groups of a
 // wave's store fall on sixteen different pieces.  All of a thread's loads are on their way before the first is used.
+// Memory bounds it where it is large (dY 4096 x 4096 bf16 and X 4096 x 25088 in one launch: 53 us, 256 MB at 4.8 TB/s), and a
+// workgroup's own latency, about 4 us, where it is small (2047 x 1000 and 2047 x 4095: 10.5 us for 640 workgroups).
 struct TransposeShared {
     u32x2 t[128 * 16];
     unsigned exps[4][64];   // of two neighbouring columns

@@ -11,6 +11,9 @@
 // the largest logit, the sums and the gradient (distill_row_kernel: a wave a row while 8 chunks a lane hold it,
 // then 256 or 1024 threads).  Rows of more chunks than that are read again.  Where there are few rows of many
 // classes, a row is cut into segments: one kernel takes their largest logits and sums, the next joins them.
+// 4096 x 50001 bf16: loss and gradient 161 to 170 us (822 MB, 4.8 to 5.1 TB/s, a copy's rate 5.2), the loss alone 85,
+// the gradient alone 158.  With two temperatures (T other than 1 and labels) the exponentials bound it as well: 212, 122
+// and 163 us.  Small calls are bound by a launch and the chain index, logit, sum (64 x 1000: 6.4 us).
 #include "kq_values.h"
 
 namespace kq {
