@@ -1467,8 +1467,8 @@ class BlockLinear:
     def __init__(self, W, bias=None, master: bool = False):
         self.out_features, self.in_features = W.shape
         self.values, self.exps = kq_quantize_blocks(W, KQ_BLOCK)
-        self.master = W.float().clone() if master else None
-        self.bias = None if bias is None else _dev(bias, torch.float32, "bias", (self.out_features,)).clone()
+        self.master = W.detach().float().clone() if master else None
+        self.bias = None if bias is None else _dev(bias, torch.float32, "bias", (self.out_features,)).detach().clone()
 
     def __call__(self, X, dtype=None):
         return kq_block_linear(X, self.values, self.exps, self.bias, dtype=dtype)

@@ -616,6 +616,18 @@ def test_layer_trains():
 
 # ---- refusals ---------------------------------------------------------------------------------
 
+def test_layer_of_parameters():
+    """A layer made from a network's parameters keeps no graph, and its steps build none."""
+    W = torch.nn.Parameter(torch.randn(130, 200, device=DEV))
+    b = torch.nn.Parameter(torch.randn(130, device=DEV))
+    fc = kq.BlockLinear(W, b, master=True)
+    X = torch.randn(9, 200, device=DEV, dtype=BF, requires_grad=True)
+    Y, kept = fc.forward(X)
+    fc.step(*fc.backward(torch.ones_like(Y), kept)[1:], 0.1)
+    assert not any(t.requires_grad for t in (fc.master, fc.bias, Y, fc.weight(), fc(X), *kept))
+    assert fc.master.data_ptr() != W.data_ptr() and fc.bias.data_ptr() != b.data_ptr()
+
+
 def test_refusals():
     (values, exps), _ = layer(100, 200, 1)
     X = acts(5, 200, BF, 1).to(DEV)
