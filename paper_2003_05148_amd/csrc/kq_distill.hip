@@ -666,10 +666,12 @@ __global__ __launch_bounds__(256) void distill_segment_kernel(const DistillParam
 }
 
 // ---- which kernels a call takes -------------------------------------------------------------------------------------
-// Rows are cut where they are few and long: into about 512 segments in all, each at least 512 chunks (16 x 131071 fp32, loss and
-// gradient in one call: 17.8 us; 256 segments 18.4, 2048 22.1).  The gradient alone takes 1024 chunks a workgroup, four a
-// thread (4096 x 50001 bf16: 162 us; 512 chunks 187, 2048 183).
-constexpr int kFewRows = 192, kLongRow = 1024;  // rows; chunks
+// Rows are cut where they are few and long, since that takes a second launch: loss and gradient in segments and by a workgroup a
+// row, bf16 16 x 32000 11.1 and 10.8 us, 16 x 65536 11.0 and 16.9, 64 x 131072 17.6 and 31.7, 150 x 65536 21.2 and 19.4; fp32 16
+// x 16384 10.3 and 7.8, 16 x 32000 10.4 and 10.7, 150 x 131072 46.7 and 43.2.  Into about 512 segments in all, each at least 512
+// chunks (16 x 131071 fp32 17.8 us; 256 segments 18.4, 2048 22.1).  The gradient alone takes 1024 chunks a workgroup, four a
+// thread (4096 x 50001 bf16 with ordinary stores: 162 us; 512 chunks 187, 2048 183).
+constexpr int kFewRows = 128, kLongRow = 4096, kLongRowF32 = 7500;  // rows; chunks
 constexpr int kGradSegment = 1024;
 struct DistillPlan {
     int segments, chunks_per_segment;
@@ -680,7 +682,7 @@ static DistillPlan distill_plan(int64_t m, int64_t v, int top, int chunk) {
     const int64_t chunks = ceil_div64(v, chunk);
     d.segments = 1;
     d.chunks_per_segment = (int)chunks;
-    if (m < kFewRows && chunks > kLongRow) {
+    if (m < kFewRows && chunks > (chunk == 4 ? kLongRowF32 : kLongRow)) {
         const int64_t want = ceil_div64(512, m), most = ceil_div64(chunks, 512);
         const int64_t s = want < most ? want : most;
         if (s > 1) {
