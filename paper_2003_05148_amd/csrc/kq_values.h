@@ -26,7 +26,8 @@ __device__ __forceinline__ float load_value_as(const void* base, int64_t at) {
     else return Act<TYPE == KQ_T_BF16>::lo(((const uint16_t*)base)[at]);
 }
 // 4-byte aligned pieces of a stream that is written once and not read soon: past the caches' normal ways
-// (fp32 weights of 4096 x 25088 rebuilt: 75 us, 131 us with ordinary stores).
+// (fp32 weights of 4096 x 25088 rebuilt: 75 us, 131 us with ordinary stores).  Only where a thread's values lie on their own
+// size: pieces of lines are slow that way (4096 x 25087: 134 us with ordinary stores, 182 streamed).
 __device__ __forceinline__ void stream_store(void* at, const unsigned* v, int words) {
     if (words == 4) {
         using u32x4_a4 = __attribute__((ext_vector_type(4), aligned(4))) unsigned;
@@ -45,7 +46,10 @@ __device__ __forceinline__ void store_values(void* base, int64_t at, const float
             unsigned h[N];
             __builtin_memcpy(h, v, 4 * N);
 #pragma unroll
-            for (int t = 0; t < N; t += 4) stream_store(o + t, h + t, 4);
+            for (int t = 0; t < N; t += 4) {
+                if (((uintptr_t)o & 15) == 0) stream_store(o + t, h + t, 4);
+                else __builtin_memcpy(o + t, h + t, 16);
+            }
         } else {
 #pragma unroll
             for (int t = 0; t < N; ++t)
@@ -57,7 +61,7 @@ __device__ __forceinline__ void store_values(void* base, int64_t at, const float
             unsigned h[N / 2];
 #pragma unroll
             for (int t = 0; t < N / 2; ++t) h[t] = Act<TYPE == KQ_T_BF16>::pack(v[2 * t], v[2 * t + 1]);
-            if (((uintptr_t)o & 3) == 0) stream_store(o, h, N / 2);
+            if (((uintptr_t)o & (2 * N - 1)) == 0) stream_store(o, h, N / 2);
             else __builtin_memcpy(o, h, 2 * N);
         } else {
 #pragma unroll
