@@ -134,7 +134,6 @@ struct BlockMatvecParams {
     int64_t ldy;
     float* part;             // partial sums [splits][m][n], or NULL
     int splits, blocks_per_split;
-    bool odd_rows;           // 16-bit rows of X that begin between two dwords
 };
 struct BlockMatvecPlan {
     int row_tiles, waves, splits, blocks_per_split;

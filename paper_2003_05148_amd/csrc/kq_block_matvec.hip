@@ -13,25 +13,26 @@
 
 namespace kq {
 
-// A lane's 32 columns of a block of a row of X: 16 from 16 q and 16 from 64 + 16 q, as they lie in memory.
+// A lane's 32 columns of a block of a row of X: 16 from 16 q and 16 from 64 + 16 q, as they lie in memory.  ODD: 16-bit rows that
+// begin between two dwords.
 using u32x4_a4 = __attribute__((ext_vector_type(4), aligned(4))) unsigned;
-template <int TYPE>
+template <int TYPE, bool ODD>
 struct XBlock {
     static constexpr int kRegs = TYPE == KQ_T_E4M3 ? 2 : TYPE == KQ_T_F32 ? 8 : 4;  // of 16 bytes
     static constexpr int kBytes = TYPE == KQ_T_E4M3 ? 1 : TYPE == KQ_T_F32 ? 4 : 2;
     u32x4 r[kRegs];
     unsigned e;   // KQ_T_E4M3: the exponent
-    __device__ __forceinline__ void load(const char* row, int b, int q, int64_t k, bool odd_rows) {
+    __device__ __forceinline__ void load(const char* row, int b, int q, int64_t k) {
         const int64_t c0 = (int64_t)b * kBlock + 16 * q;
-        if (!(TYPE == KQ_T_BF16 || TYPE == KQ_T_F16) || !odd_rows ? TYPE == KQ_T_E4M3 || c0 + 80 <= k : c0 + 80 < k) {
-            if (!(TYPE == KQ_T_BF16 || TYPE == KQ_T_F16) || !odd_rows) {
+        if (TYPE == KQ_T_E4M3 || c0 + 80 + ODD <= k) {
+            if constexpr (!ODD) {
 #pragma unroll
                 for (int i = 0; i < kRegs; ++i)
                     __builtin_memcpy(&r[i], row + (c0 + i / (kRegs / 2) * 64) * kBytes + i % (kRegs / 2) * 16, 16);
-            } else if constexpr (TYPE == KQ_T_BF16 || TYPE == KQ_T_F16) {
-                // Rows of an odd pitch begin between two dwords, where a 16-byte load takes several times as long: the first value
-                // alone, the others (and one more) from the next dword on, moved up (16 rows through 1000 x 1023: 5.5 us, 7.3
-                // without; but 5.6 and 4.6 where no row begins so).
+            } else {
+                // A 16-byte load takes several times as long there: the first value alone, the others (and one more) from the next
+                // dword on, moved up (16 rows through 1000 x 1023: 5.5 us, 7.3 without; but 5.6 and 4.6 where no row begins
+                // so).
                 const char* const at = row + c0 * 2;
                 const unsigned odd = (unsigned)(uintptr_t)at & 2u;
                 unsigned lead[2];
@@ -133,7 +134,7 @@ struct XBlock {
 };
 
 // RT: 16-row tiles of W a workgroup takes; they share what a wave does to X.
-template <int TYPE, int WAVES, int RT>
+template <int TYPE, int WAVES, int RT, bool ODD>
 __global__ __launch_bounds__(64 * WAVES) void block_matvec_kernel(const BlockMatvecParams p) {
     __shared__ f32x4 s_sum[RT * WAVES * 64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -149,7 +150,7 @@ __global__ __launch_bounds__(64 * WAVES) void block_matvec_kernel(const BlockMat
     const uint8_t* const w_exp = p.exps + (n0 >> 7) * blocks;
     const int xr0 = (int)blockIdx.z * 16 + r16;
     const int64_t xr = min(xr0, p.m - 1);
-    const char* const x_row = (const char*)p.X + xr * p.ldx * XBlock<TYPE>::kBytes;
+    const char* const x_row = (const char*)p.X + xr * p.ldx * XBlock<TYPE, ODD>::kBytes;
     const uint8_t* const x_exp = TYPE == KQ_T_E4M3 ? p.x_exps + xr * blocks : nullptr;
     f32x4 y[RT];
 #pragma unroll
@@ -158,7 +159,7 @@ __global__ __launch_bounds__(64 * WAVES) void block_matvec_kernel(const BlockMat
     struct Block {
         u32x4 w[RT][2];
         unsigned ew;
-        XBlock<TYPE> x;
+        XBlock<TYPE, ODD> x;
     };
     auto fetch = [&](Block& f, int b) {
 #pragma unroll
@@ -167,7 +168,7 @@ __global__ __launch_bounds__(64 * WAVES) void block_matvec_kernel(const BlockMat
             f.w[t][1] = *(const u32x4*)(w_row[t] + (int64_t)b * kBlock + 64);
         }
         f.ew = w_exp[b];
-        f.x.load(x_row, b, q, p.k, p.odd_rows);
+        f.x.load(x_row, b, q, p.k);
         if constexpr (TYPE == KQ_T_E4M3) f.x.e = x_exp[b];
     };
     Block next;
@@ -262,29 +263,31 @@ BlockMatvecPlan block_matvec_plan(int x_type, int m, int64_t n, int64_t k) {
     return v;
 }
 
-template <int TYPE>
+template <int TYPE, bool ODD = false>
 static void launch_matvec_type(const BlockMatvecPlan& v, const BlockMatvecParams& p, hipStream_t s) {
     const dim3 grid((unsigned)ceil_div64(p.n, 16 * v.row_tiles), (unsigned)p.splits, (unsigned)ceil_div64(p.m, 16)), block(64 * v.waves);
     if (v.row_tiles == 4) {
-        block_matvec_kernel<TYPE, 4, 4><<<grid, block, 0, s>>>(p);
+        block_matvec_kernel<TYPE, 4, 4, ODD><<<grid, block, 0, s>>>(p);
     } else if (v.row_tiles == 2) {
-        if (v.waves == 8) block_matvec_kernel<TYPE, 8, 2><<<grid, block, 0, s>>>(p);
-        else block_matvec_kernel<TYPE, 4, 2><<<grid, block, 0, s>>>(p);
+        if (v.waves == 8) block_matvec_kernel<TYPE, 8, 2, ODD><<<grid, block, 0, s>>>(p);
+        else block_matvec_kernel<TYPE, 4, 2, ODD><<<grid, block, 0, s>>>(p);
     } else {
-        if (v.waves == 16) block_matvec_kernel<TYPE, 16, 1><<<grid, block, 0, s>>>(p);
-        else if (v.waves == 8) block_matvec_kernel<TYPE, 8, 1><<<grid, block, 0, s>>>(p);
-        else block_matvec_kernel<TYPE, 4, 1><<<grid, block, 0, s>>>(p);
+        if (v.waves == 16) block_matvec_kernel<TYPE, 16, 1, ODD><<<grid, block, 0, s>>>(p);
+        else if (v.waves == 8) block_matvec_kernel<TYPE, 8, 1, ODD><<<grid, block, 0, s>>>(p);
+        else block_matvec_kernel<TYPE, 4, 1, ODD><<<grid, block, 0, s>>>(p);
     }
 }
 
 hipError_t launch_block_matvec(const BlockMatvecPlan& plan, BlockMatvecParams p, hipStream_t s) {
     p.splits = plan.splits;
     p.blocks_per_split = plan.blocks_per_split;
-    p.odd_rows = (p.x_type == KQ_T_BF16 || p.x_type == KQ_T_F16) && (((uintptr_t)p.X & 2) || (p.m > 1 && (p.ldx & 1)));
+    const bool odd = ((uintptr_t)p.X & 2) || (p.m > 1 && (p.ldx & 1));
     if (p.splits == 1) p.part = nullptr;
     if (p.x_type == KQ_T_E4M3) launch_matvec_type<KQ_T_E4M3>(plan, p, s);
     else if (p.x_type == KQ_T_F32) launch_matvec_type<KQ_T_F32>(plan, p, s);
+    else if (p.x_type == KQ_T_BF16 && odd) launch_matvec_type<KQ_T_BF16, true>(plan, p, s);
     else if (p.x_type == KQ_T_BF16) launch_matvec_type<KQ_T_BF16>(plan, p, s);
+    else if (odd) launch_matvec_type<KQ_T_F16, true>(plan, p, s);
     else launch_matvec_type<KQ_T_F16>(plan, p, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
