@@ -756,6 +756,9 @@ kq_status kq_block_linear_grad_weight(const void* dY, int32_t type, int64_t ldy,
  *   exp((z - largest) / T) and that of exp(z - largest) (0 where it is not needed).
  * kq_distill_grad -- dZ (may be Z) from the same inputs, stats and dloss (device [m] fp32, or NULL for `scale`).
  *   Sums in fp32, in an order that the call, the sizes, the weights of the terms and the alignment of Z's rows decide.
+ *   The loss' first term is off by a few 2^-24 of (1 - alpha) T^2 (1 + log v).  Above T = 4 it is off by a few 2^-24 of itself
+ *   and of the logits' range times its root, however large T is, where the entries are all classes of the row that are not
+ *   masked out; where other classes hold more than 2^-20 of the sum of exp(z / T), by a few 2^-24 of itself over that share.
  *   workspace: kq_distill_workspace_bytes(type, m, v, top) (may be 0).
  */
 #define KQ_DISTILL_MAX_CLASSES (1 << 24)

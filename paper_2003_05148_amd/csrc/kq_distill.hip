@@ -210,13 +210,29 @@ struct __attribute__((aligned(16))) TopEntries {
     float t[KQ_DISTILL_MAX_TOP];   // teacher's logit less its largest
     float p[KQ_DISTILL_MAX_TOP];   // 0 for absent ones
     float z[KQ_DISTILL_MAX_TOP];   // the network's own logit there
+    float row[8];                  // the row's sums and Teacher, where registers hold the row in between
 };
 __device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
+// Above this temperature the divergence of p and q that are close is taken in a way of its own.  Up to it T^2 times the
+// rounding of a plain sum is 10^-5 at most, and that way costs 0.4 to 1 us (64 x 1000 bf16 6.3 and 7.3 us, the loss alone of 4096
+// x 32000 47.6 and 51.7).
+constexpr float kCloseFrom = 4.0f;
 
 struct Teacher {
     float St;         // sum of exp(t / T); 0 without a present entry
     int label;        // -1: absent
     float zy;         // the network's logit there
+    __device__ __forceinline__ void keep(float* at) const {
+        at[0] = St;
+        at[1] = __builtin_bit_cast(float, label);
+        at[2] = zy;
+    }
+    __device__ __forceinline__ void take(const float* at) {
+        St = at[0];
+        label = __builtin_bit_cast(int, at[1]);
+        zy = at[2];
+    }
     // reads z at the entries and the label
     template <int TYPE>
     __device__ __forceinline__ void init(const DistillParams& p, const Row<TYPE>& r, TopEntries& s, int64_t row, int lane, const Exponential& eT) {
@@ -259,8 +275,44 @@ struct Teacher {
         for (int j = lane; j < p.top; j += 64) s.p[j] = s.idx[j] >= 0 ? s.p[j] * inv : 0.0f;
         wave_fence();
     }
+    // The divergence sum p (log p - log q) of p and q that are close (large temperatures, a network near its teacher), where
+    // the sum of logarithms is a small difference of large terms and T^2 would multiply its rounding (100 classes, all of them
+    // entries, T = 1024: 0.0055 for 0.4400).  With x_j = (t_j - z_j) / T less its mean under p,
+    //   S_T / S_t e^mean = 1 + sum p_j (e^-x_j - 1 + x_j) + rest e^mean / S_t,
+    // and the divergence is the logarithm of that: no term is below zero but for classes that stand twice, so nothing
+    // cancels.  rest, of the classes that are no entries, is itself a difference of sums: below 2^-20 of S_T it may be
+    // nothing but their rounding and counts as zero.
+    __device__ __forceinline__ float close_divergence(const DistillParams& p, const TopEntries& s, int lane, const Sums& r, const Exponential& eT, float invT) const {
+        float mean = 0.0f;
+        for (int j = lane; j < p.top; j += 64)
+            if (s.idx[j] >= 0 && s.p[j] != 0.0f) mean += s.p[j] * ((s.t[j] - (s.z[j] - r.M)) * invT);
+        mean = wave_sum(mean);
+        const float shift = Exponential{p.e1_hi, p.e1_lo}(mean) / St;
+        float more = 0.0f, inside = 0.0f;
+        for (int j = lane; j < p.top; j += 64) {
+            const float pj = s.p[j];
+            if (s.idx[j] < 0 || pj == 0.0f) continue;
+            const float d = s.z[j] - r.M, e = eT(d), x = (s.t[j] - d) * invT - mean;
+            inside += e;
+            more += __builtin_fabsf(x) < 1.0f ? pj * above_tangent(x) : e * shift + pj * (x - 1.0f);
+        }
+        more = wave_sum(more);
+        const float rest = r.sT - wave_sum(inside);
+        if (__builtin_fabsf(rest) > 0x1p-20f * r.sT) more += rest * shift;
+        // log(1 + y) for |y| < 0.3 as 2 artanh(y / (2 + y))
+        const float y = more / (2.0f + more), y2 = y * y;
+        return 2.0f * y * (1.0f + y2 * (1.0f / 3 + y2 * (1.0f / 5 + y2 * (1.0f / 7 + y2 * (1.0f / 9)))));
+    }
+    // e^-x - 1 + x for |x| < 1, by its power series (the first term left out is below 2^-27 of it)
+    static __device__ __forceinline__ float above_tangent(float x) {
+        constexpr float c[] = {1.0f / 2, -1.0f / 6, 1.0f / 24, -1.0f / 120, 1.0f / 720, -1.0f / 5040, 1.0f / 40320, -1.0f / 362880, 1.0f / 3628800, -1.0f / 39916800};
+        float y = c[9];
+#pragma unroll
+        for (int i = 8; i >= 0; --i) y = __builtin_fmaf(y, x, c[i]);
+        return y * x * x;
+    }
     // the row's loss, in every lane
-    __device__ __forceinline__ float loss(const DistillParams& p, const TopEntries& s, int lane, const Sums& r) const {
+    __device__ __forceinline__ float loss(const DistillParams& p, const TopEntries& s, int lane, const Sums& r, const Exponential& eT) const {
         float sum = 0.0f;
         if (St != 0.0f) {  // (also where it is NaN)
             const float lse = logf(r.sT) - logf(St), invT = 1.0f / p.T;
@@ -268,7 +320,9 @@ struct Teacher {
                 const float pj = s.p[j];
                 if (s.idx[j] >= 0 && pj != 0.0f) sum += pj * ((s.t[j] - (s.z[j] - r.M)) * invT + lse);
             }
-            sum = wave_sum(sum) * ((1.0f - p.alpha) * p.T * p.T);
+            sum = wave_sum(sum);
+            if (p.T > kCloseFrom && __builtin_fabsf(sum) < 0.25f) sum = close_divergence(p, s, lane, r, eT, invT);
+            sum *= (1.0f - p.alpha) * p.T * p.T;
         }
         return label >= 0 ? sum + p.alpha * (logf(r.s1) - (zy - r.M)) : sum;
     }
@@ -438,6 +492,9 @@ template <int TYPE, int CH, int WAVES, bool LOSS, bool GRAD>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, WAVES == 16 ? (CH > 8 ? 4 : 8) : 1) void distill_row_kernel(const DistillParams p) {
     constexpr int NT = 64 * WAVES;
     constexpr int kHeld = CH ? CH : 1;
+    // Of many chunks the loss comes after the dense stores, when no registers hold them and the stores are on their way (before
+    // them it took up to 4 registers more than 8 waves a SIMD have); of few before (64 x 1000 bf16 0.1 us less).
+    constexpr bool kLate = LOSS && GRAD && CH >= 8;
     __shared__ float s_red[3][WAVES];
     __shared__ float s_row[2];
     __shared__ TopEntries s_top[WAVES == 1 ? 4 : 1];
@@ -495,8 +552,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, WAVES == 16 ? (CH > 
         add_single(s, x1, two, eT, e1);
         s = join_sums<WAVES>(s, s_red, wave, two, eT, e1);
         if (!two) s.s1 = ce ? s.sT : 0.0f;
-        if (leader) {
-            const float loss = te.loss(p, entries, lane, s);
+        if (!kLate && leader) {
+            const float loss = te.loss(p, entries, lane, s, eT);
             if (lane == 0) {
                 p.loss[row] = loss;
                 if (p.stats) {
@@ -505,6 +562,14 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, WAVES == 16 ? (CH > 
                     p.stats[3 * row + 2] = s.s1;
                 }
             }
+        }
+    }
+    if constexpr (kLate) {
+        if (leader && lane == 0) {
+            entries.row[0] = s.M;
+            entries.row[1] = s.sT;
+            entries.row[2] = s.s1;
+            te.keep(entries.row + 3);
         }
     }
     if constexpr (GRAD) {
@@ -524,6 +589,13 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, WAVES == 16 ? (CH > 
             }
         }
         if (single >= 0) store_one<TYPE>(out, single, d.of(x1));
+        if (kLate && leader) {
+            wave_fence();
+            const Sums own = {entries.row[0], entries.row[1], entries.row[2]};
+            te.take(entries.row + 3);
+            const float loss = te.loss(p, entries, lane, own, eT);
+            if (lane == 0) p.loss[row] = loss;
+        }
         __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the dense stores have ended
         if constexpr (WAVES > 1) __syncthreads();
         else wave_fence();
@@ -632,7 +704,7 @@ __global__ __launch_bounds__(256) void distill_segment_kernel(const DistillParam
         s.s1 = two ? wave_sum(s.s1) : ce ? s.sT : 0.0f;
     }
     if (p.loss && segment == 0 && wave == 0) {
-        const float loss = te.loss(p, entries, lane, s);
+        const float loss = te.loss(p, entries, lane, s, eT);
         if (lane == 0) {
             p.loss[row] = loss;
             if (p.stats) {
