@@ -759,6 +759,8 @@ kq_status kq_block_linear_grad_weight(const void* dY, int32_t type, int64_t ldy,
  *   The loss' first term is off by a few 2^-24 of (1 - alpha) T^2 (1 + log v).  Above T = 4 it is off by a few 2^-24 of itself
  *   and of the logits' range times its root, however large T is, where the entries are all classes of the row that are not
  *   masked out; where other classes hold more than 2^-20 of the sum of exp(z / T), by a few 2^-24 of itself over that share.
+ *   The gradient at the entries is off by a few 2^-24 of d (1 - alpha) T (q + p); above T = 4 and of such rows of itself and of p
+ *   times the logits' range (but for kq_distill_grad of rows of more than 8 KB).
  *   workspace: kq_distill_workspace_bytes(type, m, v, top) (may be 0).
  */
 #define KQ_DISTILL_MAX_CLASSES (1 << 24)

@@ -207,7 +207,7 @@ __device__ __forceinline__ Sums join_sums(Sums s, float (*s_red)[WAVES], int wav
 // ---- the teacher's entries of a row and its label, by one wave ------------------------------------------------------
 struct __attribute__((aligned(16))) TopEntries {
     int idx[KQ_DISTILL_MAX_TOP];   // -1: absent (and behind the last, up to a multiple of 8)
-    float t[KQ_DISTILL_MAX_TOP];   // teacher's logit less its largest
+    float t[KQ_DISTILL_MAX_TOP];   // teacher's logit less its largest; of a close row q - p from its divergence on
     float p[KQ_DISTILL_MAX_TOP];   // 0 for absent ones
     float z[KQ_DISTILL_MAX_TOP];   // the network's own logit there
     float row[8];                  // the row's sums and Teacher, where registers hold the row in between
@@ -281,8 +281,9 @@ struct Teacher {
     //   S_T / S_t e^mean = 1 + sum p_j (e^-x_j - 1 + x_j) + rest e^mean / S_t,
     // and the divergence is the logarithm of that: no term is below zero but for classes that stand twice, so nothing
     // cancels.  rest, of the classes that are no entries, is itself a difference of sums: below 2^-20 of S_T it may be
-    // nothing but their rounding and counts as zero.
-    __device__ __forceinline__ float close_divergence(const DistillParams& p, const TopEntries& s, int lane, const Sums& r, const Exponential& eT, float invT) const {
+    // nothing but their rounding and counts as zero.  The gradient's q - p = p (e^-x S_t e^-mean / S_T - 1) is taken of the
+    // same (100 classes, T = 2^20: T q - T p is 10 % off).
+    __device__ __forceinline__ float close_divergence(const DistillParams& p, TopEntries& s, int lane, const Sums& r, const Exponential& eT, float invT) const {
         float mean = 0.0f;
         for (int j = lane; j < p.top; j += 64)
             if (s.idx[j] >= 0 && s.p[j] != 0.0f) mean += s.p[j] * ((s.t[j] - (s.z[j] - r.M)) * invT);
@@ -299,6 +300,11 @@ struct Teacher {
         more = wave_sum(more);
         const float rest = r.sT - wave_sum(inside);
         if (__builtin_fabsf(rest) > 0x1p-20f * r.sT) more += rest * shift;
+        for (int j = lane; j < p.top; j += 64) {
+            const float pj = s.p[j], d = s.z[j] - r.M, x = (s.t[j] - d) * invT - mean;
+            s.t[j] = pj != 0.0f && __builtin_fabsf(x) < 1.0f ? pj * (above_tangent(x) - x - more) / (1.0f + more) : eT(d) / r.sT - pj;
+        }
+        wave_fence();
         // log(1 + y) for |y| < 0.3 as 2 artanh(y / (2 + y))
         const float y = more / (2.0f + more), y2 = y * y;
         return 2.0f * y * (1.0f + y2 * (1.0f / 3 + y2 * (1.0f / 5 + y2 * (1.0f / 7 + y2 * (1.0f / 9)))));
@@ -311,8 +317,9 @@ struct Teacher {
         for (int i = 8; i >= 0; --i) y = __builtin_fmaf(y, x, c[i]);
         return y * x * x;
     }
-    // the row's loss, in every lane
-    __device__ __forceinline__ float loss(const DistillParams& p, const TopEntries& s, int lane, const Sums& r, const Exponential& eT) const {
+    // sum p (log p - log q), in every lane; 0 without a present entry.  close: the entries' t is q - p now.
+    __device__ __forceinline__ float divergence(const DistillParams& p, TopEntries& s, int lane, const Sums& r, const Exponential& eT, bool& close) const {
+        close = false;
         float sum = 0.0f;
         if (St != 0.0f) {  // (also where it is NaN)
             const float lse = logf(r.sT) - logf(St), invT = 1.0f / p.T;
@@ -321,9 +328,14 @@ struct Teacher {
                 if (s.idx[j] >= 0 && pj != 0.0f) sum += pj * ((s.t[j] - (s.z[j] - r.M)) * invT + lse);
             }
             sum = wave_sum(sum);
-            if (p.T > kCloseFrom && __builtin_fabsf(sum) < 0.25f) sum = close_divergence(p, s, lane, r, eT, invT);
-            sum *= (1.0f - p.alpha) * p.T * p.T;
+            close = p.T > kCloseFrom && __builtin_fabsf(sum) < 0.25f;
+            if (close) sum = close_divergence(p, s, lane, r, eT, invT);
         }
+        return sum;
+    }
+    // the row's loss, in every lane
+    __device__ __forceinline__ float loss(const DistillParams& p, TopEntries& s, int lane, const Sums& r, const Exponential& eT, bool& close) const {
+        const float sum = divergence(p, s, lane, r, eT, close) * ((1.0f - p.alpha) * p.T * p.T);
         return label >= 0 ? sum + p.alpha * (logf(r.s1) - (zy - r.M)) : sum;
     }
 };
@@ -413,7 +425,7 @@ struct Dense {
 // than once is written by its first place, with all of its p, in order.
 template <int TYPE>
 __device__ __forceinline__ void write_exceptions(const DistillParams& p, const TopEntries& s, char* out, int lane, int label, float zy,
-                                                 const Dense& d, int c_begin, int c_end) {
+                                                 const Dense& d, bool close, int c_begin, int c_end) {
     bool hit = false;
     if (p.alpha < 1.0f) {
         for (int j0 = 0; j0 < p.top; j0 += 64) {
@@ -435,7 +447,9 @@ __device__ __forceinline__ void write_exceptions(const DistillParams& p, const T
                     first = first && !(same && o + u < j);
                 }
             }
-            if (first) store_one<TYPE>(out, own, d.of(s.z[j]) - d.f.wT * sum - (own == label ? d.f.w1 : 0.0f));
+            if (!first) continue;
+            const float g = close ? d.f.wT * (s.t[j] - (sum - s.p[j])) + d.f.f1 * d.e1(s.z[j] - d.M) : d.of(s.z[j]) - d.f.wT * sum;
+            store_one<TYPE>(out, own, g - (own == label ? d.f.w1 : 0.0f));
         }
     }
     if (__builtin_amdgcn_ballot_w64(hit) == 0 && lane == 0 && label >= c_begin && label < c_end)
@@ -517,6 +531,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, WAVES == 16 ? (CH > 
     const int single = r.single(tid);
     const float x1 = single >= 0 ? r.at(single) : -__builtin_inff();
     Teacher te;
+    bool close = false;
     if (leader) te.init<TYPE>(p, r, entries, row, lane, eT);
     if (WAVES > 1 && wave == 0) __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): what was read of Z is here before it may be written
     if (WAVES > 1 && threadIdx.x == 0) {
@@ -553,7 +568,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, WAVES == 16 ? (CH > 
         s = join_sums<WAVES>(s, s_red, wave, two, eT, e1);
         if (!two) s.s1 = ce ? s.sT : 0.0f;
         if (!kLate && leader) {
-            const float loss = te.loss(p, entries, lane, s, eT);
+            const float loss = te.loss(p, entries, lane, s, eT, close);
             if (lane == 0) {
                 p.loss[row] = loss;
                 if (p.stats) {
@@ -593,13 +608,14 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, WAVES == 16 ? (CH > 
             wave_fence();
             const Sums own = {entries.row[0], entries.row[1], entries.row[2]};
             te.take(entries.row + 3);
-            const float loss = te.loss(p, entries, lane, own, eT);
+            const float loss = te.loss(p, entries, lane, own, eT, close);
             if (lane == 0) p.loss[row] = loss;
         }
         __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the dense stores have ended
         if constexpr (WAVES > 1) __syncthreads();
         else wave_fence();
-        if (leader) write_exceptions<TYPE>(p, entries, out, lane, label, te.zy, d, 0, p.v);
+        if (!LOSS && p.T > kCloseFrom) te.divergence(p, entries, lane, s, eT, close);  // (one wave a row)
+        if (leader) write_exceptions<TYPE>(p, entries, out, lane, label, te.zy, d, close, 0, p.v);
     }
 }
 
@@ -703,9 +719,11 @@ __global__ __launch_bounds__(256) void distill_segment_kernel(const DistillParam
         s.sT = wave_sum(s.sT);
         s.s1 = two ? wave_sum(s.s1) : ce ? s.sT : 0.0f;
     }
-    if (p.loss && segment == 0 && wave == 0) {
-        const float loss = te.loss(p, entries, lane, s, eT);
-        if (lane == 0) {
+    // (Of the gradient alone the logits of classes in other segments may be gone: no row is close there.)
+    bool close = false;
+    if (p.loss && wave == 0 && (segment == 0 || p.T > kCloseFrom)) {
+        const float loss = te.loss(p, entries, lane, s, eT, close);
+        if (segment == 0 && lane == 0) {
             p.loss[row] = loss;
             if (p.stats) {
                 p.stats[3 * row] = s.M;
@@ -729,10 +747,11 @@ __global__ __launch_bounds__(256) void distill_segment_kernel(const DistillParam
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the dense stores have ended
     __syncthreads();
     if (wave == 0) {
-        write_exceptions<TYPE>(p, entries, out, lane, te.label, te.zy, d, r.head + c_begin * N, r.head + c_end * N);
-        if (segment == 0) {
-            write_exceptions<TYPE>(p, entries, out, lane, te.label, te.zy, d, 0, r.head);
-            write_exceptions<TYPE>(p, entries, out, lane, te.label, te.zy, d, r.head + r.chunks * N, p.v);
+        // (the first segment's single values: before its chunks and behind the last)
+#pragma unroll 1
+        for (int i = 0; i < (segment == 0 ? 3 : 1); ++i) {
+            const int from = i == 0 ? r.head + c_begin * N : i == 1 ? 0 : r.head + r.chunks * N;
+            write_exceptions<TYPE>(p, entries, out, lane, te.label, te.zy, d, close, from, i == 0 ? r.head + c_end * N : i == 1 ? r.head : p.v);
         }
     }
 }

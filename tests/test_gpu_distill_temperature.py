@@ -11,6 +11,12 @@ loss is T^2 sum p (e^-x - 1 + x) (its logarithm changes nothing but for large x)
 1.72 |x| p T^2 for |x| <= 1: 16 A eps 1.72 T sum p |x| <= 28 A eps sqrt(2 L 1.4) with L the loss itself, since
 x^2 / 2 <= 1.4 (e^-x - 1 + x).  The p_j are off by (3 A / T log2 e + 16) eps of themselves, sums of at most 256 terms by 16
 eps more: 2 (16 + 16 + 5 A / T) eps L.  In all 32 eps (1.5 A sqrt(L) + (2 + A / T) L).
+
+Tolerance of the gradient T (q - p) = T p ((e^-x - 1) - y) / (1 + y), y what the logarithm above is taken of: x's five roundings
+are 5 A eps / T, the mean's as many and 32 eps A / T for those of the p; T p times that, times e^|x| / (1 + y) <= 1.4
+where T is above 4 and x is small, is below 64 A eps p.  p, y and the other factors are off by at most 64 eps of the result.  Then
+half a step of dz's type.  kq_distill_grad of rows of more than 512 chunks of 16 bytes takes q - p as it stands: 64 + 8 A / T +
+v / 32 eps of T (q + p) (tests/test_gpu_distill.py).
 """
 import numpy as np
 import pytest
@@ -59,6 +65,21 @@ def near(loss, want, A, T, weight=1.0):
     assert np.all(np.abs(got - want) <= tol), (got, want, tol)
 
 
+U = {BF: 2.0 ** -8, HF: 2.0 ** -11, F32: 2.0 ** -24}
+TINY = {BF: 2.0 ** -126, HF: 2.0 ** -25, F32: 2.0 ** -126}
+
+
+def near_gradient(dz, Z, idx, less, p, A, T, d, plain=False):
+    """less: p - q at the entries.  Masked classes have no gradient at all."""
+    assert torch.all(dz.cpu()[torch.isinf(Z)] == 0)
+    got = dz.double().cpu().gather(1, idx).numpy().astype(np.longdouble)
+    want, A = -d * np.longdouble(T) * less, A[:, None]
+    tol = EPS * (64 * A * p * d + 64 * np.abs(want)) + U[dz.dtype] * np.abs(want) + TINY[dz.dtype]
+    if plain:
+        tol = tol + EPS * (64 + 8 * A / T + Z.shape[1] / 32) * d * T * (2 * p - less)
+    assert np.all(np.abs(got - want) <= tol), (np.abs(got - want) / tol).max()
+
+
 TEMPERATURES = [4.25, 7.0, 20.0, 100.0, 1024.0, 2.0 ** 20]
 SIZES = [(5, 10, 10), (5, 100, 100), (3, 256, 256), (9, 1000, 100), (5, 3000, 256), (5, 9001, 60), (4, 20000, 100), (3, 33000, 7),
          (3, 70001, 100), (130, 70001, 50), (130, 140001, 30)]
@@ -78,6 +99,58 @@ def test_loss_of_rows_whose_classes_are_all_entries(m, v, top, T):
         near(kq.kq_distill_loss(z, tv, ti, T)[0], loss, A, T)
         inplace = z.clone()
         near(kq.kq_distill(inplace, tv, ti, temperature=T, dZ=inplace)[0], loss, A, T)
+
+
+@pytest.mark.parametrize("T", TEMPERATURES)
+@pytest.mark.parametrize("m,v,top", SIZES)
+def test_gradient_of_rows_whose_classes_are_all_entries(m, v, top, T):
+    for dtype in (F32, HF, BF) if v < 100000 else (F32,):
+        Z, t, idx = rows(m, v, top, dtype, v + top + 1, noise=1.0 if T > 5 else 0.02)
+        _, less, p, A = exact(Z, t, idx, T)
+        z, tv, ti = Z.to(DEV), t.to(DEV), idx.to(DEV)
+        near_gradient(kq.kq_distill(z, tv, ti, temperature=T, scale=0.5)[1], Z, idx, less, p, A, T, 0.5)
+        stats = kq.kq_distill_loss(z, tv, ti, T)[1]
+        plain = v // (4 if dtype == F32 else 8) > 512
+        near_gradient(kq.kq_distill_grad(z, tv, ti, stats, None, T, scale=0.5), Z, idx, less, p, A, T, 0.5, plain)
+        inplace = z.clone()
+        kq.kq_distill(inplace, tv, ti, temperature=T, scale=0.5, dZ=inplace)
+        near_gradient(inplace, Z, idx, less, p, A, T, 0.5)
+
+
+@pytest.mark.parametrize("T", [20.0, 2.0 ** 20])
+def test_gradient_of_classes_that_stand_twice_and_labels(T):
+    """The label's term is added to a close row's, and an entry that stands twice has both its p.  The sum of the entries'
+    exponentials passes S_T by one class then: the difference of two sums of at most 91 terms, each off by at most 64 eps of
+    itself, is 128 eps S_T of y more, and 128 eps T p of the gradient."""
+    m, v, alpha = 6, 90, 0.25
+    Z, t, idx = rows(m, v, v, F32, 4)
+    labels = idx[:, 7].contiguous()
+    t2, idx2 = torch.cat([t, t[:, 5:6]], 1), torch.cat([idx, idx[:, 5:6]], 1)
+    w = t2.double().numpy().astype(np.longdouble) / np.longdouble(T)
+    p2 = np.exp(w - w.max(1, keepdims=True))
+    p2 /= p2.sum(1, keepdims=True)
+    u = Z.double().numpy().astype(np.longdouble)
+    A = np.maximum(np.ptp(t.numpy(), 1), np.ptp(u, 1)).astype(np.longdouble)[:, None]
+
+    def soft(x):
+        e = np.exp(x - x.max(1, keepdims=True))
+        return e / e.sum(1, keepdims=True)
+    want = (1 - alpha) * np.longdouble(T) * soft(u / np.longdouble(T))
+    s = soft(u)
+    for r in range(m):
+        for j in range(v + 1):
+            want[r, int(idx2[r, j])] -= (1 - alpha) * np.longdouble(T) * p2[r, j]
+        want[r] += alpha * s[r]
+        want[r, int(labels[r])] -= alpha
+    z, tv, ti, y = Z.to(DEV), t2.to(DEV), idx2.to(DEV), labels.to(DEV)
+    stats = kq.kq_distill_loss(z, tv, ti, T, y, alpha)[1]
+    for dz in (kq.kq_distill(z, tv, ti, temperature=T, labels=y, alpha=alpha)[1], kq.kq_distill_grad(z, tv, ti, stats, None, T, y, alpha)):
+        got = dz.double().cpu().numpy().astype(np.longdouble)
+        p = soft(t.double().numpy().astype(np.longdouble) / np.longdouble(T))
+        byclass = np.zeros_like(p)
+        np.put_along_axis(byclass, idx.numpy(), p, 1)
+        tol = EPS * (64 * A * byclass + 128 * T * byclass + 64 * np.abs(want) + 64 * alpha * (s + 1))
+        assert np.all(np.abs(got - want) <= tol), (np.abs(got - want) / tol).max()
 
 
 @pytest.mark.parametrize("T", [20.0, 2.0 ** 20])
