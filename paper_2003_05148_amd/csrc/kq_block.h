@@ -144,4 +144,13 @@ BlockMatvecPlan block_matvec_plan(int m, int64_t n, int64_t k);              // 
 BlockMatvecPlan block_matvec_plan(int x_type, int m, int64_t n, int64_t k);  // more of them
 hipError_t launch_block_matvec(const BlockMatvecPlan& plan, BlockMatvecParams p, hipStream_t s);
 
+// What kq_block_linear of a size takes, and its workspace.
+struct BlockLinearPlan {
+    bool few;
+    BlockMatvecPlan few_plan;
+    BlockGemmPlan plan;
+    size_t x, x_exps, total;  // X quantized, where it is not already
+};
+BlockLinearPlan block_linear_plan(int x_type, int y_type, int64_t m, int64_t n, int64_t k);
+
 }  // namespace kq

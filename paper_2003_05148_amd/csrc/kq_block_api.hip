@@ -44,31 +44,6 @@ struct Regions {
     }
 };
 
-// Few rows are multiplied row by row of W, others in large tiles: up to 16 the former is always the faster, beyond the two plans'
-// modelled times decide (the quantizer's launch takes 2.8 us, of fp32 4.2).
-struct LinearSizes {
-    bool few;
-    BlockMatvecPlan few_plan = {};
-    BlockGemmPlan plan = {};
-    size_t x = 0, x_exps = 0, total;  // X quantized, where it is not already
-    LinearSizes(int32_t x_type, int32_t y_type, int64_t m, int64_t n, int64_t k) {
-        few = m <= kBlockMatvecRows;
-        if (few) {
-            few_plan = block_matvec_plan((int)m, n, k);
-        } else {
-            plan = block_gemm_plan(y_type == KQ_T_F32, n, m, k);
-            if (m <= kBlockMatvecMost) {
-                few_plan = block_matvec_plan(x_type, (int)m, n, k);
-                few = few_plan.us < plan.us + (x_type == KQ_T_E4M3 ? 0.0f : x_type == KQ_T_F32 ? 4.2f : 2.8f);
-            }
-        }
-        total = few_plan.ws_bytes;
-        if (few) return;
-        x = x_type == KQ_T_E4M3 ? 0 : region(m * block_pitch(k));
-        x_exps = x_type == KQ_T_E4M3 ? 0 : region(m * (block_pitch(k) / kBlock));
-        total = plan.part_bytes + x + x_exps;
-    }
-};
 struct GradInputSizes {
     BlockGemmPlan plan;
     size_t dy, dy_exps, total;
@@ -101,6 +76,32 @@ struct GradWeightSizes {
 
 }  // namespace
 
+namespace kq {
+
+// Few rows are multiplied row by row of W, others in large tiles: up to 16 the former is always the faster, beyond the two plans'
+// modelled times decide (the quantizer's launch takes 2.8 us, of fp32 4.2).
+BlockLinearPlan block_linear_plan(int x_type, int y_type, int64_t m, int64_t n, int64_t k) {
+    BlockLinearPlan z = {};
+    z.few = m <= kBlockMatvecRows;
+    if (z.few) {
+        z.few_plan = block_matvec_plan((int)m, n, k);
+    } else {
+        z.plan = block_gemm_plan(y_type == KQ_T_F32, n, m, k);
+        if (m <= kBlockMatvecMost) {
+            z.few_plan = block_matvec_plan(x_type, (int)m, n, k);
+            z.few = z.few_plan.us < z.plan.us + (x_type == KQ_T_E4M3 ? 0.0f : x_type == KQ_T_F32 ? 4.2f : 2.8f);
+        }
+    }
+    z.total = z.few_plan.ws_bytes;
+    if (z.few) return z;
+    z.x = x_type == KQ_T_E4M3 ? 0 : region(m * block_pitch(k));
+    z.x_exps = x_type == KQ_T_E4M3 ? 0 : region(m * (block_pitch(k) / kBlock));
+    z.total = z.plan.part_bytes + z.x + z.x_exps;
+    return z;
+}
+
+}  // namespace kq
+
 extern "C" {
 
 kq_status kq_quantize_blocks(const void* X, int32_t type, int64_t ldx, int64_t m, int64_t k, int32_t rows, uint8_t* values,
@@ -127,7 +128,7 @@ kq_status kq_reconstruct_blocks(const uint8_t* values, const uint8_t* exps, int6
 
 size_t kq_block_linear_workspace_bytes(int32_t x_type, int32_t y_type, int64_t m, int64_t n, int64_t k) {
     if (m < 1 || check_layer(m, n, k) != KQ_OK || !(plain_type(x_type) || x_type == KQ_T_E4M3) || !plain_type(y_type)) return 0;
-    return LinearSizes(x_type, y_type, m, n, k).total;
+    return block_linear_plan(x_type, y_type, m, n, k).total;
 }
 
 kq_status kq_block_linear(const void* X, int32_t x_type, int64_t ldx, const uint8_t* x_exps, int64_t m, int64_t n, int64_t k,
@@ -144,7 +145,7 @@ kq_status kq_block_linear(const void* X, int32_t x_type, int64_t ldx, const uint
         return KQ_ERR_ARG;
     if (!valid_tensor(Y, y_type, ldy, n)) return KQ_ERR_ARG;
     const hipStream_t s = (hipStream_t)stream;
-    const LinearSizes z(x_type, y_type, m, n, k);
+    const BlockLinearPlan z = block_linear_plan(x_type, y_type, m, n, k);
     if ((st = check_ws(ws, ws_bytes, z.total)) != KQ_OK) return st;
     if (z.few) {
         const BlockMatvecParams p = {values, exps, n, k, kp, X, x_type, ldx, x_exps, (int)m, bias, Y, y_type, ldy,
