@@ -1,5 +1,6 @@
 """kq_block_linear in tiles (more than 1024 rows, or products too large to go row by row of W), in every tile and kind of plan:
-whole and split contractions, the last columns in a tile of their own.  The sizes are those that tests/test_block_choice.py holds to their kernel.  Tolerances: those of tests/test_gpu_block_linear.py's
+whole and split contractions, the last columns in a tile of their own; and that few rows and small products are exact.  The
+sizes are those that tests/test_block_choice.py holds to their kernel.  Tolerances: those of tests/test_gpu_block_linear.py's
 head.
 """
 import math
@@ -9,7 +10,7 @@ import torch
 
 pytestmark = pytest.mark.gpu
 
-from test_block_choice import LARGE_TILES, TILES
+from test_block_choice import FEW, LARGE_TILES, TILES
 from test_gpu_block_linear import BF, DEV, F32, HF, TINY, U, acts, check, gen, hat, layer
 
 kq = pytest.importorskip("paper_2003_05148_amd")
@@ -218,3 +219,19 @@ def test_leading_sizes_layer_and_no_host_helper(monkeypatch):
     monkeypatch.setattr(kq, "_fast", None)
     for a, c in zip(want, calls()):
         assert a.dtype == c.dtype and torch.equal(a, c)
+
+
+# ---- few rows and small products ---------------------------------------------------------------------
+
+@pytest.mark.parametrize("m,n,k", FEW)
+def test_few_rows_and_small_products_are_exact(m, n, k):
+    """Whatever X's and the output's type: the tolerance without the 8-bit matrix instruction's."""
+    (values, exps), W = layer(n, k, m + n)
+    bias = torch.randn(n, generator=gen(n))
+    for dtype in (BF, HF, F32):
+        X = acts(m, k, dtype, m)
+        x, Xh = kq.kq_quantize_blocks(X.to(DEV)), hat(X, 1)
+        for out in (BF, HF, F32):
+            y = kq.kq_block_linear(X.to(DEV), values, exps, bias.to(DEV), dtype=out)
+            check(y, Xh, W, k, True, bias.double())
+            check(kq.kq_block_linear(x[0], values, exps, bias.to(DEV), x[1], dtype=out), Xh, W, k, True, bias.double())
