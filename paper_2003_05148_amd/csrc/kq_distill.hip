@@ -501,9 +501,10 @@ __device__ __forceinline__ void add_single(Sums& s, float x, bool two, const Exp
 
 // ---- a row in one workgroup or wave ------------------------------------------------------------------------------
 // CH chunks a thread in registers, WAVES waves a row (1: four rows a workgroup).  CH = 0: the row is read again.
-// LOSS, GRAD: what is asked for; the gradient alone takes a row's stats.
+// LOSS, GRAD: what is asked for; the gradient alone takes a row's stats, and a wave (longer rows: distill_segment_kernel).
 template <int TYPE, int CH, int WAVES, bool LOSS, bool GRAD>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, WAVES == 16 ? (CH > 8 ? 4 : 8) : 1) void distill_row_kernel(const DistillParams p) {
+    static_assert(LOSS || WAVES == 1, "the gradient alone");
     constexpr int NT = 64 * WAVES;
     constexpr int kHeld = CH ? CH : 1;
     // Of many chunks the loss comes after the dense stores, when no registers hold them and the stores are on their way (before
@@ -541,7 +542,6 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, WAVES == 16 ? (CH > 
     Sums s = {x1, 0.0f, 0.0f};
     if constexpr (!LOSS) {
         s = {p.part[3 * row], p.part[3 * row + 1], p.part[3 * row + 2]};
-        if constexpr (WAVES > 1) __syncthreads();  // (s_row)
     } else {
         if constexpr (CH > 0) {
 #pragma unroll
