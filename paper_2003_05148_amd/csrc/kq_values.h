@@ -26,8 +26,11 @@ __device__ __forceinline__ float load_value_as(const void* base, int64_t at) {
     else return Act<TYPE == KQ_T_BF16>::lo(((const uint16_t*)base)[at]);
 }
 // 4-byte aligned pieces of a stream that is written once and not read soon: past the caches' normal ways
-// (fp32 weights of 4096 x 25088 rebuilt: 75 us, 131 us with ordinary stores).  Only where a thread's values lie on their own
-// size: pieces of lines are slow that way (4096 x 25087: 134 us with ordinary stores, 182 streamed).
+// (fp32 weights of 4096 x 25088 rebuilt: 75 us, 131 us with ordinary stores).  Four values a thread only where they lie on
+// their own size: pieces of lines are slow that way (rebuilt from 4 bits, ordinary and streamed: 4096 x 25087 fp32 133 and 181
+// us, 4096 x 25090 bf16 56 and 128; rows that begin on their own size inside a line are as slow, 4096 x 25092 bf16 123).
+// Eight 16-bit values on any dword (checkpoints of 4096 x 25090 bf16 restored: 46.7 us, 52.9 with ordinary stores; 4096 x 25087
+// 47.3 and 54.6).
 __device__ __forceinline__ void stream_store(void* at, const unsigned* v, int words) {
     if (words == 4) {
         using u32x4_a4 = __attribute__((ext_vector_type(4), aligned(4))) unsigned;
@@ -61,7 +64,7 @@ __device__ __forceinline__ void store_values(void* base, int64_t at, const float
             unsigned h[N / 2];
 #pragma unroll
             for (int t = 0; t < N / 2; ++t) h[t] = Act<TYPE == KQ_T_BF16>::pack(v[2 * t], v[2 * t + 1]);
-            if (((uintptr_t)o & (2 * N - 1)) == 0) stream_store(o, h, N / 2);
+            if (((uintptr_t)o & (N == 8 ? 3 : 2 * N - 1)) == 0) stream_store(o, h, N / 2);
             else __builtin_memcpy(o, h, 2 * N);
         } else {
 #pragma unroll
