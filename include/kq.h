@@ -709,8 +709,9 @@ kq_status kq_checkpoint_grad_weight(const void* dY, int32_t type, int64_t ldy, i
  *   subnormal).  dw_type is any but KQ_T_E4M3.  dbias (fp32 [n], or NULL): sum_m dY[m][o], not quantized.
  *   Sums.  Where the output is fp32, and in kq_block_linear of up to 16 rows and of small products, products are exact and
  *   sums are fp32.  Otherwise the 8-bit matrix instruction adds them: eight products at a time, each cut off 13 bits below the
- *   largest of the eight (on random operands 1.5e-5 of the result's norm, where rounding to bf16 is 1.7e-3 and to
- *   fp16 2.1e-4), and the eights in fp32.  The order of a sum goes by the sizes alone.
+ *   largest of the eight (1.1e-5 to 4.1e-5 of the result's norm on what was measured, where rounding to bf16 is 1.7e-3 and
+ *   to fp16 2.1e-4), and the eights in fp32.  Which products are small and the order of a sum go by the sizes and the types
+ *   alone; so X and its 8-bit values may give other last bits.
  *   workspaces: the *_workspace_bytes of the same arguments (may be 0: ws may be NULL then).
  */
 #define KQ_T_E4M3 3

@@ -1459,8 +1459,8 @@ class BlockLinear:
     """A fully-connected layer in 8-bit floats: e4m3 values with a power of two for each 128 x 128 block, an fp32 master
     copy of the weight for training (master=True) and an fp32 bias or None, on the weight's device.
 
-    ``layer(X)`` is the serving call.  ``layer.forward(X)`` also returns the 8-bit values of X that
-    ``layer.backward(dY, kept)`` takes the weight's gradient from; ``layer.step`` moves the master copy and the bias
+    ``layer(X)`` is the serving call.  ``layer.forward(X)`` also returns the 8-bit values of X (its Y may have other last
+    bits) that ``layer.backward(dY, kept)`` takes the weight's gradient from; ``layer.step`` moves the master copy and the bias
     against them and quantizes the weight again.  Not an autograd function: an X that requires a gradient gets it
     from ``layer.backward``."""
 

@@ -12,9 +12,11 @@
 // read costs the product 1 to 5 %).
 //
 // Two forms.  The scaled 8-bit instruction takes the bytes and both exponents as they are, at twice the 16-bit rate;
-// it adds eight products at a time and cuts each off 13 bits below the largest of them.  That is 1.5e-5 of the
-// result's norm on random operands, which an output of 16 bits hides (its own rounding is 1.7e-3 or 2.1e-4) and
-// one of 32 does not: there the bytes are decoded to bf16 between LDS and the 16-bit instruction, which is exact.
+// it adds eight products at a time and cuts each off 13 bits below the largest of them.  That is 1.1e-5 to 1.5e-5 of the
+// result's norm on Gaussian operands and on activations after a ReLU, and 4.1e-5 in a weight's gradient from such activations
+// with rows of very different size (4096 deep); an output of 16 bits hides it (its own rounding is 1.7e-3 or 2.1e-4: 1 to
+// 2 % of 4096 x 4096 bf16 results are the neighbour of what exact sums round to) and one of 32 does not: there the bytes are
+// decoded to bf16 between LDS and the 16-bit instruction, which is exact.
 //
 // What bounds it.  4096 x 4096 x 25088 in 8 bits takes 310 to 335 us (2.5 to 2.7 PFLOP/s; torch's 8-bit product with one scale
 // for all reaches 2.9 at 8192^3, where this takes 415 to 425 us, 2.6): the clock falls to 1.86 GHz under it, the matrix
@@ -224,9 +226,10 @@ __global__ __launch_bounds__(64 * WI * WJ, 1) void block_gemm_kernel(const Block
     lb.init(p.B, j0, p.J, lane, wave);
     const uint8_t* const a_base = COLUMNS ? p.A.v : p.A.v + i0 * p.A.pitch;
     const uint8_t* const b_base = p.B.v + j0 * p.B.pitch;
-    // Exponents.  Of an operand with one a row a lane holds eight blocks' at a time, and takes the next eight two blocks
-    // before they are needed (one byte at a time each row's cache line came back for every block: 351 us instead of 318
-    // at 4096 x 4096 x 25088).  Of the 128 x 128 form lane l holds block l's of 64.  Blocks behind the last have 0.
+    // Exponents.  Of an operand with one a row a lane holds eight blocks' at a time, and loads the next eight four blocks
+    // before they are needed (a byte for each of the next two blocks, two blocks before, each row's cache line comes back again
+    // and again: 4096 x 4096 x 25088, of one operand 314 to 320 us instead of 303 to 308, of both, a weight's gradient,
+    // 477 to 490 instead of 402).  Of the 128 x 128 form lane l holds block l's of 64.  Blocks behind the last have 0.
     RowExponents<AROWS ? MI : 1> ea;
     RowExponents<MJ> eb;
     if constexpr (AROWS) ea.init(p.A, iw, p.I, r32, p.steps, b_end);
@@ -442,8 +445,10 @@ __global__ __launch_bounds__(64 * WI * WJ, 1) void block_gemm_kernel(const Block
 // CUs have one, `full` where all 256 have (the clock and the caches give way), and a CU with n of them n times `shared`; a
 // split contraction pays the joining launch and its partial sums, written and read at about 6 MB a us.  Where the tiles of
 // 256 x 256 are a little over a number of full rounds, the columns of the last one are a product of their own (98 x 16 tiles
-// of 4096 deep: six rounds and 128 small tiles instead of seven).  Fitted to sweeps, us for one output size with 4096 deep,
-// 8-bit / exact:
+// of 4096 deep: six rounds and 128 small tiles instead of seven).  What a whole contraction's results take to store is in the
+// fixed part, once however many rounds there are; so large results of one to four blocks take longer than it says (exact,
+// 25088 x 4096 of two blocks 115 us for 50, of four 177 for 90; 4096 x 4096 21 to 29 for 12, 28 for 19), and which tile is
+// the fastest there has not been measured.  Fitted to sweeps, all 4096 deep, us for one output size, 8-bit / exact:
 //   4096 x 256:  128x64 14.8 / 20.8, 128x128 18.1 / 21.5 (four splits), 256x256 28 / 33
 //   4096 x 1024: 128x64 25.5 / 38.3, 128x128 25.1 / 39.3, 256x256 40 / 51
 //   4096 x 2048: 128x64 50.6 / 71.0, 128x128 35.4 / 61.6, 256x256 52.7 / 75.8
